@@ -104,10 +104,19 @@ typedef enum {
  * cc_counter_causal_attention take bf16 only (CC_ERR_UNSUPPORTED).  The
  * scoring passes and the append attend over an exact bf16 copy of each
  * layer's codes, made in the workspace's activation buffer (which needs
- * 4 * Hkv * head_dim <= 2 * d_ff bytes per slot, else CC_ERR_UNSUPPORTED). */
+ * 4 * Hkv * head_dim <= 2 * d_ff bytes per slot, else CC_ERR_UNSUPPORTED).
+ *
+ * The block format keeps e4m3 codes too, with a scale of its own for every
+ * block of kv_block slots and KV head, K and V apart, held as one byte e: an
+ * element is code * 2^(e - 127).  A power of two costs a floating-point code no
+ * precision, makes an element exact in bf16 and lets a block that meets a
+ * larger value be rescaled exactly.  It is written by cc_kv_append and read by
+ * cc_kv_attention; the calls that run the model's layers themselves refuse it
+ * (CC_ERR_UNSUPPORTED). */
 typedef enum {
   CC_KV_BF16 = 0,
-  CC_KV_E4M3 = 1
+  CC_KV_E4M3 = 1,
+  CC_KV_E4M3_BLOCK = 2
 } cc_kv_format;
 
 /* Order of the cached K/V buffers of a (not paged) cache: slot-major
@@ -220,6 +229,14 @@ typedef struct {
    * kernels that do not need it.  Leave kv_ready NULL for calls recorded into a graph
    * (cc_graph_begin): the waits are for eager calls whose inputs are still arriving. */
   void *const *kv_ready;
+  /* CC_KV_E4M3_BLOCK: slots per scale (16, 32, 64 or 128, dividing cap) and HOST arrays
+   * [n_layers] of device uint8 scale exponents, ordered as the codes: a slot-major cache's
+   * [batch][cap / kv_block][Hkv], a paged one's [n_pages][page_size / kv_block][Hkv], a
+   * head-major one's [batch][Hkv][cap / kv_block].  e = 1 .. 254 stands for 2^(e - 127),
+   * 0 for a scale of 0 (e = 255 is not a number).  cc_kv_append writes 10 .. 247. */
+  int32_t kv_block;
+  void *const *k_exp;
+  void *const *v_exp;
 } cc_kv_cache;
 
 /* ---- scoring (Sec. 3.1) ---------------------------------------------------
@@ -420,6 +437,93 @@ cc_status cc_score_h2o(const cc_kv_cache *cache, int32_t recent, float *scores, 
 cc_status cc_compact_kv_static(const cc_model_cfg *cfg, const cc_kv_cache *cache,
                                const int32_t *keep_idx, const int32_t *keep_count,
                                void *stream);
+
+/* ---- one layer's serving step with the caller's projections -------------------
+ * The paper has no counterpart: the parts of cc_append_chunk that touch the
+ * cache, for a model whose projections are computed elsewhere.  Per layer
+ * cc_kv_append, then cc_kv_attention; after the last layer cc_kv_advance.
+ *
+ * New tokens are rows of packed buffers, sequence after sequence: rows
+ * [row_start[b], row_start[b + 1]) belong to sequence b and take its slots
+ * seq_len[b], seq_len[b] + 1, ...  A sequence whose rows are out of order, more
+ * than max_rows, past n_rows or past cap, or whose seq_len is outside [0, cap],
+ * is reported as CC_ERR_DEVICE_ARG and skipped (nothing of it is written).  A
+ * block-table entry outside the pool is reported and its slots are skipped.
+ * seq_len stays as it is until cc_kv_advance. */
+typedef enum { CC_BF16 = 0, CC_F16 = 1, CC_F32 = 2 } cc_dtype;
+
+typedef struct {
+  int32_t n_rows;            /* rows of the row buffers; 0: the call does nothing          */
+  int32_t max_rows;          /* rows of one sequence at most (1 <= max_rows <= n_rows)     */
+  const int32_t *row_start;  /* device int32 [batch + 1], or NULL: one row per sequence
+                                (n_rows == batch, max_rows == 1)                           */
+  const int32_t *pos;        /* device int32 [n_rows]: original positions (>= 0; a negative
+                                one is reported and taken as 0), or NULL: those following
+                                pos[b][seq_len[b] - 1] of the cache (from 0 when empty)    */
+} cc_rows;
+
+/* cc_kv_append -- rotates the rows' keys (rotate-half pairs, the angles of
+ * cfg) at their positions and writes keys and values into k[layer], v[layer],
+ * in any format and layout of the cache; with q, writes the rotated queries to
+ * q_out too (in place is fine).  rotate = 0 leaves q and k as they are.
+ *   k, v:  device [n_rows][Hkv * head_dim] of `dtype`, rows k_ld, v_ld elements apart;
+ *   q, q_out: device [n_rows][Hq * head_dim] of `dtype`, rows q_ld, q_out_ld apart, or both NULL.
+ * Pointers start on 16 bytes and rows lie a multiple of 16 bytes apart, so q, k
+ * and v may be columns of one projection's output.
+ * bf16 elements are rounded to nearest; e4m3 codes as in cc_append_chunk.
+ * Block format: a block's exponent is the least that holds its new values -- K
+ * by a bound of each pair's radius, which no rotation exceeds -- and, where it
+ * already holds this sequence's older slots, the exponent these have; when that
+ * grows, their codes are rescaled in place (rounded to nearest).  What lies past
+ * seq_len does not count.  Infinities and NaN take no part in the exponent and
+ * become the NaN code. */
+cc_status cc_kv_append(const cc_model_cfg *cfg, const cc_kv_cache *cache, int32_t layer,
+                       const cc_rows *rows, cc_dtype dtype, int32_t rotate, const void *k,
+                       int64_t k_ld, const void *v, int64_t v_ld, const void *q, int64_t q_ld,
+                       void *q_out, int64_t q_out_ld, void *stream);
+
+/* cc_kv_attention -- the rows' attention over one layer of a block-format cache
+ * (others: CC_ERR_UNSUPPORTED):
+ *   out[r][t] = softmax_j(q[r][t] . K[j] / sqrt(head_dim)) V[j],
+ * heads t reading KV head t / (Hq/Hkv).  The row of slot i sees slots j <= i,
+ * the appended ones among them; with memory_only != 0 the seq_len[b] slots of
+ * the memory alone, whatever follows them (then rows need not fit in cap).
+ *   q, out: device [n_rows][Hq * head_dim], bf16 or fp16 (`dtype`), rows q_ld,
+ *           out_ld elements apart, aligned as above;
+ *   lse:    device fp32 [n_rows][Hq], or NULL: ln sum_j exp(score_j), by which
+ *           results over disjoint slots join.
+ * A row that sees no slot gets 0 and -inf.  A row with a score that is NaN or
+ * infinite gets 0 (its lse is no finite number).  Slots that a row does not see
+ * may hold any bits.  Up to a few dozen query rows a KV head are
+ * bound by the cache's bytes; a chunk of more bf16 rows runs on tcgen05 over a
+ * bf16 copy of the layer in the workspace (exact). */
+size_t cc_kv_attention_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *cache,
+                                      const cc_rows *rows);
+cc_status cc_kv_attention(const cc_model_cfg *cfg, const cc_kv_cache *cache, int32_t layer,
+                          const cc_rows *rows, cc_dtype dtype, int32_t memory_only,
+                          const void *q, int64_t q_ld, void *out, int64_t out_ld, float *lse,
+                          void *ws, size_t ws_bytes, void *stream);
+
+/* cc_kv_advance -- ends a step: the rows' positions and, with tokens (device
+ * int32 [n_rows]), token ids into the cache's pos and tokens, then seq_len[b]
+ * grows by the sequence's rows. */
+cc_status cc_kv_advance(const cc_kv_cache *cache, const cc_rows *rows, const int32_t *tokens,
+                        void *stream);
+
+/* cc_token_logprobs -- what a step answers with, from each row's logits z
+ * (device [rows][vocab] of `dtype`, rows ld elements apart, any alignment of
+ * the type):
+ *   logprob[r]  = z[target] - lse,  lse = ln sum_j e^z_j      (targets != NULL)
+ *   entropy[r]  = -sum_j p_j ln p_j,  p = softmax(z)          (entropy != NULL)
+ *   top_ids[r][i], top_logprob[r][i], i < top: the largest logits in descending
+ *     order, ties to the lower id (either may be NULL; 0 <= top <= 32, <= vocab).
+ * -inf is a forbidden token: probability 0, no part of the entropy, ranked last
+ * by id.  A target of -1 means none (logprob 0); any other outside [0, vocab) is
+ * reported as CC_ERR_DEVICE_ARG (logprob 0).  A row that allows nothing, or that
+ * holds +inf or NaN, has log-probabilities and entropy NaN; NaN ranks as -inf. */
+cc_status cc_token_logprobs(const void *logits, cc_dtype dtype, int32_t rows, int32_t vocab,
+                            int64_t ld, const int32_t *targets, float *logprob, float *entropy,
+                            int32_t top, int32_t *top_ids, float *top_logprob, void *stream);
 
 /* ---- captured call sequences (CUDA graphs) -----------------------------------
  * The paper has no counterpart: this is a library convenience for

@@ -40,6 +40,12 @@ Parity status per function (what pins it, in tests/test_oracle_*.py):
   append_chunk             into an empty cache = causal_forward; chunk-by-chunk
                            appends = one append (no refresh between); the layer's
                            attention after a compaction by scalar brute force
+  rotate_rows              rope (pinned above) at the same positions
+  block_exponent           values the definition names; least exponent by search
+  append_blocks            one row at a time = all at once where no exponent grows;
+                           every written value within half a step; a scalar case
+  attend_rows              torch SDPA with an explicit mask (library routine)
+  token_logprobs           torch log_softmax, topk (library routines); scipy entropy
 The paper prints no worked example with score values, so no pin is a
 printed number; every step of the score is pinned by the checks above.
 """
@@ -51,3 +57,5 @@ from .refresh import (rms_norm, rope, rope_angles, rope_inv_freq, project, softm
                       key_attention_colsums, importance_scores, h2o_update, h2o_scores,
                       decode_step)
 from .fp8 import e4m3_decode, e4m3_encode, kv_quantize  # noqa: F401
+from .step import (append_blocks, attend_rows, block_exponent, k_bound, rotate_rows,  # noqa: F401
+                   token_logprobs, v_bound)

@@ -7,5 +7,5 @@ binding (one function per C entry point); `shard` splits one refresh over the
 ranks of a torch.distributed group by query rows.
 """
 from . import cc  # noqa: F401
-from .cc import (CCError, Cache, Weights, SCORE_LOGIT, SCORE_LOGPROB, model_cfg,  # noqa: F401
+from .cc import (CCError, Cache, Rows, Weights, SCORE_LOGIT, SCORE_LOGPROB, model_cfg,  # noqa: F401
                  load_library)

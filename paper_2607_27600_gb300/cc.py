@@ -68,9 +68,16 @@ class cc_kv_cache(ctypes.Structure):
                 ("kv_scale", ctypes.POINTER(ctypes.c_float)),
                 ("block_table", ctypes.c_void_p), ("page_size", ctypes.c_int32),
                 ("n_pages", ctypes.c_int32), ("kv_layout", ctypes.c_int32),
-                ("kv_ready", ctypes.POINTER(ctypes.c_void_p))]
+                ("kv_ready", ctypes.POINTER(ctypes.c_void_p)),
+                ("kv_block", ctypes.c_int32), ("k_exp", ctypes.POINTER(ctypes.c_void_p)),
+                ("v_exp", ctypes.POINTER(ctypes.c_void_p))]
 
-KV_BF16, KV_E4M3 = 0, 1
+
+class cc_rows(ctypes.Structure):
+    _fields_ = [("n_rows", ctypes.c_int32), ("max_rows", ctypes.c_int32),
+                ("row_start", ctypes.c_void_p), ("pos", ctypes.c_void_p)]
+
+KV_BF16, KV_E4M3, KV_E4M3_BLOCK = 0, 1, 2
 KV_SLOT_MAJOR, KV_HEAD_MAJOR = 0, 1
 
 
@@ -151,8 +158,24 @@ _SIGS = {
                                          ctypes.POINTER(ctypes.c_double)]),
     "cc_kernel_name": (ctypes.c_char_p, [ctypes.c_int32]),
     "cc_debug_withhold_compact_unit": (ctypes.c_int, [ctypes.c_int32]),
+    "cc_kv_append": (ctypes.c_int, [ctypes.POINTER(cc_model_cfg), ctypes.POINTER(cc_kv_cache),
+                                    ctypes.c_int32, ctypes.POINTER(cc_rows), ctypes.c_int,
+                                    ctypes.c_int32] + [ctypes.c_void_p, ctypes.c_int64] * 4
+                     + [ctypes.c_void_p]),
+    "cc_kv_attention_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(cc_model_cfg),
+                                                         ctypes.POINTER(cc_kv_cache),
+                                                         ctypes.POINTER(cc_rows)]),
+    "cc_kv_attention": (ctypes.c_int, [ctypes.POINTER(cc_model_cfg), ctypes.POINTER(cc_kv_cache),
+                                       ctypes.c_int32, ctypes.POINTER(cc_rows), ctypes.c_int,
+                                       ctypes.c_int32] + [ctypes.c_void_p, ctypes.c_int64] * 2
+                        + [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "cc_kv_advance": (ctypes.c_int, [ctypes.POINTER(cc_kv_cache), ctypes.POINTER(cc_rows),
+                                     ctypes.c_void_p, ctypes.c_void_p]),
+    "cc_token_logprobs": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int32,
+                                         ctypes.c_int32, ctypes.c_int64] + [ctypes.c_void_p] * 3
+                          + [ctypes.c_int32] + [ctypes.c_void_p] * 3),
 }
-KERNEL_COUNT = 19
+KERNEL_COUNT = 22
 
 
 def library_path() -> str:
@@ -267,8 +290,11 @@ class Cache:
     [B, cap, d] or None); with "block_table" (int32 [B, cap // page_size]),
     "page_size" and k[l], v[l] page pools [n_pages, page_size, Hkv, dh] the
     K/V are paged; with "kv_layout": KV_HEAD_MAJOR, k[l], v[l] are
-    [B, Hkv, cap, dh].  Keeps the tensors alive.  set_kv_ready() attaches the
-    per-layer events of K/V uploads still in flight on another stream."""
+    [B, Hkv, cap, dh].  With "kv_block" (16, 32, 64 or 128) and per layer uint8
+    scale exponents "k_exp", "v_exp" in the codes' order (one per kv_block slots
+    and KV head), k[l] and v[l] are codes of the block format.  Keeps the tensors
+    alive.  set_kv_ready() attaches the per-layer events of K/V uploads still in
+    flight on another stream."""
 
     def __init__(self, c: dict):
         self.d = c
@@ -284,6 +310,14 @@ class Cache:
                 raise ValueError("kv_scale needs one (K, V) pair per layer")
             self._scale = (ctypes.c_float * len(flat))(*flat)
             fmt = KV_E4M3
+        block, self._ke, self._ve = int(c.get("kv_block", 0)), None, None
+        if block:
+            if sc is not None:
+                raise ValueError("kv_block and kv_scale exclude each other")
+            fmt = KV_E4M3_BLOCK
+            self._check_block(c, block)
+            self._ke = (ctypes.c_void_p * len(ks))(*[_dev_ptr(x, "k_exp") for x in c["k_exp"]])
+            self._ve = (ctypes.c_void_p * len(vs))(*[_dev_ptr(x, "v_exp") for x in c["v_exp"]])
         table, page, n_pages = c.get("block_table"), 0, 0
         if table is not None:
             page = int(c["page_size"])
@@ -293,8 +327,24 @@ class Cache:
                              _dev_ptr(c.get("h_last"), "h_last"),
                              _dev_ptr(c.get("h2o_acc"), "h2o_acc"), fmt, self._scale,
                              _dev_ptr(table, "block_table"), page, n_pages,
-                             int(c.get("kv_layout", KV_SLOT_MAJOR)), None)
+                             int(c.get("kv_layout", KV_SLOT_MAJOR)), None, block, self._ke,
+                             self._ve)
         self._ready = None
+
+    @staticmethod
+    def _check_block(c, block):
+        """One scale exponent for each `block` slots and KV head of every layer."""
+        for name in ("k", "v"):
+            if len(c[name + "_exp"]) != len(c[name]):
+                raise ValueError(f"{name}_exp needs one tensor per layer")
+            for x, e in zip(c[name], c[name + "_exp"]):
+                if x is None:
+                    continue
+                if x.element_size() != 1 or e.dtype != torch.uint8:
+                    raise ValueError("the block format holds one-byte codes and uint8 exponents")
+                if e.numel() * block * x.shape[-1] != x.numel():
+                    raise ValueError(f"{name}_exp holds {e.numel()} exponents for {x.numel()} codes "
+                                     f"in blocks of {block}")
 
     def set_kv_ready(self, events):
         """events: one torch.cuda.Event (already recorded once) or None per
@@ -546,6 +596,125 @@ def cc_counter_causal_attention_split(q, k, v, seq_len, out, batch, cap, n_q_hea
         _dev_ptr(q, "q"), _dev_ptr(k, "k"), _dev_ptr(v, "v"), _dev_ptr(seq_len, "seq_len"),
         _dev_ptr(out, "out"), batch, cap, n_q_heads, n_kv_heads, head_dim, _stream(stream))
     _check(code, "cc_counter_causal_attention_split")
+
+
+# ---- one layer's serving step with the caller's projections -------------------
+
+DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}   # cc_dtype
+
+
+class Rows:
+    """cc_rows: new tokens as packed rows, sequence b's from row_start[b] (device
+    int32 [B + 1]; None: one row per sequence), at positions pos (device int32
+    [n_rows]; None: those following the cache's), at most max_rows of one
+    sequence.  Keeps the tensors alive."""
+
+    def __init__(self, n_rows: int, row_start=None, pos=None, max_rows: int = 1):
+        for t, n, name in ((row_start, None, "row_start"), (pos, n_rows, "pos")):
+            if t is not None and (t.dtype != torch.int32 or (n is not None and t.numel() != n)):
+                raise ValueError(f"{name} must be int32" + (f" of {n} elements" if n is not None else ""))
+        self.row_start, self.pos = row_start, pos
+        self.c = cc_rows(int(n_rows), int(max_rows), _dev_ptr(row_start, "row_start"),
+                         _dev_ptr(pos, "pos"))
+
+
+def _row_ptr(t, name, n_rows, width, dtype):
+    """(pointer, elements between rows) of a CUDA tensor [n_rows, heads, head_dim] (or
+    [n_rows, heads * head_dim]) whose rows are contiguous."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype}, not {dtype}")
+    shape, stride = t.shape, t.stride()
+    inner = 1
+    for i in range(t.dim() - 1, 0, -1):
+        if shape[i] != 1 and stride[i] != inner:
+            raise ValueError(f"{name}: the elements of a row must be contiguous")
+        inner *= shape[i]
+    if shape[0] != n_rows or inner != width:
+        raise ValueError(f"{name} has shape {tuple(shape)}; {n_rows} rows of {width} elements expected")
+    return t.data_ptr(), (stride[0] if n_rows > 1 else width)
+
+
+def _dtype(t, name):
+    code = DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be bf16, fp16 or fp32")
+    return code
+
+
+def cc_kv_append(cfg, cache: Cache, layer: int, rows: Rows, k, v, q=None, q_out=None,
+                 rotate: bool = True, stream=None):
+    """Rotates the rows' keys (and queries: q to q_out) at their positions and
+    writes keys and values into layer `layer` of the cache, after each
+    sequence's seq_len slots.  k, v: [n_rows, Hkv, dh], q, q_out: [n_rows, Hq, dh],
+    of one type, any 16-byte aligned pitch."""
+    c, n = _cfg(cfg), rows.c.n_rows
+    kv, hq = c.n_kv_heads * c.head_dim, c.n_q_heads * c.head_dim
+    args = (*_row_ptr(k, "k", n, kv, k.dtype), *_row_ptr(v, "v", n, kv, k.dtype),
+            *_row_ptr(q, "q", n, hq, k.dtype), *_row_ptr(q_out, "q_out", n, hq, k.dtype))
+    _check(load_library().cc_kv_append(c, cache.c, layer, rows.c, _dtype(k, "k"), 1 if rotate else 0,
+                                       *args, _stream(stream)), "cc_kv_append")
+
+
+def cc_kv_attention_workspace_size(cfg, cache: Cache, rows: Rows) -> int:
+    return int(load_library().cc_kv_attention_workspace_size(_cfg(cfg), cache.c, rows.c))
+
+
+def cc_kv_attention(cfg, cache: Cache, layer: int, rows: Rows, q, out, ws, lse=None,
+                    memory_only: bool = False, stream=None):
+    """Attention of the rows (q [n_rows, Hq, dh], bf16 or fp16) over layer `layer`
+    of a block-format cache into out; lse: fp32 [n_rows, Hq] or None.  The rows
+    see the slots up to their own, or with memory_only the seq_len slots alone."""
+    c, n = _cfg(cfg), rows.c.n_rows
+    hq = c.n_q_heads * c.head_dim
+    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != n * c.n_q_heads):
+        raise ValueError("lse must be fp32 [n_rows, Hq]")
+    _check(load_library().cc_kv_attention(
+        c, cache.c, layer, rows.c, _dtype(q, "q"), 1 if memory_only else 0,
+        *_row_ptr(q, "q", n, hq, q.dtype), *_row_ptr(out, "out", n, hq, q.dtype),
+        _dev_ptr(lse, "lse"), _dev_ptr(ws, "ws"), ws.numel() * ws.element_size(),
+        _stream(stream)), "cc_kv_attention")
+
+
+def cc_kv_advance(cache: Cache, rows: Rows, tokens=None, stream=None):
+    """Ends a step: positions and tokens (int32 [n_rows] or None) of the rows
+    into the cache, and seq_len grows."""
+    if tokens is not None and (tokens.dtype != torch.int32 or tokens.numel() != rows.c.n_rows):
+        raise ValueError(f"tokens must be int32 of {rows.c.n_rows} elements")
+    _check(load_library().cc_kv_advance(cache.c, rows.c, _dev_ptr(tokens, "tokens"),
+                                        _stream(stream)), "cc_kv_advance")
+
+
+def cc_token_logprobs(logits, targets=None, logprob=None, entropy=None, top_ids=None,
+                      top_logprob=None, stream=None):
+    """Of each row of logits [rows, vocab] (bf16, fp16 or fp32, any row pitch): the
+    log-probability of targets (int32 [rows]) into logprob, the entropy, and the
+    most likely ids [rows, top] with their log-probabilities.  Outputs are fp32
+    but the int32 ids; any may be None."""
+    if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
+        raise TypeError("logits must be a CUDA tensor")
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be [rows, vocab] with contiguous rows")
+    n, vocab = logits.shape
+    top = 0
+    for t, name, dtype in ((targets, "targets", torch.int32), (logprob, "logprob", torch.float32),
+                           (entropy, "entropy", torch.float32)):
+        if t is not None and (t.dtype != dtype or t.numel() != n):
+            raise ValueError(f"{name} must be {dtype} of {n} elements")
+    for t, name, dtype in ((top_ids, "top_ids", torch.int32), (top_logprob, "top_logprob", torch.float32)):
+        if t is None:
+            continue
+        if t.dtype != dtype or t.dim() != 2 or t.shape[0] != n or (top and t.shape[1] != top):
+            raise ValueError(f"{name} must be {dtype} [{n}, top]")
+        top = t.shape[1]
+    _check(load_library().cc_token_logprobs(
+        logits.data_ptr(), _dtype(logits, "logits"), n, vocab, logits.stride(0) if n > 1 else vocab,
+        _dev_ptr(targets, "targets"), _dev_ptr(logprob, "logprob"), _dev_ptr(entropy, "entropy"), top,
+        _dev_ptr(top_ids, "top_ids"), _dev_ptr(top_logprob, "top_logprob"), _stream(stream)),
+        "cc_token_logprobs")
 
 
 def cc_timing_enable(on: bool):

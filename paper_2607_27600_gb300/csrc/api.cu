@@ -25,6 +25,9 @@
 #include "gemm.cuh"
 #include "gemv.cuh"
 #include "keyattn.cuh"
+#include "kvappend.cuh"
+#include "kvattn.cuh"
+#include "logprob.cuh"
 #include "rowops.cuh"
 #include "select.cuh"
 #include "../../include/cc_kernels.h"
@@ -227,9 +230,8 @@ KvFmt kv_fmt(const cc_model_cfg *c, const cc_kv_cache *kv, int l) {
 }
 int kv_elem_bytes(const cc_kv_cache *kv) { return kv->kv_format == CC_KV_E4M3 ? 1 : 2; }
 
-// The cache's format fields: a known format; e4m3 needs finite positive
-// scales for every layer.
-bool kv_format_ok(const cc_model_cfg *c, const cc_kv_cache *kv) {
+// The cache's layout fields.
+bool kv_layout_ok(const cc_kv_cache *kv) {
   if (kv->kv_layout != CC_KV_SLOT_MAJOR && kv->kv_layout != CC_KV_HEAD_MAJOR) return false;
   if (kv->kv_layout == CC_KV_HEAD_MAJOR && kv->block_table) return false;   // not paged
   if (kv->block_table) {   // pages of whole 128-slot key tiles that divide cap
@@ -237,6 +239,14 @@ bool kv_format_ok(const cc_model_cfg *c, const cc_kv_cache *kv) {
         kv->n_pages < 1 || (uint64_t)kv->n_pages * kv->page_size >= (1ull << 31))
       return false;
   }
+  return true;
+}
+
+// The cache's format and layout fields: a known format; e4m3 needs finite
+// positive scales for every layer.  (The block format is not among them: only
+// a serving step's calls take it.)
+bool kv_format_ok(const cc_model_cfg *c, const cc_kv_cache *kv) {
+  if (!kv_layout_ok(kv)) return false;
   if (kv->kv_format == CC_KV_BF16) return true;
   if (kv->kv_format != CC_KV_E4M3 || !kv->kv_scale) return false;
   for (int i = 0; i < 2 * c->n_layers; ++i)
@@ -773,6 +783,7 @@ cc_status check_append_args(const cc_model_cfg *c, const cc_model_weights *w,
   if (!w || !kv || !w->layers || !w->embed || !kv->k || !kv->v || !tokens_in || max_count < 0 ||
       (!count && max_count != 1))   // no count array: one token each
     return CC_ERR_INVALID_ARG;
+  if (kv->kv_format == CC_KV_E4M3_BLOCK) return CC_ERR_UNSUPPORTED;
   if (kv->batch < 1 || kv->cap < 1 || !kv->seq_len || !kv->tokens || !kv->pos ||
       !kv_format_ok(c, kv))
     return CC_ERR_INVALID_ARG;
@@ -1111,6 +1122,7 @@ cc_status check_score_args(const cc_model_cfg *c, const cc_model_weights *w, con
       (mode & ~(0xFF | CC_SCORE_PRECISE | CC_SCORE_RANGE_ONLY | CC_SCORE_F16)) ||
       ((mode & CC_SCORE_PRECISE) && (mode & CC_SCORE_F16)))
     return CC_ERR_INVALID_ARG;
+  if (kv->kv_format == CC_KV_E4M3_BLOCK) return CC_ERR_UNSUPPORTED;
   if (kv->batch < 1 || kv->cap < 1 || !kv->seq_len || !kv->tokens || !kv->pos ||
       !kv_format_ok(c, kv))
     return CC_ERR_INVALID_ARG;
@@ -1339,6 +1351,7 @@ int g_withhold_unit = -1;   // cc_debug_withhold_compact_unit: consumed by the n
 cc_status compact_plan(const cc_model_cfg *c, const cc_kv_cache *kv, CompactPlan &plan) {
   cc_status s = check_cfg(c);
   if (s != CC_OK) return s;
+  if (kv && kv->kv_format == CC_KV_E4M3_BLOCK) return CC_ERR_UNSUPPORTED;
   if (!kv || kv->batch < 1 || kv->cap < 1 || !kv->k || !kv->v || !kv->tokens || !kv->pos ||
       !kv->seq_len || !kv_format_ok(c, kv))
     return CC_ERR_INVALID_ARG;
@@ -1760,6 +1773,219 @@ const char *cc_status_str(cc_status s) {
   return "unknown status";
 }
 
+// ---- one layer's serving step with the caller's projections --------------------
+
+namespace {
+
+// The fields of a call's cache and rows that every call reads.
+cc_status check_step(const cc_kv_cache *kv, const cc_rows *rows) {
+  if (!kv || !rows || kv->batch < 1 || kv->cap < 1 || !kv->seq_len) return CC_ERR_INVALID_ARG;
+  if ((uint64_t)kv->batch * kv->cap >= (1ull << 31)) return CC_ERR_UNSUPPORTED;
+  if (rows->n_rows < 0) return CC_ERR_INVALID_ARG;
+  if (rows->n_rows == 0) return CC_OK;
+  if (rows->max_rows < 1 || rows->max_rows > rows->n_rows) return CC_ERR_INVALID_ARG;
+  if (!rows->row_start && (rows->n_rows != kv->batch || rows->max_rows != 1))
+    return CC_ERR_INVALID_ARG;
+  return CC_OK;
+}
+
+bool block_size_ok(const cc_kv_cache *kv) {
+  const int b = kv->kv_block;
+  return (b == 16 || b == 32 || b == 64 || b == 128) && kv->cap % b == 0;
+}
+
+// One layer of a cache of any format and layout, ready to be read or written.
+cc_status check_layer(const cc_model_cfg *c, const cc_kv_cache *kv, int l) {
+  if (l < 0 || l >= c->n_layers || !kv->k || !kv->v || !kv->k[l] || !kv->v[l] ||
+      !aligned16(kv->k[l]) || !aligned16(kv->v[l]) || !kv_layout_ok(kv))
+    return CC_ERR_INVALID_ARG;
+  if (kv->kv_format == CC_KV_E4M3_BLOCK) {
+    if (!block_size_ok(kv) || !kv->k_exp || !kv->v_exp || !kv->k_exp[l] || !kv->v_exp[l])
+      return CC_ERR_INVALID_ARG;
+    return CC_OK;
+  }
+  return kv_format_ok(c, kv) ? CC_OK : CC_ERR_INVALID_ARG;
+}
+
+// Rows of `heads` heads: a pitch that holds them, on 16-byte boundaries.
+bool rows_ok(const cc_model_cfg *c, const void *p, int64_t ld, int heads, int bytes) {
+  return p && aligned16(p) && ld >= (int64_t)heads * c->head_dim && ld * bytes % 16 == 0;
+}
+
+StepRows step_rows(const cc_kv_cache *kv, const cc_rows *rows) {
+  return {rows->n_rows, rows->max_rows, kv->batch, kv->cap, rows->row_start, kv->seq_len};
+}
+
+// SMs that the attention's partial rows are sized for, so that the workspace
+// size needs no device.
+constexpr int kStepMaxSms = 160;
+
+KvAttnParams kv_attn_params(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows,
+                            int sms) {
+  KvAttnParams p{};
+  p.rows = step_rows(kv, rows);
+  p.block = kv->kv_block;
+  p.pg = kv_layout(c, kv);
+  p.hq = c->n_q_heads;
+  p.hkv = c->n_kv_heads;
+  p.head_dim = c->head_dim;
+  p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)c->head_dim));
+  kv_attn_plan(p, std::min(sms, kStepMaxSms));
+  return p;
+}
+
+}  // namespace
+
+cc_status cc_kv_append(const cc_model_cfg *cfg, const cc_kv_cache *kv, int32_t layer,
+                       const cc_rows *rows, cc_dtype dtype, int32_t rotate, const void *k,
+                       int64_t k_ld, const void *v, int64_t v_ld, const void *q, int64_t q_ld,
+                       void *q_out, int64_t q_out_ld, void *stream) {
+  cc_status s = check_cfg(cfg);
+  if (s == CC_OK) s = check_step(kv, rows);
+  if (s == CC_OK) s = check_layer(cfg, kv, layer);
+  if (s != CC_OK) return s;
+  if (dtype != CC_BF16 && dtype != CC_F16 && dtype != CC_F32) return CC_ERR_INVALID_ARG;
+  if (rows->n_rows == 0) return CC_OK;
+  const int bytes = dtype == CC_F32 ? 4 : 2;
+  if (!rows_ok(cfg, k, k_ld, cfg->n_kv_heads, bytes) || !rows_ok(cfg, v, v_ld, cfg->n_kv_heads, bytes))
+    return CC_ERR_INVALID_ARG;
+  if ((q || q_out) && (!rows_ok(cfg, q, q_ld, cfg->n_q_heads, bytes) ||
+                       !rows_ok(cfg, q_out, q_out_ld, cfg->n_q_heads, bytes)))
+    return CC_ERR_INVALID_ARG;
+  if (rotate && !rows->pos && !kv->pos) return CC_ERR_INVALID_ARG;
+  DevState *dev;
+  if (!dev_state(&dev)) return device_fail();
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  KvAppendParams p{};
+  p.rows = step_rows(kv, rows);
+  p.pos = rows->pos;
+  p.cache_pos = kv->pos;
+  p.k = k;
+  p.v = v;
+  p.q = q;
+  p.q_out = q_out;
+  p.k_ld = k_ld;
+  p.v_ld = v_ld;
+  p.q_ld = q_ld;
+  p.q_out_ld = q_out_ld;
+  p.dtype = dtype;
+  p.kc = kv->k[layer];
+  p.vc = kv->v[layer];
+  p.format = kv->kv_format;
+  p.block = 32;
+  p.k_qscale = p.v_qscale = 1.f;
+  if (kv->kv_format == CC_KV_E4M3_BLOCK) {
+    p.ke = reinterpret_cast<uint8_t *>(kv->k_exp[layer]);
+    p.ve = reinterpret_cast<uint8_t *>(kv->v_exp[layer]);
+    p.block = kv->kv_block;
+  } else if (kv->kv_format == CC_KV_E4M3) {
+    p.k_qscale = 1.f / kv->kv_scale[2 * layer];
+    p.v_qscale = 1.f / kv->kv_scale[2 * layer + 1];
+  }
+  p.pg = kv_layout(cfg, kv);
+  p.hq = cfg->n_q_heads;
+  p.hkv = cfg->n_kv_heads;
+  p.head_dim = cfg->head_dim;
+  p.rotate = rotate ? 1 : 0;
+  if (p.rotate) rope_turns(cfg, p.turns);
+  p.status = dev->status;
+  CC_TRY(wait_kv_ready(kv, layer, layer + 1, st));
+  TimedScope t(CC_KERNEL_KV_APPEND, st);
+  CC_TRY(launch_kv_append(p, dev->sms, st));
+  return CC_OK;
+}
+
+size_t cc_kv_attention_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *kv,
+                                      const cc_rows *rows) {
+  if (check_cfg(cfg) != CC_OK || check_step(kv, rows) != CC_OK || rows->n_rows == 0) return 0;
+  return align256(kv_attn_part_bytes(kv_attn_params(cfg, kv, rows, kStepMaxSms)));
+}
+
+cc_status cc_kv_attention(const cc_model_cfg *cfg, const cc_kv_cache *kv, int32_t layer,
+                          const cc_rows *rows, cc_dtype dtype, int32_t memory_only, const void *q,
+                          int64_t q_ld, void *out, int64_t out_ld, float *lse, void *ws,
+                          size_t ws_bytes, void *stream) {
+  cc_status s = check_cfg(cfg);
+  if (s == CC_OK) s = check_step(kv, rows);
+  if (s == CC_OK) s = check_layer(cfg, kv, layer);
+  if (s != CC_OK) return s;
+  if (kv->kv_format != CC_KV_E4M3_BLOCK || dtype == CC_F32) return CC_ERR_UNSUPPORTED;
+  if (dtype != CC_BF16 && dtype != CC_F16) return CC_ERR_INVALID_ARG;
+  if (rows->n_rows == 0) return CC_OK;
+  if (!rows_ok(cfg, q, q_ld, cfg->n_q_heads, 2) || !rows_ok(cfg, out, out_ld, cfg->n_q_heads, 2))
+    return CC_ERR_INVALID_ARG;
+  if (!ws || !aligned16(ws) || ws_bytes < cc_kv_attention_workspace_size(cfg, kv, rows))
+    return CC_ERR_WORKSPACE;
+  DevState *dev;
+  if (!dev_state(&dev)) return device_fail();
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  KvAttnParams p = kv_attn_params(cfg, kv, rows, dev->sms);
+  p.memory_only = memory_only ? 1 : 0;
+  p.f16 = dtype == CC_F16 ? 1 : 0;
+  p.q = q;
+  p.out = out;
+  p.q_ld = q_ld;
+  p.out_ld = out_ld;
+  p.lse = lse;
+  p.k = reinterpret_cast<const uint8_t *>(kv->k[layer]);
+  p.v = reinterpret_cast<const uint8_t *>(kv->v[layer]);
+  p.ke = reinterpret_cast<const uint8_t *>(kv->k_exp[layer]);
+  p.ve = reinterpret_cast<const uint8_t *>(kv->v_exp[layer]);
+  p.status = dev->status;
+  p.part_o = reinterpret_cast<float *>(ws);
+  p.part_ml = reinterpret_cast<float4 *>(p.part_o + (size_t)2 * p.ctas * 8 * p.nt * p.head_dim);
+  CC_TRY(wait_kv_ready(kv, layer, layer + 1, st));
+  TimedScope t(CC_KERNEL_KV_ATTENTION, st);
+  CC_TRY(launch_kv_attn(p, st));
+  return CC_OK;
+}
+
+cc_status cc_kv_advance(const cc_kv_cache *kv, const cc_rows *rows, const int32_t *tokens,
+                        void *stream) {
+  const cc_status s = check_step(kv, rows);
+  if (s != CC_OK) return s;
+  if (!kv->pos || (tokens && !kv->tokens)) return CC_ERR_INVALID_ARG;
+  if (rows->n_rows == 0) return CC_OK;
+  DevState *dev;
+  if (!dev_state(&dev)) return device_fail();
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  TimedScope t(CC_KERNEL_KV_APPEND, st);
+  CC_TRY(launch_kv_advance(step_rows(kv, rows), rows->pos, tokens, kv->seq_len, kv->tokens, kv->pos,
+                           dev->status, st));
+  return CC_OK;
+}
+
+cc_status cc_token_logprobs(const void *logits, cc_dtype dtype, int32_t rows, int32_t vocab,
+                            int64_t ld, const int32_t *targets, float *logprob, float *entropy,
+                            int32_t top, int32_t *top_ids, float *top_logprob, void *stream) {
+  if (dtype != CC_BF16 && dtype != CC_F16 && dtype != CC_F32) return CC_ERR_INVALID_ARG;
+  if (rows < 0 || vocab < 1 || ld < vocab || top < 0 || top > vocab) return CC_ERR_INVALID_ARG;
+  if (top > kMaxTop) return CC_ERR_UNSUPPORTED;
+  if ((targets == nullptr) != (logprob == nullptr)) return CC_ERR_INVALID_ARG;
+  if (rows == 0) return CC_OK;
+  if (!logits || reinterpret_cast<uintptr_t>(logits) % (dtype == CC_F32 ? 4 : 2))
+    return CC_ERR_INVALID_ARG;
+  DevState *dev;
+  if (!dev_state(&dev)) return device_fail();
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  LogprobParams p{};
+  p.logits = logits;
+  p.dtype = dtype;
+  p.rows = rows;
+  p.vocab = vocab;
+  p.ld = ld;
+  p.targets = targets;
+  p.logprob = logprob;
+  p.entropy = entropy;
+  p.top = top_ids || top_logprob ? top : 0;
+  p.top_ids = top_ids;
+  p.top_logprob = top_logprob;
+  p.status = dev->status;
+  TimedScope t(CC_KERNEL_TOKEN_LOGPROB, st);
+  CC_TRY(launch_token_logprobs(p, dev->sms, st));
+  return CC_OK;
+}
+
 // ---- kernel-level entry points (include/cc_kernels.h) ----------------------
 
 cc_status cc_linear_f32(const void *x, const void *w, float *y, int32_t rows, int32_t n,
@@ -1911,7 +2137,8 @@ const char *cc_kernel_name(int32_t kind) {
   static const char *names[CC_KERNEL_COUNT] = {
       "rmsnorm", "embed", "gemm_qrope", "attention", "gemm_oproj", "gemm_gateup", "gemm_down",
       "head_logit", "gemm_lmhead", "lse_combine", "select", "compact", "other",
-      "gemm_kv", "attention_causal", "append", "gemm_qkv", "keyattn", "kv_dequant"};
+      "gemm_kv", "attention_causal", "append", "gemm_qkv", "keyattn", "kv_dequant",
+      "kv_append", "kv_attention", "token_logprob"};
   return (kind >= 0 && kind < CC_KERNEL_COUNT) ? names[kind] : "unknown";
 }
 
