@@ -448,7 +448,8 @@ cc_status cc_compact_kv_static(const cc_model_cfg *cfg, const cc_kv_cache *cache
  * seq_len[b], seq_len[b] + 1, ...  A sequence whose rows are out of order, more
  * than max_rows, past n_rows or past cap, or whose seq_len is outside [0, cap],
  * is reported as CC_ERR_DEVICE_ARG and skipped (nothing of it is written).  A
- * block-table entry outside the pool is reported and its slots are skipped.
+ * block-table entry outside the pool is reported too: its slots are not written,
+ * and attention leaves them out or sets the rows that would see them to 0.
  * seq_len stays as it is until cc_kv_advance. */
 typedef enum { CC_BF16 = 0, CC_F16 = 1, CC_F32 = 2 } cc_dtype;
 
@@ -494,9 +495,9 @@ cc_status cc_kv_append(const cc_model_cfg *cfg, const cc_kv_cache *cache, int32_
  *           results over disjoint slots join.
  * A row that sees no slot gets 0 and -inf.  A row with a score that is NaN or
  * infinite gets 0 (its lse is no finite number).  Slots that a row does not see
- * may hold any bits.  Up to a few dozen query rows a KV head are
- * bound by the cache's bytes; a chunk of more bf16 rows runs on tcgen05 over a
- * bf16 copy of the layer in the workspace (exact). */
+ * may hold any bits.  Chunks of more than a few dozen query rows a KV head run on
+ * tcgen05 over a bf16 copy of the layer in the workspace (exact; fp16 rows as
+ * bf16 pairs), which the workspace size includes. */
 size_t cc_kv_attention_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *cache,
                                       const cc_rows *rows);
 cc_status cc_kv_attention(const cc_model_cfg *cfg, const cc_kv_cache *cache, int32_t layer,

@@ -1834,6 +1834,97 @@ KvAttnParams kv_attn_params(const cc_model_cfg *c, const cc_kv_cache *kv, const 
   return p;
 }
 
+// Whether a step's rows take the tile attention: chunks, of so many query rows
+// per KV head and sequence on average.
+constexpr int kTileRows = 64, kTileMinRows = 16;
+bool step_on_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows) {
+  const long long group = c->n_q_heads / c->n_kv_heads;
+  return rows->row_start && rows->max_rows >= kTileMinRows &&
+         rows->n_rows * group >= (long long)kTileRows * kv->batch;
+}
+
+// Workspace of the tile attention: the layer as bf16, the sequences' rows, fp16
+// queries as pairs, and the partial rows of key splits.
+struct StepTileWs {
+  size_t k, v, lo, hi, base, pairs, part_o, part_ml, total;
+};
+StepTileWs step_tile_layout(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows) {
+  StepTileWs w{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off = align256(off + bytes); return o; };
+  const size_t copy = (size_t)kv->batch * kv->cap * c->n_kv_heads * c->head_dim * 2;
+  w.k = take(copy);
+  w.v = take(copy);
+  w.lo = take((size_t)kv->batch * 4);
+  w.hi = take((size_t)kv->batch * 4);
+  w.base = take((size_t)kv->batch * 4);
+  w.pairs = take((size_t)rows->n_rows * c->n_q_heads * c->head_dim * 4);
+  w.part_o = take((size_t)kAttnMaxSplitSlots * 256 * c->head_dim * 4);
+  w.part_ml = take((size_t)kAttnMaxSplitSlots * 256 * 8);
+  w.total = off;
+  return w;
+}
+
+// The rows' attention as tiles of 256 query rows (attn.cu) over a bf16 copy of
+// the layer; fp16 rows as bf16 pairs, P as pairs too (twice the products).
+cc_status run_step_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows,
+                         const KvAttnParams &kp, void *ws, int sms, cudaStream_t st) {
+  const StepTileWs L = step_tile_layout(c, kv, rows);
+  uint8_t *w = reinterpret_cast<uint8_t *>(ws);
+  auto ints = [&](size_t o) { return reinterpret_cast<int32_t *>(w + o); };
+  const KvTileRows tr{ints(L.lo), ints(L.hi), ints(L.base)};
+  const int dh = c->head_dim, G = c->n_q_heads / c->n_kv_heads, P = attn_positions_per_unit(G);
+  const uint64_t R = (uint64_t)kv->batch * kv->cap;
+  {
+    TimedScope t(CC_KERNEL_KV_DEQUANT, st);
+    CC_TRY(launch_kv_block_copy(kp, w + L.k, w + L.v, tr, st));
+    if (kp.f16) CC_TRY(launch_kv_split_rows(kp, w + L.pairs, st));
+  }
+  CUtensorMap tq, tk, tv;
+  {
+    const uint64_t heads = (uint64_t)c->n_q_heads * (kp.f16 ? 2 : 1);
+    const uint64_t ld = kp.f16 ? heads * dh : (uint64_t)kp.q_ld;
+    const uint64_t dims[3] = {(uint64_t)dh, heads, (uint64_t)rows->n_rows};
+    const uint64_t strides[2] = {(uint64_t)dh * 2, ld * 2};
+    const uint32_t box[3] = {64, (uint32_t)G, (uint32_t)P};
+    if (!make_tmap(&tq, kp.f16 ? w + L.pairs : kp.q, 3, dims, strides, box)) return tmap_fail();
+  }
+  const uint64_t dims[3] = {(uint64_t)dh, (uint64_t)c->n_kv_heads, R};
+  const uint64_t strides[2] = {(uint64_t)dh * 2, (uint64_t)c->n_kv_heads * dh * 2};
+  const uint32_t box[3] = {64, 1, 128};
+  if (!make_tmap(&tk, w + L.k, 3, dims, strides, box) || !make_tmap(&tv, w + L.v, 3, dims, strides, box))
+    return tmap_fail();
+  AttnParams p{};
+  p.batch = kv->batch;
+  p.cap = kv->cap;
+  p.n_q_heads = c->n_q_heads;
+  p.n_kv_heads = c->n_kv_heads;
+  p.head_dim = dh;
+  p.group = G;
+  p.P = P;
+  p.seq_len = tr.hi;
+  p.out = reinterpret_cast<__nv_bfloat16 *>(kp.out);
+  p.out_ld = (int)kp.out_ld;
+  p.q_split = kp.f16;
+  p.scale_log2 = kp.scale_log2;
+  p.v_scale = 1.f;
+  p.pg.hkv = c->n_kv_heads;
+  p.kv_rows = (int)R;
+  p.status = kp.status;
+  p.causal = 1;
+  p.row_lo = tr.lo;
+  p.pbase = tr.base;
+  p.key_end = kp.memory_only ? tr.lo : nullptr;
+  p.lse = kp.lse;
+  p.q_span = rows->max_rows;
+  p.kv_splits = attn_key_splits(attn_units(p), kv->cap, sms);
+  p.part_o = reinterpret_cast<float *>(w + L.part_o);
+  p.part_ml = reinterpret_cast<float2 *>(w + L.part_ml);
+  CC_TRY(launch_attention(tq, tk, tv, p, st));
+  if (!kp.memory_only) CC_TRY(launch_kv_restore_nan(kp, st));
+  return CC_OK;
+}
+
 }  // namespace
 
 cc_status cc_kv_append(const cc_model_cfg *cfg, const cc_kv_cache *kv, int32_t layer,
@@ -1898,6 +1989,7 @@ cc_status cc_kv_append(const cc_model_cfg *cfg, const cc_kv_cache *kv, int32_t l
 size_t cc_kv_attention_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *kv,
                                       const cc_rows *rows) {
   if (check_cfg(cfg) != CC_OK || check_step(kv, rows) != CC_OK || rows->n_rows == 0) return 0;
+  if (step_on_tiles(cfg, kv, rows)) return step_tile_layout(cfg, kv, rows).total;
   return align256(kv_attn_part_bytes(kv_attn_params(cfg, kv, rows, kStepMaxSms)));
 }
 
@@ -1932,9 +2024,13 @@ cc_status cc_kv_attention(const cc_model_cfg *cfg, const cc_kv_cache *kv, int32_
   p.ke = reinterpret_cast<const uint8_t *>(kv->k_exp[layer]);
   p.ve = reinterpret_cast<const uint8_t *>(kv->v_exp[layer]);
   p.status = dev->status;
-  p.part_o = reinterpret_cast<float *>(ws);
-  p.part_ml = reinterpret_cast<float4 *>(p.part_o + (size_t)2 * p.ctas * 8 * p.nt * p.head_dim);
   CC_TRY(wait_kv_ready(kv, layer, layer + 1, st));
+  if (step_on_tiles(cfg, kv, rows)) {
+    if (out_ld > 0x7FFFFFFF) return CC_ERR_UNSUPPORTED;
+    TimedScope t(CC_KERNEL_KV_ATTENTION, st);
+    return run_step_tiles(cfg, kv, rows, p, ws, dev->sms, st);
+  }
+  kv_attn_bind(p, ws);
   TimedScope t(CC_KERNEL_KV_ATTENTION, st);
   CC_TRY(launch_kv_attn(p, st));
   return CC_OK;

@@ -29,7 +29,11 @@
 // codes (made by the caller), its K scale folded into the softmax scale and
 // its V scale into the output normalisation.
 //
-// SPLIT (the precise scoring pass over a bf16 cache): the queries arrive as
+// With key_end (a serving step's attention over the memory alone) every row of
+// CAUSAL sees the slots [0, key_end): the rows' own slots lie past them.
+//
+// SPLIT (the precise scoring pass over a bf16 cache; causal: a serving step's fp16
+// rows, which a bf16 pair holds exactly, with fp16 output): the queries arrive as
 // bf16 pairs hi + lo (hi = bf16(q), lo = bf16(q - hi)), so S = Q_hi K^T +
 // Q_lo K^T accumulates both products in TMEM, and P is handed to P V as the
 // pair P_hi (TMEM columns [0, 64) of the S block) + P_lo (columns [64, 128)),
@@ -77,6 +81,12 @@ CC_DEV float fast_exp2(float x) {
   return y;
 }
 
+
+// ln of the sum of e^score of a row with reference max m of the raw scores and
+// row sum l (sl2: log2(e) times the score scale); -inf for a row that sees no key.
+CC_DEV float row_lse(float m, float l, float sl2) {
+  return l == 0.f ? -INFINITY : (m * sl2 + log2f(l)) * 0.69314718055994531f;
+}
 
 template <int DH, bool SPLIT = false>
 struct AttnSmem {
@@ -134,7 +144,9 @@ CC_DEV UnitInfo decode_unit(const AttnParams &p, int unit_id, bool causal) {
   u.q_lo = (causal || p.row_lo) ? p.row_lo[u.b] : 0;
   // query rows end: the sequence end, or a counter-causal row range's end
   const int q_hi = (!causal && p.row_hi) ? p.row_hi[u.b] : u.n;
-  u.bad = u.n < 0 || u.n > p.cap || u.q_lo < 0 || u.q_lo > q_hi || q_hi > u.n;
+  // (with key_end the rows' slots lie past the keys and need not fit)
+  u.bad = u.n < 0 || (u.n > p.cap && !(causal && p.key_end)) || u.q_lo < 0 || u.q_lo > q_hi ||
+          q_hi > u.n;
   u.p0 = u.q_lo + pb * p.P;
   u.valid = !u.bad && u.p0 < q_hi;
   u.p_last = min(u.p0 + p.P, q_hi) - 1;
@@ -153,6 +165,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                 const __grid_constant__ CUtensorMap tmV, const __grid_constant__ AttnParams p) {
   using L = AttnSmem<DH, SPLIT>;
+  constexpr bool OUT_F16 = F16 || (SPLIT && CAUSAL);
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                               ~uintptr_t(1023));
@@ -181,10 +194,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     return;
   }
   if (!u.valid) return;                      // the whole block lies past the sequence end
-  const int b = u.b, g = u.g, n = u.n, p0 = u.p0, p_last = u.p_last;
+  const int b = u.b, g = u.g, p0 = u.p0, p_last = u.p_last;
+  const int n = CAUSAL && p.key_end ? p.key_end[b] : u.n;   // end of the keys
   // counter-causal: key tiles holding slots p0+1 .. n-1; causal: slots 0 .. p_last
   const int t0 = CAUSAL ? 0 : (p0 + 1) / BKV;
-  const int t1 = CAUSAL ? p_last / BKV : (n - 1) / BKV;
+  const int t1 = !CAUSAL ? (n - 1) / BKV : n > 0 ? min(p_last, n - 1) / BKV : -1;
   const int ntiles_unit = t1 - t0 + 1;
   const size_t row_base = (size_t)slot0_row<CAUSAL>(p, u);   // (modulo 2^64: rows add back)
   // this CTA's share of the unit's key tiles (all of them without splits):
@@ -216,6 +230,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       int pos = p0 + idx / G, hl = idx % G;
       __nv_bfloat16 *o = p.out + (row_base + pos) * p.out_ld + (size_t)(g * G + hl) * DH;
       for (int v = 0; v < DH / 8; ++v) reinterpret_cast<uint4 *>(o)[v] = make_uint4(0, 0, 0, 0);
+      if (CAUSAL && p.lse) p.lse[(row_base + pos) * p.n_q_heads + g * G + hl] = -INFINITY;
       if (p.out_lo > 0)
         for (int v = 0; v < DH / 8; ++v)
           reinterpret_cast<uint4 *>(o + p.out_lo)[v] = make_uint4(0, 0, 0, 0);
@@ -469,7 +484,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
       for (int u = 0; u < 8; ++u) mp[u] = -INFINITY;
       // uniform over the CTA: rows past P*G have zero queries and need no mask
-      const bool need_mask = CAUSAL ? (j0 + BKV - 1 > p0) : ((j0 <= p0 + P - 1) || (j0 + BKV > n));
+      const bool need_mask = CAUSAL ? (j0 + BKV - 1 > min(p0, n - 1))
+                                    : ((j0 <= p0 + P - 1) || (j0 + BKV > n));
       if (need_mask) {
         // counter-causal: key j kept iff pos < j < n; causal: iff j <= min(pos, n - 1)
         const int lo = CAUSAL ? -1 : pos - j0;                    // keep c > lo
@@ -562,6 +578,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc_fence_after();
       const bool store = row_used && pos <= p_last;
       const float inv = l > 0.f ? p.v_scale / l : 0.f;   // V scale: e4m3 cache (else 1)
+      if (CAUSAL && p.lse && store)
+        p.lse[(row_base + pos) * p.n_q_heads + g * G + hl] = row_lse(m_used, l, sl2);
       __nv_bfloat16 *dst =
           p.out + (row_base + (store ? pos : p0)) * p.out_ld + (size_t)(g * G + hl) * DH;
 #pragma unroll 1
@@ -572,8 +590,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t pk[16];
 #pragma unroll
         for (int k = 0; k < 32; k += 2)
-          pk[k / 2] = F16 ? pack_f16x2(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv)
-                          : pack_bf16x2(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv);
+          pk[k / 2] = OUT_F16 ? pack_f16x2(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv)
+                              : pack_bf16x2(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv);
         if (store) {
           uint4 *d = reinterpret_cast<uint4 *>(dst + c);
 #pragma unroll
@@ -611,7 +629,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // chunk) took 19 us with a block and a barrier chain per row.
 constexpr int kCombineWarps = 8;
 
-template <int DH, bool CAUSAL>
+template <int DH, bool CAUSAL, bool OUT_F16>
 __global__ void __launch_bounds__(kCombineWarps * 32)
     attn_combine_kernel(const __grid_constant__ AttnParams p) {
   constexpr int DPL = DH / 32;
@@ -666,12 +684,16 @@ __global__ void __launch_bounds__(kCombineWarps * 32)
     m = mx;
   }
   const float inv = l > 0.f ? p.v_scale / l : 0.f;
+  if (CAUSAL && p.lse && lane == 0)
+    p.lse[(slot0_row<CAUSAL>(p, u) + pos) * p.n_q_heads + u.g * G + hl] = row_lse(m, nan ? NAN : l, c);
   __nv_bfloat16 *dst = p.out + (size_t)(slot0_row<CAUSAL>(p, u) + pos) * p.out_ld +
                        (size_t)(u.g * G + hl) * DH + lane * DPL;
 #pragma unroll
   for (int e = 0; e < DPL; e += 2)
     *reinterpret_cast<uint32_t *>(dst + e) =
-        l > 0.f && !nan ? pack_bf16x2(o[e] * inv, o[e + 1] * inv) : 0u;
+        !(l > 0.f) || nan ? 0u
+        : OUT_F16         ? pack_f16x2(o[e] * inv, o[e + 1] * inv)
+                          : pack_bf16x2(o[e] * inv, o[e + 1] * inv);
 }
 
 template <int DH, bool CAUSAL, bool SPLIT = false, bool F16 = false>
@@ -711,8 +733,8 @@ cudaError_t launch_dh(const CUtensorMap &q, const CUtensorMap &k, const CUtensor
   if (S > 1) {
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    if (p.out_lo > 0 || F16) return cudaErrorInvalidValue;   // splits: the append's bf16 rows only
-    return launch_pdl(attn_combine_kernel<DH, CAUSAL>, dim3(256 / kCombineWarps, (unsigned)units),
+    if (p.out_lo > 0 || F16) return cudaErrorInvalidValue;   // splits: an append's rows only
+    return launch_pdl(attn_combine_kernel<DH, CAUSAL, SPLIT && CAUSAL>, dim3(256 / kCombineWarps, (unsigned)units),
                       dim3(kCombineWarps * 32), 0, stream, pp);
   }
   return cudaGetLastError();
@@ -1145,7 +1167,10 @@ cudaError_t launch_attention(const CUtensorMap &q, const CUtensorMap &k, const C
     if (p.head_dim == 64) return launch_dh<64, false, false, true>(q, k, v, p, stream);
     return cudaErrorInvalidValue;
   }
-  if (p.causal) {
+  if (p.causal && p.q_split) {   // fp16 rows of a serving step
+    if (p.head_dim == 128) return launch_dh<128, true, true>(q, k, v, p, stream);
+    if (p.head_dim == 64) return launch_dh<64, true, true>(q, k, v, p, stream);
+  } else if (p.causal) {
     if (p.head_dim == 128) return launch_dh<128, true>(q, k, v, p, stream);
     if (p.head_dim == 64) return launch_dh<64, true>(q, k, v, p, stream);
   } else if (p.q_split) {   // the precise scoring pass

@@ -12,9 +12,10 @@ struct AttnParams {
   __nv_bfloat16 *out;       // row r, head t at out + r*out_ld + t*head_dim
   int out_ld;               // elements per output row (n_q_heads*head_dim, or twice that)
   int out_lo;               // > 0: also write lo = bf16(o - hi) at element offset out_lo
-  int q_split;              // counter-causal, bf16 cache: Q rows are [hi | lo] bf16 pairs
+  int q_split;              // bf16 K and V: Q rows are [hi | lo] bf16 pairs
                             // (the Q map spans 2 * n_q_heads heads, lo at head n_q_heads + t):
-                            // S = Q_hi K^T + Q_lo K^T, and P enters P V as hi + lo too
+                            // S = Q_hi K^T + Q_lo K^T, and P enters P V as hi + lo too; causal:
+                            // the pairs are fp16 values, and so is the output
   float scale_log2;         // log2(e) / sqrt(head_dim)
   int streams_per_group;    // unit order (set by launch_attention): see attn.cu
   int causal;               // 0: counter-causal (rows [0, n) attend (i, n)); 1: causal over
@@ -28,6 +29,9 @@ struct AttnParams {
   const int32_t *pbase;     // causal: null (query and output rows b * cap + slot) or device
                             // [batch]: packed rows, slot i of sequence b at row
                             // pbase[b] + i - row_lo[b]
+  const int32_t *key_end;   // causal: null, or device [batch]: every row sees the slots [0, key_end[b])
+                            // and no others (its own slot, past them, only names its row)
+  float *lse;               // causal: null, or [row][n_q_heads]: ln of the sum of e^score
   int q_span;               // query slots per sequence at most (cap, or the chunk size)
   int kv_splits;            // > 1: each unit's key tiles split over kv_splits CTAs (few units)
   float *part_o;            // kv_splits > 1: [unit][split][256 rows][head_dim] unnormalised O

@@ -18,11 +18,14 @@
 // for the CTAs of one resident wave, so that ragged batches balance; a unit that
 // spans shares is joined by kv_combine_kernel in share order.
 //
-// A lane copies exactly the 16-byte pieces that it will itself multiply
-// (cp.async into a slot of its own), so the ring needs no barrier: K rows
-// lane/4 and lane/4 + 8, V rows 2 (lane%4) + {0, 1, 8, 9}.  Which element of a
-// piece meets which k index is free as long as Q agrees; transposing V is a byte
-// permute of two rows' words before they are widened.
+// Each warp streams its own 16 keys a step through a ring of its own (cp.async, no
+// barrier wider than the warp).  A copy takes whole 128-byte lines: with the two
+// halves of a line in two instructions the same stream ran at 5.1 instead of 6.9 TB/s.
+// Which element of a row meets which k index is free as long as Q agrees, so a lane
+// reads 16 bytes of a K row as four k steps' operands; transposing V is a byte
+// permute of two rows' words before they are widened.  The 16 keys are taken in an
+// order (row_of) in which, with the rows' pieces swizzled, neither product's reads
+// meet in a bank.
 #include "kvattn.cuh"
 
 #include <algorithm>
@@ -39,19 +42,30 @@ constexpr float kNone = -1e30f;    // reference of a row that has seen no key
 constexpr float kSumLimit = 64.f;  // log2 of a term of the sum below
 constexpr float kTop = 15.f, kHead = 8.f;   // log2 of a term above: limit, and what a new reference leaves
 
-template <int NT>
-constexpr int stages() { return 4; }
+// CTAs per SM (registers: the rows' sums grow with NT)
+constexpr int kv_attn_resident(int nt) { return nt == 1 ? 3 : 2; }
 
 template <int DH, int NT>
 struct KvSmem {
-  static constexpr int KP = DH / 32;              // 16-byte pieces of K per lane and stage
-  static constexpr int VB = DH / 8;               // bytes of V per lane and row
-  static constexpr int STAGE = 32 * (KP * 16 + 4 * VB);   // bytes of a warp's stage
-  static constexpr int ST = stages<NT>();
+  static constexpr int HALF = 16 * DH;            // bytes of K (or V) of a warp's stage
+  static constexpr int STAGE = 2 * HALF;
+  static constexpr int VB = DH / 8;               // bytes of a V row that a lane reads
+  static constexpr int PIECES = DH / 16;          // 16-byte pieces of a row
+  static constexpr int RPC = 32 / PIECES;         // rows of one copy instruction of the warp
+  static constexpr int ST = 4;
   static constexpr int RING = ST * STAGE;         // bytes of a warp's ring
+  // piece c of row r: eight consecutive pieces of 128 bytes differ for the
+  // rows that are read at once
+  CC_DEV static int at(int r, int c) {
+    return DH == 128 ? r * DH + ((c ^ (r & 7)) << 4) : r * DH + ((c ^ ((r >> 1) & 3)) << 4);
+  }
   static constexpr int ROWS = 8 * NT;
   static constexpr int MERGE = ROWS * DH * 4;     // a warp's partial rows
-  static constexpr int BYTES = kWarps * (RING > MERGE ? RING : MERGE);
+  static constexpr int WARP = RING > MERGE ? RING : MERGE;
+  // the queries as operands: in registers, or past 16 rows in shared memory
+  static constexpr bool Q_SHARED = NT > 2;
+  static constexpr int OFF_Q = kWarps * WARP;
+  static constexpr int BYTES = OFF_Q + (Q_SHARED ? NT * (DH / 16) * 32 * 8 : 0);
 };
 
 CC_DEV float ex2(float x) {
@@ -64,6 +78,11 @@ CC_DEV uint32_t widen2(uint32_t two) {   // e4m3 pair (low 16 bits) -> fp16 pair
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)two));
   return r;
 }
+CC_DEV uint32_t nan_bytes(uint32_t w) {   // 0xFF in every byte of w that is a NaN code
+  return __vcmpeq4(w & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+}
+// Key of index n of the products' 16: odd ones half an 8-row group away.
+CC_DEV int row_of(int n) { return n ^ ((n & 1) << 2); }
 CC_DEV uint32_t transpose8(uint32_t x) {
   uint32_t r;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
@@ -76,14 +95,13 @@ CC_DEV void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-template <int BYTES>
-CC_DEV void copy_async(uint32_t dst, const void *src, bool there) {   // else zeros
-  if constexpr (BYTES == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
-                 "r"(there ? 16 : 0) : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src),
-                 "r"(there ? 8 : 0) : "memory");
+CC_DEV void copy16(uint32_t dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// From src + off where it is there, else zeros (then src, which is, is named but not read).
+CC_DEV void copy16_if(uint32_t dst, const uint8_t *src, int off, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src + (there ? off : 0)),
+               "r"(there ? 16 : 0) : "memory");
 }
 CC_DEV void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -185,32 +203,34 @@ CC_DEV void store2(const KvAttnParams &p, const RowAt &r, int d, int dh, float o
 // the kernel
 // ---------------------------------------------------------------------------
 template <typename T, int DH, int NT>
-__global__ void __launch_bounds__(kWarps * 32, NT == 4 ? 2 : 3)
+__global__ void __launch_bounds__(kWarps * 32, kv_attn_resident(NT))
     kv_attn_kernel(const __grid_constant__ KvAttnParams p) {
   using L = KvSmem<DH, NT>;
   constexpr int KS = DH / 16;        // k steps of K Q^T
   constexpr int DT = DH / 16;        // M tiles of V^T P^T
-  constexpr int KP = L::KP, ST = L::ST, VW = DH / 32;
+  constexpr int ST = L::ST, VW = DH / 32;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float s_m[kWarps][L::ROWS], s_mv[kWarps][L::ROWS], s_l[kWarps][L::ROWS];
   pdl_trigger();   // the combine may launch: it waits for this grid
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n8 = lane >> 2, quad = lane & 3;
   const long long total = total_tiles<NT>(p);
   const int n_ctas = sharing_ctas(p, total), cta = blockIdx.x;
-  if (cta >= n_ctas) return;
+  int4 cut = make_int4(0, 0, 0, -1);   // the unit that starts here and goes on in the next share
+  if (cta >= n_ctas) {
+    if (tid == 0) p.cut[cta] = cut;
+    return;
+  }
   long long at = total * cta / n_ctas;
   const long long end = total * (cta + 1) / n_ctas;
   // reported once, by the first CTA: sequences whose rows or lengths are bad
   if (cta == 0)
     for (int b = tid; b < p.rows.batch; b += kWarps * 32)
       if (!seq_rows(p.rows, b, !p.memory_only).ok) set_status(p.status, CC_ERR_DEVICE_ARG);
-  if (at >= end) return;
-
-  long long before;
-  int b = find_tile<NT>(p, at, before);
-  if (b >= p.rows.batch) return;   // (at < total)
+  long long before = 0;
+  int b = at < end ? find_tile<NT>(p, at, before) : 0;   // (below the batch: at < total)
   const uint32_t ring = smem_u32(smem) + warp * L::RING;
-  const int vstep = p.pg.head_major ? 1 : p.hkv;
+  const int hs = p.pg.head_major ? 1 : p.hkv, step = hs * DH;   // bytes from a slot to the next
+  const int log_block = 31 - __clz(p.block);
   SeqPlan sq = seq_plan<NT>(p, b);
   bool first = true;   // the share's first segment
   while (at < end) {
@@ -223,6 +243,7 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 4 ? 2 : 3)
     const int tile0 = (int)(in_seq - (long long)unit * sq.tiles);
     const int tile1 = (int)min((long long)sq.tiles, tile0 + (end - at));
     const SeqRows s = sq.s;
+    const int gs = p.pg.head_major ? 0 : g;
     const int G = p.hq / p.hkv, R0 = grp * L::ROWS;
     // seen slots of the group's first and last row
     const int last_pos = min(s.count - 1, (R0 + L::ROWS - 1) / G);
@@ -230,40 +251,72 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 4 ? 2 : 3)
     const int seen_hi = p.memory_only ? s.seq : s.seq + last_pos + 1;
 
     // ---- the ring of 16-key steps of this warp: step i is keys
-    // (tile0 + i) * 64 + 16 warp + [0, 16)
+    // (tile0 + i) * 64 + 16 warp + [0, 16), which lie in one page
     const int steps = tile1 - tile0;
+    int next = tile0 * kTile + warp * 16;   // slot of the next step to issue
+    // where slot 0 (of the page) of this head lies, and the step's slot in it
+    const int crow = lane / L::PIECES, cpiece = lane % L::PIECES;   // of this lane's copies
+    const long long lane_off = (long long)crow * step + cpiece * 16;
+    const uint8_t *kb, *vb, *keb, *veb;
+    int off = next, page = 0, page_end = 0x7FFFFFFF;
+    bool ok = true;
+    auto enter = [&](long long row0) {   // rows of hs vectors, of which this head's is the gs-th
+      const long long vec = row0 * hs + gs, e = (row0 >> log_block) * hs + gs;
+      kb = p.k + vec * DH + lane_off;
+      vb = p.v + vec * DH + lane_off;
+      keb = p.ke + e;
+      veb = p.ve + e;
+    };
+    auto enter_page = [&]() {
+      const int e = p.pg.table[(long long)b * p.pg.pages_per_seq + page];
+      ok = e >= 0 && e < p.pg.n_pages;
+      enter(ok ? (long long)e * p.pg.page : 0);
+    };
+    if (p.pg.table) {
+      page = next / p.pg.page;
+      off = next - page * p.pg.page;
+      page_end = p.pg.page;
+      if (next < seen_hi) enter_page();
+    } else {
+      enter(p.pg.head_major ? ((long long)b * p.hkv + g) * p.rows.cap : (long long)b * p.rows.cap);
+    }
     int issued = 0;
     auto issue = [&](int &ek, int &ev) {
-      const int slot = (tile0 + issued) * kTile + warp * 16;
       const uint32_t dst = ring + (issued % ST) * L::STAGE;
-      ek = ev = 127;
-      if (issued < steps && slot < seen_hi) {
-        const long long vec = kv_vec(p.pg, p.rows.cap, b, g, slot);
-        const bool ok = vec >= 0;
-        const long long v0 = ok ? vec : 0;
-        if (!ok && lane == 0) set_status(p.status, CC_ERR_DEVICE_ARG);
-        const int left = ok ? seen_hi - slot : 0;
-        const long long ei = p.pg.head_major ? v0 / p.block : v0 / p.hkv / p.block * p.hkv + g;
-        ek = p.ke[ei];
-        ev = p.ve[ei];
-        const uint8_t *kp = p.k + v0 * DH + quad * 16, *vp = p.v + v0 * DH + n8 * L::VB;
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const int row = n8 + 8 * r;
-          const bool there = row < left;
-          const uint8_t *src = kp + (there ? row * vstep * DH : 0);
-#pragma unroll
-          for (int h = 0; h < KP / 2; ++h)
-            copy_async<16>(dst + ((r * (KP / 2) + h) * 32 + lane) * 16, src + h * 64, there);
+      ek = ev = -1;   // not seen
+      if (issued < steps && next < seen_hi) {
+        if (off >= page_end) {
+          off -= page_end;
+          ++page;
+          enter_page();
         }
+        if (!ok) {
+          if (lane == 0) set_status(p.status, CC_ERR_DEVICE_ARG);
+        } else {
+          const int eo = (off >> log_block) * hs;
+          ek = keb[eo];
+          ev = veb[eo];
+          const uint8_t *kp = kb + (long long)off * step, *vp = vb + (long long)off * step;
+          const int left = seen_hi - next;
+          if (left >= 16) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int row = 2 * quad + (r & 1) + 8 * (r >> 1);
-          const bool there = row < left;
-          copy_async<L::VB>(dst + KP * 512 + (r * 32 + lane) * L::VB,
-                            vp + (there ? row * vstep * DH : 0), there);
+            for (int c = 0; c < 16 / L::RPC; ++c) {
+              const int to = L::at(crow + c * L::RPC, cpiece), from = c * L::RPC * step;
+              copy16(dst + to, kp + from);
+              copy16(dst + L::HALF + to, vp + from);
+            }
+          } else {   // what lies past the end reads as zeros
+#pragma unroll
+            for (int c = 0; c < 16 / L::RPC; ++c) {
+              const int row = crow + c * L::RPC, to = L::at(row, cpiece);
+              // (the step's first row is there: named from there)
+              copy16_if(dst + to, kp - lane_off, (int)lane_off + c * L::RPC * step, row < left);
+              copy16_if(dst + L::HALF + to, vp - lane_off, (int)lane_off + c * L::RPC * step, row < left);
+            }
+          }
         }
-        if (!ok) ek = -1;   // its slots are not seen
+        off += kTile;
+        next += kTile;
       }
       ++issued;
       copy_commit();
@@ -274,7 +327,8 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 4 ? 2 : 3)
 
     // ---- queries: row 8 t + n8 of the group as the second operand, fp16,
     // scaled to a largest magnitude of [2^7, 2^8)
-    uint32_t qb[NT][KS][2];
+    uint32_t qb[L::Q_SHARED ? 1 : NT][KS][2];
+    uint2 *q_sh = reinterpret_cast<uint2 *>(smem + L::OFF_Q);   // [NT][KS][lane]
     float qf[NT][2];           // of rows 2 quad, 2 quad + 1: what undoes the scale, with the softmax's
     int seen[NT][2];           // slots they see
 #pragma unroll
@@ -311,8 +365,14 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 4 ? 2 : 3)
       const float down = p.scale_log2 * __uint_as_float((uint32_t)max(e - 7, 1) << 23);
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        qb[t][k][0] = pack_f16x2(x[4 * k] * up, x[4 * k + 1] * up);
-        qb[t][k][1] = pack_f16x2(x[4 * k + 2] * up, x[4 * k + 3] * up);
+        const uint32_t b0 = pack_f16x2(x[4 * k] * up, x[4 * k + 1] * up);
+        const uint32_t b1 = pack_f16x2(x[4 * k + 2] * up, x[4 * k + 3] * up);
+        if constexpr (L::Q_SHARED) {
+          if (t % kWarps == warp) q_sh[(t * KS + k) * 32 + lane] = make_uint2(b0, b1);
+        } else {
+          qb[t][k][0] = b0;
+          qb[t][k][1] = b1;
+        }
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -321,6 +381,7 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 4 ? 2 : 3)
         seen[t][c] = p.memory_only ? s.seq : s.seq + pos + 1;
       }
     }
+    if constexpr (L::Q_SHARED) __syncthreads();
     float o[NT][DT][4], m[NT][2], mv[NT][2], l[NT][2];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -332,33 +393,47 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 4 ? 2 : 3)
         for (int k = 0; k < 4; ++k) o[t][d][k] = 0.f;
     }
 
+    // where this lane reads in a stage: K row row_of(n8), piece quad (+ 4); V rows
+    // row_of(2 quad), row_of(2 quad + 1), bytes n8 * VB
+    const int k_at = L::at(row_of(n8), quad);
+    int v_at[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+      v_at[r] = L::at(row_of(2 * quad + r), n8 * L::VB / 16) + n8 * L::VB % 16;
 #pragma unroll 1
     for (int i0 = 0; i0 < steps; i0 += ST) {
 #pragma unroll
       for (int u = 0; u < ST; ++u) {
         const int i = i0 + u;
         if (i >= steps) break;
+        copy_wait<ST - 2>();
+        __syncwarp();   // every lane's copies of this step; every lane is done with the last one
         issue(ek_q[(u + ST - 1) % ST], ev_q[(u + ST - 1) % ST]);
-        copy_wait<ST - 1>();
         const int slot = (tile0 + i) * kTile + warp * 16;
-        if (slot >= seen_hi || ek_q[u] < 0) continue;
+        if (ek_q[u] < 0) continue;
         const uint8_t *st = smem + warp * L::RING + (i % ST) * L::STAGE;
         // ---- S^T: keys n8, n8 + 8 x rows 2 quad, 2 quad + 1
         float sc[NT][4];
 #pragma unroll
         for (int t = 0; t < NT; ++t) sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
 #pragma unroll
-        for (int h = 0; h < KP / 2; ++h) {
-          const uint4 ua = *reinterpret_cast<const uint4 *>(st + (h * 32 + lane) * 16);
-          const uint4 ub = *reinterpret_cast<const uint4 *>(st + ((KP / 2 + h) * 32 + lane) * 16);
+        for (int h = 0; h < DH / 64; ++h) {
+          const uint4 ua = *reinterpret_cast<const uint4 *>(st + (k_at ^ (h * 64)));
+          const uint4 ub = *reinterpret_cast<const uint4 *>(st + 8 * DH + (k_at ^ (h * 64)));
           const uint32_t wa[4] = {ua.x, ua.y, ua.z, ua.w}, wb[4] = {ub.x, ub.y, ub.z, ub.w};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const uint32_t a0 = widen2(wa[j]), a2 = widen2(wa[j] >> 16);
             const uint32_t a1 = widen2(wb[j]), a3 = widen2(wb[j] >> 16);
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-              mma_f16(sc[t], a0, a1, a2, a3, qb[t][4 * h + j][0], qb[t][4 * h + j][1]);
+            for (int t = 0; t < NT; ++t) {
+              if constexpr (L::Q_SHARED) {
+                const uint2 q2 = q_sh[(t * KS + 4 * h + j) * 32 + lane];
+                mma_f16(sc[t], a0, a1, a2, a3, q2.x, q2.y);
+              } else {
+                mma_f16(sc[t], a0, a1, a2, a3, qb[t][4 * h + j][0], qb[t][4 * h + j][1]);
+              }
+            }
           }
         }
         // ---- scores in the log2 domain, against the references
@@ -371,7 +446,7 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 4 ? 2 : 3)
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             sc[t][k] *= qf[t][k & 1] * kf;
-            if (mask && slot + n8 + 8 * (k >> 1) >= seen[t][k & 1]) sc[t][k] = -INFINITY;
+            if (mask && slot + row_of(n8) + 8 * (k >> 1) >= seen[t][k & 1]) sc[t][k] = -INFINITY;
           }
 #pragma unroll
           for (int c = 0; c < 2; ++c)
@@ -417,11 +492,51 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 4 ? 2 : 3)
         uint32_t w[4][VW];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const uint8_t *src = st + KP * 512 + (r * 32 + lane) * L::VB;
+          const uint8_t *src = st + L::HALF + (r >> 1) * 8 * DH + v_at[r & 1];
           if constexpr (VW == 4)
             *reinterpret_cast<uint4 *>(w[r]) = *reinterpret_cast<const uint4 *>(src);
           else
             *reinterpret_cast<uint2 *>(w[r]) = *reinterpret_cast<const uint2 *>(src);
+        }
+        if (mask) {
+          // keys that some rows do not see: a NaN among their values may reach only
+          // the rows that do (0 times NaN is NaN), so it leaves the product
+          uint32_t any = 0;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < VW; ++j) any |= nan_bytes(w[r][j]);
+          if (__any_sync(0xFFFFFFFFu, any != 0)) {
+            uint32_t bits[4];   // of row r: which of the lane's VB values
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              bits[r] = 0;
+#pragma unroll
+              for (int j = 0; j < VW; ++j) {
+                const uint32_t x = nan_bytes(w[r][j]);
+                w[r][j] &= ~x;
+                bits[r] |= ((x & 1u) | ((x >> 7) & 2u) | ((x >> 14) & 4u) | ((x >> 21) & 8u)) << (4 * j);
+              }
+            }
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k) {   // of the quad's lane k, which holds keys of its own
+              uint32_t hit[4];
+#pragma unroll
+              for (int r = 0; r < 4; ++r) hit[r] = __shfl_sync(0xFFFFFFFFu, bits[r], (lane & ~3) | k);
+#pragma unroll
+              for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                  uint32_t here = 0;
+#pragma unroll
+                  for (int r = 0; r < 4; ++r)
+                    here |= slot + row_of(2 * k + (r & 1)) + 8 * (r >> 1) < seen[t][c] ? hit[r] : 0u;
+#pragma unroll
+                  for (int d = 0; d < L::VB; ++d)
+                    if ((here >> d) & 1u) o[t][d >> 1][(d & 1) * 2 + c] = NAN;
+                }
+            }
+          }
         }
 #pragma unroll
         for (int j = 0; j < VW; ++j)
@@ -461,6 +576,8 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 4 ? 2 : 3)
       }
     __syncthreads();
     const bool whole = tile0 == 0 && tile1 == sq.tiles;
+    if (tile0 == 0 && !whole)
+      cut = make_int4(b, g, grp, cta_of_tile(at + sq.tiles - 1, total, n_ctas));
     // a unit in several shares: what this one has of it, after (0) or from (1) its start
     const long long slot = 2ll * cta + (first && tile0 > 0 ? 0 : 1);
     for (int i = tid; i < L::ROWS * DH / 2; i += kWarps * 32) {
@@ -492,12 +609,13 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 4 ? 2 : 3)
     at += tile1 - tile0;
     first = false;
   }
+  if (tid == 0) p.cut[cta] = cut;
 }
 
 // Joins the shares of a unit, one row of it per CTA, in share order: kGroups
 // groups of DH / 2 threads take every kGroups-th share.  CTA (c, row) joins the
-// unit that the boundary between shares c and c + 1 cuts, if it is the first
-// that does.
+// unit that starts in share c and goes on past it, as that share's CTA wrote it
+// down.
 constexpr int kGroups = 4;
 
 template <typename T, int DH, int NT>
@@ -509,20 +627,11 @@ __global__ void __launch_bounds__(kGroups * DH / 2)
   pdl_trigger();
   pdl_wait();
   const int c0 = blockIdx.x, R = blockIdx.y;
-  const long long total = total_tiles<NT>(p);
-  const int n_ctas = sharing_ctas(p, total);
-  if (c0 + 1 >= n_ctas) return;
-  const long long cut = total * (c0 + 1) / n_ctas;   // the first tile of the next share
-  long long before;
-  const int b = find_tile<NT>(p, cut, before);
-  if (b >= p.rows.batch) return;
-  const SeqPlan sq = seq_plan<NT>(p, b);
-  const int unit = (int)((cut - before) / sq.tiles), g = unit / sq.groups, grp = unit - g * sq.groups;
-  const long long t0 = before + (long long)unit * sq.tiles;
-  if (t0 == cut || cta_of_tile(t0, total, n_ctas) != c0) return;
-  const RowAt r = row_at(p, sq.s, g, grp * ROWS + R);
+  const int4 u = p.cut[c0];   // sequence, KV head, group of rows, last share (none: no unit)
+  if (u.w <= c0) return;
+  const RowAt r = row_at(p, seq_rows(p.rows, u.x, !p.memory_only), u.y, u.z * ROWS + R);
   if (!r.live) return;
-  const int c1 = cta_of_tile(t0 + sq.tiles - 1, total, n_ctas);
+  const int c1 = u.w;
   const int part_id = threadIdx.x / (DH / 2), d = (threadIdx.x - part_id * (DH / 2)) * 2;
   // share c0 holds the unit's start, those after it start inside the unit
   auto slot = [&](int c) { return (2ll * c + (c == c0 ? 1 : 0)) * ROWS + R; };
@@ -581,6 +690,7 @@ cudaError_t launch_nt(const KvAttnParams &p, cudaStream_t st) {
   switch (p.nt) {
     case 1: return launch_as<T, DH, 1>(p, st);
     case 2: return launch_as<T, DH, 2>(p, st);
+    case 3: return launch_as<T, DH, 3>(p, st);
     case 4: return launch_as<T, DH, 4>(p, st);
     default: return cudaErrorInvalidValue;
   }
@@ -590,9 +700,12 @@ cudaError_t launch_dh(const KvAttnParams &p, cudaStream_t st) {
   return p.head_dim == 128 ? launch_nt<T, 128>(p, st) : launch_nt<T, 64>(p, st);
 }
 
-// A slot's 16 elements of K and V per thread.
+// ---------------------------------------------------------------------------
+// around the tile attention
+// ---------------------------------------------------------------------------
+// 16 elements of K and of V per thread.
 __global__ void __launch_bounds__(256)
-    kv_block_copy_kernel(const __grid_constant__ KvAttnParams p, uint16_t *ko, uint16_t *vo, int32_t *ends) {
+    kv_block_copy_kernel(const __grid_constant__ KvAttnParams p, uint16_t *ko, uint16_t *vo, KvTileRows t) {
   const int dh = p.head_dim, chunks = p.hkv * dh / 16, cap = p.rows.cap;
   const long long idx = (long long)blockIdx.x * blockDim.x + threadIdx.x;
   if (idx >= (long long)p.rows.batch * cap * chunks) return;
@@ -600,49 +713,108 @@ __global__ void __launch_bounds__(256)
   const int c = (int)(idx - row * chunks);
   const int b = (int)(row / cap), i = (int)(row - (long long)b * cap);
   const SeqRows s = seq_rows(p.rows, b, !p.memory_only);
-  const int end = s.ok ? s.seq + (p.memory_only ? 0 : s.count) : 0;
   if (i == 0 && c == 0) {
-    ends[b] = end;
+    t.lo[b] = s.ok ? s.seq : 0;
+    t.hi[b] = s.ok ? s.seq + s.count : 0;
+    t.base[b] = s.r0;
     if (!s.ok) set_status(p.status, CC_ERR_DEVICE_ARG);
   }
-  if (i >= end || s.count == 0) return;
+  if (s.count == 0 || i >= s.seq + (p.memory_only ? 0 : s.count)) return;
   const int h = c * 16 / dh, e = c * 16 - h * dh;
   const long long vec = kv_vec(p.pg, cap, b, h, i);
   const size_t dst = (size_t)row * p.hkv * dh + (size_t)h * dh + e;
-  if (vec < 0) {
-    set_status(p.status, CC_ERR_DEVICE_ARG);
-    return;
-  }
-  const long long ei = p.pg.head_major ? vec / p.block : vec / p.hkv / p.block * p.hkv + h;
-  auto convert = [&](const uint8_t *in, int exp, uint16_t *out) {
+  if (vec < 0) set_status(p.status, CC_ERR_DEVICE_ARG);
+  const long long at = vec < 0 ? 0 : vec;
+  const long long ei = p.pg.head_major ? at / p.block : at / p.hkv / p.block * p.hkv + h;
+  auto convert = [&](const uint8_t *in, int exp, bool clean, uint16_t *out) {
     const uint4 x = *reinterpret_cast<const uint4 *>(in);
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t w[4] = {x.x, x.y, x.z, x.w};
     const float f = __uint_as_float((uint32_t)exp << 23);
     uint32_t o[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t h2 = widen2(w[j / 2] >> (16 * (j & 1)));
-      const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&h2));
-      o[j] = pack_bf16x2(y.x * f, y.y * f);
+    for (int j = 0; j < 4; ++j) {
+      if (clean) w[j] &= ~nan_bytes(w[j]);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t h2 = widen2(w[j] >> (16 * k));
+        const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&h2));
+        o[2 * j + k] = pack_bf16x2(y.x * f, y.y * f);
+      }
     }
     uint4 *d = reinterpret_cast<uint4 *>(out);
     d[0] = make_uint4(o[0], o[1], o[2], o[3]);
     d[1] = make_uint4(o[4], o[5], o[6], o[7]);
   };
-  convert(p.k + vec * dh + e, p.ke[ei], ko + dst);
-  convert(p.v + vec * dh + e, p.ve[ei], vo + dst);
+  // (the slots of a bad page: keys of NaN, so that the rows that see them are 0)
+  convert(p.k + at * dh + e, vec < 0 ? 255 : p.ke[ei], false, ko + dst);
+  convert(p.v + at * dh + e, vec < 0 ? 0 : p.ve[ei], i >= s.seq || vec < 0, vo + dst);
+}
+
+// A warp per new token and KV head: where its values hold NaN codes, the
+// outputs of its own and the later rows of its sequence get NaN there.
+template <typename T>
+__global__ void __launch_bounds__(256) kv_restore_nan_kernel(const __grid_constant__ KvAttnParams p) {
+  const long long w = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+  const int lane = threadIdx.x & 31, r = (int)(w / p.hkv), g = (int)(w - (long long)r * p.hkv);
+  if (r >= p.rows.n_rows) return;
+  int b = 0;   // the last sequence that starts at or before row r
+  for (int hi = p.rows.batch - 1; b < hi;) {
+    const int mid = (b + hi + 1) >> 1;
+    if (p.rows.row_start[mid] <= r) b = mid; else hi = mid - 1;
+  }
+  const SeqRows s = seq_rows(p.rows, b, true);
+  if (r < s.r0 || r >= s.r0 + s.count) return;
+  const long long vec = kv_vec(p.pg, p.rows.cap, b, g, s.seq + r - s.r0);
+  if (vec < 0) return;
+  const int dh = p.head_dim, G = p.hq / p.hkv;
+  for (int d = lane; d < dh; d += 32) {
+    if ((p.v[vec * dh + d] & 0x7F) != 0x7F) continue;
+    const T nan = std::is_same_v<T, __half> ? T(__ushort_as_half(0x7FFF)) : T(__ushort_as_bfloat16(0x7FFF));
+    for (int i = r; i < s.r0 + s.count; ++i)
+      for (int h = 0; h < G; ++h)
+        reinterpret_cast<T *>(p.out)[i * p.out_ld + (long long)(g * G + h) * dh + d] = nan;
+  }
+}
+
+// 8 elements per thread.
+__global__ void __launch_bounds__(256)
+    kv_split_rows_kernel(const __grid_constant__ KvAttnParams p, __nv_bfloat16 *pairs) {
+  const int width = p.hq * p.head_dim, per = width / 8;
+  const long long idx = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  if (idx >= (long long)p.rows.n_rows * per) return;
+  const long long r = idx / per;
+  const int e = (int)(idx - r * per) * 8;
+  const uint4 u = *reinterpret_cast<const uint4 *>(reinterpret_cast<const __half *>(p.q) + r * p.q_ld + e);
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  uint32_t hi[4], lo[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+    hi[i] = pack_bf16x2(x.x, x.y);
+    lo[i] = pack_bf16x2(pair_rest(x.x, bf16_lo(hi[i])), pair_rest(x.y, bf16_hi(hi[i])));
+  }
+  __nv_bfloat16 *dst = pairs + r * 2 * width + e;
+  *reinterpret_cast<uint4 *>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+  *reinterpret_cast<uint4 *>(dst + width) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 }
 
 }  // namespace
 
 void kv_attn_plan(KvAttnParams &p, int sms) {
   const long long rows = (long long)p.rows.max_rows * (p.hq / p.hkv);
-  p.nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
-  p.ctas = sms * (p.nt == 4 ? 2 : 3);
+  p.nt = (int)std::min<long long>(4, (rows + 7) / 8);
+  p.ctas = sms * kv_attn_resident(p.nt);
 }
 
 size_t kv_attn_part_bytes(const KvAttnParams &p) {
-  return (size_t)2 * p.ctas * 8 * p.nt * (p.head_dim * sizeof(float) + sizeof(float4));
+  return (size_t)2 * p.ctas * 8 * p.nt * (p.head_dim * sizeof(float) + sizeof(float4)) +
+         p.ctas * sizeof(int4);
+}
+void kv_attn_bind(KvAttnParams &p, void *ws) {
+  const size_t rows = (size_t)2 * p.ctas * 8 * p.nt;
+  p.part_o = reinterpret_cast<float *>(ws);
+  p.part_ml = reinterpret_cast<float4 *>(p.part_o + rows * p.head_dim);
+  p.cut = reinterpret_cast<int4 *>(p.part_ml + rows);
 }
 
 cudaError_t launch_kv_attn(const KvAttnParams &p, cudaStream_t st) {
@@ -650,13 +822,28 @@ cudaError_t launch_kv_attn(const KvAttnParams &p, cudaStream_t st) {
   return p.f16 ? launch_dh<__half>(p, st) : launch_dh<__nv_bfloat16>(p, st);
 }
 
-cudaError_t launch_kv_block_copy(const KvAttnParams &p, void *ko, void *vo, int32_t *ends,
+cudaError_t launch_kv_block_copy(const KvAttnParams &p, void *ko, void *vo, const KvTileRows &t,
                                  cudaStream_t st) {
   const long long n = (long long)p.rows.batch * p.rows.cap * (p.hkv * p.head_dim / 16);
   const long long blocks = (n + 255) / 256;
   if (blocks > 0x7FFFFFFFll) return cudaErrorInvalidValue;
   kv_block_copy_kernel<<<(unsigned)blocks, 256, 0, st>>>(
-      p, reinterpret_cast<uint16_t *>(ko), reinterpret_cast<uint16_t *>(vo), ends);
+      p, reinterpret_cast<uint16_t *>(ko), reinterpret_cast<uint16_t *>(vo), t);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_kv_restore_nan(const KvAttnParams &p, cudaStream_t st) {
+  const long long blocks = ((long long)p.rows.n_rows * p.hkv + 7) / 8;
+  if (blocks > 0x7FFFFFFFll) return cudaErrorInvalidValue;
+  if (p.f16) kv_restore_nan_kernel<__half><<<(unsigned)blocks, 256, 0, st>>>(p);
+  else kv_restore_nan_kernel<__nv_bfloat16><<<(unsigned)blocks, 256, 0, st>>>(p);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_kv_split_rows(const KvAttnParams &p, void *pairs, cudaStream_t st) {
+  const long long blocks = ((long long)p.rows.n_rows * p.hq * p.head_dim / 8 + 255) / 256;
+  if (blocks > 0x7FFFFFFFll) return cudaErrorInvalidValue;
+  kv_split_rows_kernel<<<(unsigned)blocks, 256, 0, st>>>(p, reinterpret_cast<__nv_bfloat16 *>(pairs));
   return cudaGetLastError();
 }
 

@@ -18,23 +18,36 @@ struct KvAttnParams {
   int hq, hkv, head_dim;
   float scale_log2;             // log2(e) / sqrt(head_dim)
   // set by kv_attn_plan
-  int nt;                       // query rows of a unit / 8: 1, 2 or 4
+  int nt;                       // query rows of a unit / 8: 1 to 4
   int ctas;                     // CTAs that share the units' key tiles
   float *part_o;                // [2 * ctas][8 * nt][head_dim]: what a CTA leaves of the unit
   float4 *part_ml;              // [2 * ctas][8 * nt]            before and after its share
+  int4 *cut;                    // [ctas]: the unit that starts in a CTA's share and goes on
   unsigned *status;
 };
 
 // Rows of a unit and CTAs of a launch: p.nt and p.ctas from rows.max_rows and
 // the head counts.
 void kv_attn_plan(KvAttnParams &p, int sms);
+// Bytes of the three, and where they lie in a workspace.
 size_t kv_attn_part_bytes(const KvAttnParams &p);
+void kv_attn_bind(KvAttnParams &p, void *ws);
 cudaError_t launch_kv_attn(const KvAttnParams &p, cudaStream_t st);
 
-// The seen slots of one layer as a bf16 slot-major copy (exact) in rows
-// b * cap + i of ko, vo, and the ends seq_len + rows (memory_only: seq_len) of
-// the sequences in `ends`; a sequence without rows is not copied.
-cudaError_t launch_kv_block_copy(const KvAttnParams &p, void *ko, void *vo, int32_t *ends,
+// Around the tile attention (attn.cu) of larger chunks:
+//   the seen slots of one layer as a bf16 slot-major copy (exact) in rows
+//   b * cap + i of ko, vo; for each sequence the first and end slot of its rows
+//   (lo, hi: seq_len and on) and the first of them (base).  A sequence that is not
+//   ok has lo = hi; one without rows is not copied.  NaN codes among the values
+//   of new tokens, which earlier rows do not see, are copied as 0 ...
+struct KvTileRows {
+  int32_t *lo, *hi, *base;   // device [batch]
+};
+cudaError_t launch_kv_block_copy(const KvAttnParams &p, void *ko, void *vo, const KvTileRows &t,
                                  cudaStream_t st);
+//   ... and put into the rows that do, afterwards;
+cudaError_t launch_kv_restore_nan(const KvAttnParams &p, cudaStream_t st);
+//   fp16 rows as bf16 pairs (exact): [n_rows][hi: hq * head_dim | lo: hq * head_dim].
+cudaError_t launch_kv_split_rows(const KvAttnParams &p, void *pairs, cudaStream_t st);
 
 }  // namespace cc

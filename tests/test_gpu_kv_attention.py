@@ -102,6 +102,63 @@ def test_matches_oracle(pkg, hq, hkv, dh, block, layout, dtype, cap, lens, count
     assert torch.equal(again, got)   # the same bits, run to run
 
 
+CHUNKS = [
+    (8, 2, 64, 16, "paged", 512, [0, 130, 300], [200, 150, 64], 0),
+    (4, 1, 128, 64, "head", 1024, [777], [130], 0),
+    (7, 1, 128, 128, "slot", 384, [0, 1, 127, 128], [257, 64, 128, 129], 0),
+    (16, 2, 64, 32, "paged", 256, [10, 0, 90, 256], [100, 40, 0, 0], 8),
+    (3, 3, 128, 32, "paged", 2304, [2048], [72], 0),                    # key splits
+]
+
+
+@pytest.mark.parametrize("memory", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hq,hkv,dh,block,layout,cap,lens,counts,pad", CHUNKS)
+def test_chunks_match_oracle(pkg, hq, hkv, dh, block, layout, cap, lens, counts, pad, dtype, memory):
+    from paper_2607_27600_gb300 import cc
+    rng = np.random.default_rng(hq * 1000 + cap)
+    s, b = shape(hq, hkv, dh), len(lens)
+    codes, exps = {}, {}
+    for n in "kv":
+        codes[n], exps[n] = quantised(rng, b, cap, hkv, dh, block)
+    junk(rng, codes, exps, lens if memory else [n + m for n, m in zip(lens, counts)], block)
+    t, eps = TYPES[dtype]
+    q = torch.from_numpy(rng.standard_normal((sum(counts), hq, dh)) * 1.5).to(t).double().numpy()
+    c = DeviceCache(pkg, codes, exps, lens, layout)
+    got, ls = attend(pkg, s, c, counts, columns([q], t, 24)[0], memory, pad=pad)
+    assert cc.cc_get_status() == cc.CC_OK
+    want = oracle.attend_rows(q, values(codes["k"], exps["k"]), values(codes["v"], exps["v"]), lens,
+                              starts(counts), memory)
+    check(got, ls, *want, eps, tile=dtype == "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("counts", [[6, 2], [100, 40]])
+def test_not_a_number_of_a_later_row(pkg, counts, dtype):
+    """A NaN code among a new token's values reaches the rows that see it and no others."""
+    rng = np.random.default_rng(12)
+    s, cap, block, lens = shape(8, 2, 64), 256, 16, [120, 3]
+    codes, exps = {}, {}
+    for n in "kv":
+        codes[n], exps[n] = quantised(rng, 2, cap, 2, 64, block)
+    k, v = values(codes["k"], exps["k"]), values(codes["v"], exps["v"])
+    t, eps = TYPES[dtype]
+    q = torch.from_numpy(rng.standard_normal((sum(counts), 8, 64))).to(t).double().numpy()
+    want = oracle.attend_rows(q, k, v, lens, starts(counts))
+    row = counts[0] // 2
+    codes["v"][0, lens[0] + row, 1, [7, 40]] = [0x7F, 0xFF]
+    codes["v"][1, lens[1] + counts[1] - 1, 0, 63] = 0x7F
+    c = DeviceCache(pkg, codes, exps, lens, "paged")
+    got, ls = attend(pkg, s, c, counts, columns([q], t)[0])
+    got = got.double()
+    bad = torch.zeros(got.shape, dtype=torch.bool)
+    bad[row:counts[0], 4:, [7, 40]] = True
+    bad[-1, :4, 63] = True
+    assert torch.equal(torch.isnan(got).cpu(), bad)
+    got[bad] = torch.from_numpy(want[0])[bad].cuda()
+    check(got, ls, *want, eps, tile=dtype == "bf16" and counts[0] > 32)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_scales_far_apart(pkg, dtype):
     """Value scales over 2^+-40 between blocks, key scales over 2^+-6, queries over
