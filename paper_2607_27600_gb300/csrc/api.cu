@@ -1800,7 +1800,8 @@ cc_status check_layer(const cc_model_cfg *c, const cc_kv_cache *kv, int l) {
       !aligned16(kv->k[l]) || !aligned16(kv->v[l]) || !kv_layout_ok(kv))
     return CC_ERR_INVALID_ARG;
   if (kv->kv_format == CC_KV_E4M3_BLOCK) {
-    if (!block_size_ok(kv) || !kv->k_exp || !kv->v_exp || !kv->k_exp[l] || !kv->v_exp[l])
+    if (!block_size_ok(kv) || !kv->k_exp || !kv->v_exp || !kv->k_exp[l] || !kv->v_exp[l] ||
+        !aligned16(kv->k_exp[l]) || !aligned16(kv->v_exp[l]))
       return CC_ERR_INVALID_ARG;
     return CC_OK;
   }
@@ -1825,6 +1826,7 @@ KvAttnParams kv_attn_params(const cc_model_cfg *c, const cc_kv_cache *kv, const 
   KvAttnParams p{};
   p.rows = step_rows(kv, rows);
   p.block = kv->kv_block;
+  p.exp_bytes = kv->kv_block ? (long long)(kv_buffer_rows(kv) / kv->kv_block) * c->n_kv_heads : 0;
   p.pg = kv_layout(c, kv);
   p.hq = c->n_q_heads;
   p.hkv = c->n_kv_heads;

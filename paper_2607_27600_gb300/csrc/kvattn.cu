@@ -38,6 +38,7 @@ namespace {
 constexpr int kWarps = 4;          // of a CTA, each every fourth 16 keys of a tile
 constexpr int kTile = 16 * kWarps; // keys of a tile
 constexpr int kMinTiles = 2;       // of a share at least
+constexpr uint32_t kBadPage = 0xFFFFFFFFu;   // in place of the scales' place: nothing to see
 constexpr float kNone = -1e30f;    // reference of a row that has seen no key
 constexpr float kSumLimit = 64.f;  // log2 of a term of the sum below
 constexpr float kTop = 15.f, kHead = 8.f;   // log2 of a term above: limit, and what a new reference leaves
@@ -48,7 +49,7 @@ constexpr int kv_attn_resident(int nt) { return nt == 1 ? 3 : 2; }
 template <int DH, int NT>
 struct KvSmem {
   static constexpr int HALF = 16 * DH;            // bytes of K (or V) of a warp's stage
-  static constexpr int STAGE = 2 * HALF;
+  static constexpr int STAGE = 2 * HALF + 16;     // and a word of K's scales, of V's, their place in it
   static constexpr int VB = DH / 8;               // bytes of a V row that a lane reads
   static constexpr int PIECES = DH / 16;          // 16-byte pieces of a row
   static constexpr int RPC = 32 / PIECES;         // rows of one copy instruction of the warp
@@ -97,6 +98,9 @@ CC_DEV void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32
 }
 CC_DEV void copy16(uint32_t dst, const void *src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+CC_DEV void copy4(uint32_t dst, const void *src, int bytes) {   // fewer than 4: zeros after them
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 // From src + off where it is there, else zeros (then src, which is, is named but not read).
 CC_DEV void copy16_if(uint32_t dst, const uint8_t *src, int off, bool there) {
@@ -184,19 +188,18 @@ CC_DEV RowAt row_at(const KvAttnParams &p, const SeqRows &s, int g, int R) {
   return {s.r0 + pos, g * G + R - pos * G, pos < s.count};
 }
 
-// out and lse of one row's share of the head dimension: the joined sums.
-template <typename T>
-CC_DEV void store2(const KvAttnParams &p, const RowAt &r, int d, int dh, float o0, float o1, float m,
-                   float mv, float l) {
-  const bool good = l > 0.f && l < INFINITY;
-  const int shift = good ? (int)(mv - m) : 0;
-  const float inv = good ? 1.f / l : 0.f;
-  const uint32_t w = good ? pack2<T>(ldexpf(o0 * inv, shift), ldexpf(o1 * inv, shift)) : 0u;
-  *reinterpret_cast<uint32_t *>(reinterpret_cast<T *>(p.out) + r.row * p.out_ld +
-                                (long long)r.head * dh + d) = w;
-  if (p.lse && d == 0)
-    p.lse[(long long)r.row * p.hq + r.head] =
-        l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+// What the sum above of a row is multiplied by: 2^(mv - m) / l as two factors,
+// neither of which leaves fp32's range (0 for a row without a finite sum below).
+struct OutScale {
+  float a, b;
+};
+CC_DEV OutScale out_scale(float m, float mv, float l) {
+  if (!(l > 0.f && l < INFINITY)) return {0.f, 0.f};
+  const int shift = min(max((int)(mv - m), -250), 250), half = shift / 2;
+  return {__uint_as_float((uint32_t)(127 + half) << 23) / l, __uint_as_float((uint32_t)(127 + shift - half) << 23)};
+}
+CC_DEV float row_lse(float m, float l) {
+  return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
 // ---------------------------------------------------------------------------
@@ -211,6 +214,10 @@ __global__ void __launch_bounds__(kWarps * 32, kv_attn_resident(NT))
   constexpr int ST = L::ST, VW = DH / 32;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float s_m[kWarps][L::ROWS], s_mv[kWarps][L::ROWS], s_l[kWarps][L::ROWS];
+  __shared__ float4 s_f[L::ROWS];
+  __shared__ float s_b[L::ROWS];
+  __shared__ long long s_to[L::ROWS];
+  static_assert(kWarps == 4, "a row's weights are a float4");
   pdl_trigger();   // the combine may launch: it waits for this grid
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n8 = lane >> 2, quad = lane & 3;
   const long long total = total_tiles<NT>(p);
@@ -252,20 +259,20 @@ __global__ void __launch_bounds__(kWarps * 32, kv_attn_resident(NT))
 
     // ---- the ring of 16-key steps of this warp: step i is keys
     // (tile0 + i) * 64 + 16 warp + [0, 16), which lie in one page
-    const int steps = tile1 - tile0;
     int next = tile0 * kTile + warp * 16;   // slot of the next step to issue
+    const int steps = min(tile1 - tile0, max(0, seen_hi - next + kTile - 1) / kTile);
     // where slot 0 (of the page) of this head lies, and the step's slot in it
     const int crow = lane / L::PIECES, cpiece = lane % L::PIECES;   // of this lane's copies
     const long long lane_off = (long long)crow * step + cpiece * 16;
-    const uint8_t *kb, *vb, *keb, *veb;
+    const uint8_t *kb, *vb;
+    long long e0;   // of the slot's (page's) first scale exponent
     int off = next, page = 0, page_end = 0x7FFFFFFF;
     bool ok = true;
     auto enter = [&](long long row0) {   // rows of hs vectors, of which this head's is the gs-th
-      const long long vec = row0 * hs + gs, e = (row0 >> log_block) * hs + gs;
+      const long long vec = row0 * hs + gs;
       kb = p.k + vec * DH + lane_off;
       vb = p.v + vec * DH + lane_off;
-      keb = p.ke + e;
-      veb = p.ve + e;
+      e0 = (row0 >> log_block) * hs + gs;
     };
     auto enter_page = [&]() {
       const int e = p.pg.table[(long long)b * p.pg.pages_per_seq + page];
@@ -276,26 +283,32 @@ __global__ void __launch_bounds__(kWarps * 32, kv_attn_resident(NT))
       page = next / p.pg.page;
       off = next - page * p.pg.page;
       page_end = p.pg.page;
-      if (next < seen_hi) enter_page();
+      if (steps > 0) enter_page();
     } else {
       enter(p.pg.head_major ? ((long long)b * p.hkv + g) * p.rows.cap : (long long)b * p.rows.cap);
     }
-    int issued = 0;
-    auto issue = [&](int &ek, int &ev) {
-      const uint32_t dst = ring + (issued % ST) * L::STAGE;
-      ek = ev = -1;   // not seen
-      if (issued < steps && next < seen_hi) {
+    int left_to_issue = steps;
+    uint32_t write_at = 0, read_at = 0;   // stages of the ring
+    auto issue = [&]() {
+      if (left_to_issue > 0) {
+        --left_to_issue;
+        const uint32_t dst = ring + write_at;
+        write_at = write_at + L::STAGE == L::RING ? 0 : write_at + L::STAGE;
         if (off >= page_end) {
           off -= page_end;
           ++page;
           enter_page();
         }
-        if (!ok) {
-          if (lane == 0) set_status(p.status, CC_ERR_DEVICE_ARG);
-        } else {
-          const int eo = (off >> log_block) * hs;
-          ek = keb[eo];
-          ev = veb[eo];
+        if (!ok && lane == 0) set_status(p.status, CC_ERR_DEVICE_ARG);
+        // the block's scale exponents: the aligned words that hold them
+        const long long eo = e0 + (off >> log_block) * hs;
+        if (ok && lane < 2)
+          copy4(dst + 2 * L::HALF + lane * 4, (lane ? p.ve : p.ke) + (eo & ~3ll),
+                (int)min(4ll, p.exp_bytes - (eo & ~3ll)));
+        if (lane == 0)
+          asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + 2 * L::HALF + 8),
+                       "r"(ok ? (uint32_t)(eo & 3) * 8 : kBadPage) : "memory");
+        if (ok) {
           const uint8_t *kp = kb + (long long)off * step, *vp = vb + (long long)off * step;
           const int left = seen_hi - next;
           if (left >= 16) {
@@ -318,12 +331,10 @@ __global__ void __launch_bounds__(kWarps * 32, kv_attn_resident(NT))
         off += kTile;
         next += kTile;
       }
-      ++issued;
       copy_commit();
     };
-    int ek_q[ST], ev_q[ST];
-#pragma unroll
-    for (int i = 0; i < ST - 1; ++i) issue(ek_q[i], ev_q[i]);
+#pragma unroll 1
+    for (int i = 0; i < ST - 1; ++i) issue();
 
     // ---- queries: row 8 t + n8 of the group as the second operand, fp16,
     // scaled to a largest magnitude of [2^7, 2^8)
@@ -400,155 +411,153 @@ __global__ void __launch_bounds__(kWarps * 32, kv_attn_resident(NT))
 #pragma unroll
     for (int r = 0; r < 2; ++r)
       v_at[r] = L::at(row_of(2 * quad + r), n8 * L::VB / 16) + n8 * L::VB % 16;
-#pragma unroll 1
-    for (int i0 = 0; i0 < steps; i0 += ST) {
+#pragma unroll 1   // (one copy of the body: four overran the instruction cache)
+    for (int i = 0; i < steps; ++i) {
+      copy_wait<ST - 2>();
+      __syncwarp();   // every lane's copies of this step; every lane is done with the last one
+      issue();
+      const int slot = (tile0 + i) * kTile + warp * 16;
+      const uint8_t *st = smem + warp * L::RING + read_at;
+      read_at = read_at + L::STAGE == L::RING ? 0 : read_at + L::STAGE;
+      const uint4 ew = *reinterpret_cast<const uint4 *>(st + 2 * L::HALF);
+      if (ew.z == kBadPage) continue;
+      const uint32_t ek = (ew.x >> ew.z) & 255u, ev = (ew.y >> ew.z) & 255u;
+      // ---- S^T: keys n8, n8 + 8 x rows 2 quad, 2 quad + 1
+      float sc[NT][4];
 #pragma unroll
-      for (int u = 0; u < ST; ++u) {
-        const int i = i0 + u;
-        if (i >= steps) break;
-        copy_wait<ST - 2>();
-        __syncwarp();   // every lane's copies of this step; every lane is done with the last one
-        issue(ek_q[(u + ST - 1) % ST], ev_q[(u + ST - 1) % ST]);
-        const int slot = (tile0 + i) * kTile + warp * 16;
-        if (ek_q[u] < 0) continue;
-        const uint8_t *st = smem + warp * L::RING + (i % ST) * L::STAGE;
-        // ---- S^T: keys n8, n8 + 8 x rows 2 quad, 2 quad + 1
-        float sc[NT][4];
+      for (int t = 0; t < NT; ++t) sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
+      for (int h = 0; h < DH / 64; ++h) {
+        const uint4 ua = *reinterpret_cast<const uint4 *>(st + (k_at ^ (h * 64)));
+        const uint4 ub = *reinterpret_cast<const uint4 *>(st + 8 * DH + (k_at ^ (h * 64)));
+        const uint32_t wa[4] = {ua.x, ua.y, ua.z, ua.w}, wb[4] = {ub.x, ub.y, ub.z, ub.w};
 #pragma unroll
-        for (int h = 0; h < DH / 64; ++h) {
-          const uint4 ua = *reinterpret_cast<const uint4 *>(st + (k_at ^ (h * 64)));
-          const uint4 ub = *reinterpret_cast<const uint4 *>(st + 8 * DH + (k_at ^ (h * 64)));
-          const uint32_t wa[4] = {ua.x, ua.y, ua.z, ua.w}, wb[4] = {ub.x, ub.y, ub.z, ub.w};
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t a0 = widen2(wa[j]), a2 = widen2(wa[j] >> 16);
+          const uint32_t a1 = widen2(wb[j]), a3 = widen2(wb[j] >> 16);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t a0 = widen2(wa[j]), a2 = widen2(wa[j] >> 16);
-            const uint32_t a1 = widen2(wb[j]), a3 = widen2(wb[j] >> 16);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              if constexpr (L::Q_SHARED) {
-                const uint2 q2 = q_sh[(t * KS + 4 * h + j) * 32 + lane];
-                mma_f16(sc[t], a0, a1, a2, a3, q2.x, q2.y);
-              } else {
-                mma_f16(sc[t], a0, a1, a2, a3, qb[t][4 * h + j][0], qb[t][4 * h + j][1]);
-              }
+          for (int t = 0; t < NT; ++t) {
+            if constexpr (L::Q_SHARED) {
+              const uint2 q2 = q_sh[(t * KS + 4 * h + j) * 32 + lane];
+              mma_f16(sc[t], a0, a1, a2, a3, q2.x, q2.y);
+            } else {
+              mma_f16(sc[t], a0, a1, a2, a3, qb[t][4 * h + j][0], qb[t][4 * h + j][1]);
             }
           }
         }
-        // ---- scores in the log2 domain, against the references
-        const float kf = __uint_as_float((uint32_t)ek_q[u] << 23);
-        const float lv = (float)(ev_q[u] - 127);
-        const bool mask = slot + 16 > seen_lo;   // uniform over the warp
-        bool over = false;
+      }
+      // ---- scores in the log2 domain, against the references
+      const float kf = __uint_as_float(ek << 23);
+      const float lv = (float)((int)ev - 127);
+      const bool mask = slot + 16 > seen_lo;   // uniform over the warp
+      bool over = false;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+      for (int t = 0; t < NT; ++t) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            sc[t][k] *= qf[t][k & 1] * kf;
-            if (mask && slot + row_of(n8) + 8 * (k >> 1) >= seen[t][k & 1]) sc[t][k] = -INFINITY;
-          }
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-            over |= fmaxf(sc[t][c], sc[t][2 + c]) - m[t][c] > fminf(kSumLimit, kTop - (lv + m[t][c] - mv[t][c]));
+        for (int k = 0; k < 4; ++k) {
+          sc[t][k] *= qf[t][k & 1] * kf;
+          if (mask && slot + row_of(n8) + 8 * (k >> 1) >= seen[t][k & 1]) sc[t][k] = -INFINITY;
         }
-        if (__any_sync(0xFFFFFFFFu, over)) {
 #pragma unroll
-          for (int t = 0; t < NT; ++t)
+        for (int c = 0; c < 2; ++c)
+          over |= fmaxf(sc[t][c], sc[t][2 + c]) - m[t][c] > fminf(kSumLimit, kTop - (lv + m[t][c] - mv[t][c]));
+      }
+      if (__any_sync(0xFFFFFFFFu, over)) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              float x = fmaxf(sc[t][c], sc[t][2 + c]);
-              x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 4));
-              x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 8));
-              x = ceilf(fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 16)));
-              const float m1 = fmaxf(m[t][c], x), mv1 = fmaxf(mv[t][c], x + lv - kHead);
-              l[t][c] *= ex2(m[t][c] - m1);
-              const float f = ex2(mv[t][c] - mv1);
-              m[t][c] = m1;
-              mv[t][c] = mv1;
-#pragma unroll
-              for (int d = 0; d < DT; ++d) {
-                o[t][d][c] *= f;
-                o[t][d][2 + c] *= f;
-              }
-            }
-        }
-        uint32_t pb[NT][2];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          float y[4];
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            const float f = ex2(lv + m[t][c] - mv[t][c]);
-            const float p0 = ex2(sc[t][c] - m[t][c]), p1 = ex2(sc[t][2 + c] - m[t][c]);
-            l[t][c] += p0 + p1;
-            y[c] = p0 * f;
-            y[2 + c] = p1 * f;
-          }
-          pb[t][0] = transpose8(pack_f16x2(y[0], y[1]));   // rows of P^T: keys
-          pb[t][1] = transpose8(pack_f16x2(y[2], y[3]));
-        }
-        // ---- O^T += V^T P^T
-        uint32_t w[4][VW];
+            float x = fmaxf(sc[t][c], sc[t][2 + c]);
+            x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 4));
+            x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 8));
+            x = ceilf(fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 16)));
+            const float m1 = fmaxf(m[t][c], x), mv1 = fmaxf(mv[t][c], x + lv - kHead);
+            l[t][c] *= ex2(m[t][c] - m1);
+            const float f = ex2(mv[t][c] - mv1);
+            m[t][c] = m1;
+            mv[t][c] = mv1;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const uint8_t *src = st + L::HALF + (r >> 1) * 8 * DH + v_at[r & 1];
-          if constexpr (VW == 4)
-            *reinterpret_cast<uint4 *>(w[r]) = *reinterpret_cast<const uint4 *>(src);
-          else
-            *reinterpret_cast<uint2 *>(w[r]) = *reinterpret_cast<const uint2 *>(src);
-        }
-        if (mask) {
-          // keys that some rows do not see: a NaN among their values may reach only
-          // the rows that do (0 times NaN is NaN), so it leaves the product
-          uint32_t any = 0;
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int j = 0; j < VW; ++j) any |= nan_bytes(w[r][j]);
-          if (__any_sync(0xFFFFFFFFu, any != 0)) {
-            uint32_t bits[4];   // of row r: which of the lane's VB values
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              bits[r] = 0;
-#pragma unroll
-              for (int j = 0; j < VW; ++j) {
-                const uint32_t x = nan_bytes(w[r][j]);
-                w[r][j] &= ~x;
-                bits[r] |= ((x & 1u) | ((x >> 7) & 2u) | ((x >> 14) & 4u) | ((x >> 21) & 8u)) << (4 * j);
-              }
+            for (int d = 0; d < DT; ++d) {
+              o[t][d][c] *= f;
+              o[t][d][2 + c] *= f;
             }
-#pragma unroll 1
-            for (int k = 0; k < 4; ++k) {   // of the quad's lane k, which holds keys of its own
-              uint32_t hit[4];
-#pragma unroll
-              for (int r = 0; r < 4; ++r) hit[r] = __shfl_sync(0xFFFFFFFFu, bits[r], (lane & ~3) | k);
-#pragma unroll
-              for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                  uint32_t here = 0;
-#pragma unroll
-                  for (int r = 0; r < 4; ++r)
-                    here |= slot + row_of(2 * k + (r & 1)) + 8 * (r >> 1) < seen[t][c] ? hit[r] : 0u;
-#pragma unroll
-                  for (int d = 0; d < L::VB; ++d)
-                    if ((here >> d) & 1u) o[t][d >> 1][(d & 1) * 2 + c] = NAN;
-                }
-            }
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < VW; ++j)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {   // bytes 4 j + 2 h, + 1 of the rows: M tile 2 j + h
-            const uint32_t sel = h ? 0x7362u : 0x5140u;
-            const uint32_t lo = __byte_perm(w[0][j], w[1][j], sel), hi = __byte_perm(w[2][j], w[3][j], sel);
-            const uint32_t a0 = widen2(lo), a1 = widen2(lo >> 16), a2 = widen2(hi), a3 = widen2(hi >> 16);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) mma_f16(o[t][2 * j + h], a0, a1, a2, a3, pb[t][0], pb[t][1]);
           }
       }
+      uint32_t pb[NT][2];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        float y[4];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const float f = ex2(lv + m[t][c] - mv[t][c]);
+          const float p0 = ex2(sc[t][c] - m[t][c]), p1 = ex2(sc[t][2 + c] - m[t][c]);
+          l[t][c] += p0 + p1;
+          y[c] = p0 * f;
+          y[2 + c] = p1 * f;
+        }
+        pb[t][0] = transpose8(pack_f16x2(y[0], y[1]));   // rows of P^T: keys
+        pb[t][1] = transpose8(pack_f16x2(y[2], y[3]));
+      }
+      // ---- O^T += V^T P^T
+      uint32_t w[4][VW];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const uint8_t *src = st + L::HALF + (r >> 1) * 8 * DH + v_at[r & 1];
+        if constexpr (VW == 4)
+          *reinterpret_cast<uint4 *>(w[r]) = *reinterpret_cast<const uint4 *>(src);
+        else
+          *reinterpret_cast<uint2 *>(w[r]) = *reinterpret_cast<const uint2 *>(src);
+      }
+      if (mask) {
+        // keys that some rows do not see: a NaN among their values may reach only
+        // the rows that do (0 times NaN is NaN), so it leaves the product
+        uint32_t any = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int j = 0; j < VW; ++j) any |= nan_bytes(w[r][j]);
+        if (__any_sync(0xFFFFFFFFu, any != 0)) {
+          uint32_t bits[4];   // of row r: which of the lane's VB values
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            bits[r] = 0;
+#pragma unroll
+            for (int j = 0; j < VW; ++j) {
+              const uint32_t x = nan_bytes(w[r][j]);
+              w[r][j] &= ~x;
+              bits[r] |= ((x & 1u) | ((x >> 7) & 2u) | ((x >> 14) & 4u) | ((x >> 21) & 8u)) << (4 * j);
+            }
+          }
+#pragma unroll 1
+          for (int k = 0; k < 4; ++k) {   // of the quad's lane k, which holds keys of its own
+            uint32_t hit[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) hit[r] = __shfl_sync(0xFFFFFFFFu, bits[r], (lane & ~3) | k);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                uint32_t here = 0;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                  here |= slot + row_of(2 * k + (r & 1)) + 8 * (r >> 1) < seen[t][c] ? hit[r] : 0u;
+#pragma unroll
+                for (int d = 0; d < L::VB; ++d)
+                  if ((here >> d) & 1u) o[t][d >> 1][(d & 1) * 2 + c] = NAN;
+              }
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < VW; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {   // bytes 4 j + 2 h, + 1 of the rows: M tile 2 j + h
+          const uint32_t sel = h ? 0x7362u : 0x5140u;
+          const uint32_t lo = __byte_perm(w[0][j], w[1][j], sel), hi = __byte_perm(w[2][j], w[3][j], sel);
+          const uint32_t a0 = widen2(lo), a1 = widen2(lo >> 16), a2 = widen2(hi), a3 = widen2(hi >> 16);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) mma_f16(o[t][2 * j + h], a0, a1, a2, a3, pb[t][0], pb[t][1]);
+        }
     }
 
     // ---- the four warps' rows meet
@@ -579,30 +588,55 @@ __global__ void __launch_bounds__(kWarps * 32, kv_attn_resident(NT))
     if (tile0 == 0 && !whole)
       cut = make_int4(b, g, grp, cta_of_tile(at + sq.tiles - 1, total, n_ctas));
     // a unit in several shares: what this one has of it, after (0) or from (1) its start
-    const long long slot = 2ll * cta + (first && tile0 > 0 ? 0 : 1);
-    for (int i = tid; i < L::ROWS * DH / 2; i += kWarps * 32) {
-      const int R = i / (DH / 2), d = (i - R * (DH / 2)) * 2;
-      const RowAt r = row_at(p, s, g, R0 + R);
-      if (!r.live) continue;
-      float mt = kNone, mvt = kNone, lt = 0.f, o0 = 0.f, o1 = 0.f;
+    const long long part = (2ll * cta + (first && tile0 > 0 ? 0 : 1)) * L::ROWS;
+    if (tid < L::ROWS) {   // per row: the warps' weights, and where it goes
+      const RowAt r = row_at(p, s, g, R0 + tid);
+      float mt = kNone, mvt = kNone, lt = 0.f, f[kWarps];
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        mt = fmaxf(mt, s_m[w][R]);
-        mvt = fmaxf(mvt, s_mv[w][R]);
+        mt = fmaxf(mt, s_m[w][tid]);
+        mvt = fmaxf(mvt, s_mv[w][tid]);
       }
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {   // a warp without keys holds zeros
-        lt += s_l[w][R] * ex2(s_m[w][R] - mt);
-        const float f = ex2(s_mv[w][R] - mvt);
-        const float2 x = *reinterpret_cast<const float2 *>(so + (w * L::ROWS + R) * DH + d);
-        o0 = fmaf(f, x.x, o0);
-        o1 = fmaf(f, x.y, o1);
+        lt += s_l[w][tid] * ex2(s_m[w][tid] - mt);
+        f[w] = ex2(s_mv[w][tid] - mvt);
+      }
+      OutScale k{1.f, 1.f};
+      long long to = r.live ? (part + tid) * DH : -1;
+      if (whole) {
+        k = out_scale(mt, mvt, lt);
+        if (r.live) to = r.row * p.out_ld + (long long)r.head * DH;
+        if (r.live && p.lse) p.lse[(long long)r.row * p.hq + r.head] = row_lse(mt, lt);
+      } else {
+        p.part_ml[part + tid] = make_float4(mt, mvt, lt, 0.f);
+      }
+      s_f[tid] = make_float4(f[0] * k.a, f[1] * k.a, f[2] * k.a, f[3] * k.a);
+      s_b[tid] = k.b;
+      s_to[tid] = to;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i0 = 0; i0 < L::ROWS * DH / 4; i0 += kWarps * 32) {
+      const int i = i0 + tid, R = i / (DH / 4), d = (i - R * (DH / 4)) * 4;
+      const long long to = s_to[R];
+      if (to < 0) continue;
+      const float4 f = s_f[R];
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float4 x = *reinterpret_cast<const float4 *>(so + (w * L::ROWS + R) * DH + d);
+        const float fw = w == 0 ? f.x : w == 1 ? f.y : w == 2 ? f.z : f.w;
+        y = make_float4(fmaf(fw, x.x, y.x), fmaf(fw, x.y, y.y), fmaf(fw, x.z, y.z), fmaf(fw, x.w, y.w));
       }
       if (whole) {
-        store2<T>(p, r, d, DH, o0, o1, mt, mvt, lt);
+        const float k = s_b[R];
+        // (0 times an infinite sum would be NaN: such a row is 0)
+        const bool zero = k == 0.f;
+        *reinterpret_cast<uint2 *>(reinterpret_cast<T *>(p.out) + to + d) =
+            zero ? make_uint2(0u, 0u) : make_uint2(pack2<T>(y.x * k, y.y * k), pack2<T>(y.z * k, y.w * k));
       } else {
-        *reinterpret_cast<float2 *>(p.part_o + (slot * L::ROWS + R) * DH + d) = make_float2(o0, o1);
-        if (d == 0) p.part_ml[slot * L::ROWS + R] = make_float4(mt, mvt, lt, 0.f);
+        *reinterpret_cast<float4 *>(p.part_o + to + d) = y;
       }
     }
     __syncthreads();   // the rows are read: the ring may be refilled
@@ -664,7 +698,10 @@ __global__ void __launch_bounds__(kGroups * DH / 2)
     o0 += part[k][d / 2].x;
     o1 += part[k][d / 2].y;
   }
-  store2<T>(p, r, d, DH, o0, o1, m, mv, l);
+  const OutScale k = out_scale(m, mv, l);
+  *reinterpret_cast<uint32_t *>(reinterpret_cast<T *>(p.out) + r.row * p.out_ld + (long long)r.head * DH + d) =
+      k.b == 0.f ? 0u : pack2<T>(o0 * k.a * k.b, o1 * k.a * k.b);
+  if (p.lse && d == 0) p.lse[(long long)r.row * p.hq + r.head] = row_lse(m, l);
 }
 
 template <typename T, int DH, int NT>

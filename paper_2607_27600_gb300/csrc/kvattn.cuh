@@ -14,6 +14,7 @@ struct KvAttnParams {
   float *lse;                   // [n_rows][hq], or null
   const uint8_t *k, *v, *ke, *ve;
   int block;                    // slots per scale
+  long long exp_bytes;          // bytes of ke (and of ve)
   KvLayout pg;
   int hq, hkv, head_dim;
   float scale_log2;             // log2(e) / sqrt(head_dim)
