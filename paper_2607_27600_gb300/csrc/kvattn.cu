@@ -13,10 +13,11 @@
 // Bound by the cache's bytes: a tcgen05 tile of 128 query rows would be
 // nearly all padding, so the products are m16n8k16 with the keys (then the head
 // dimension) on the M side and the 8 * NT query rows of a unit (the heads of a KV head
-// at consecutive positions) on the N side: S^T = K Q^T, O^T = V^T P^T.  A
-// unit's key tiles of 64 are one long line over all units, cut into equal shares
-// for the CTAs of one resident wave, so that ragged batches balance; a unit that
-// spans shares is joined by kv_combine_kernel in share order.
+// at consecutive positions) on the N side: S^T = K Q^T, O^T = V^T P^T.  The key
+// tiles of 64 of all units of a KV head are one long line, cut into equal shares so
+// that ragged batches balance; the KV heads' CTAs of a share are neighbours, so that
+// the pieces of a slot are read at about one time.  A unit that spans shares is
+// joined by kv_combine_kernel in share order.
 //
 // Each warp streams its own 16 keys a step through a ring of its own (cp.async, no
 // barrier wider than the warp).  A copy takes whole 128-byte lines: with the two
@@ -38,13 +39,17 @@ namespace {
 constexpr int kWarps = 4;          // of a CTA, each every fourth 16 keys of a tile
 constexpr int kTile = 16 * kWarps; // keys of a tile
 constexpr int kMinTiles = 2;       // of a share at least
+// What a unit costs besides its tiles (its queries, the first loads' latency, its
+// rows at the end: 5 to 6 us where a tile takes 1), in tiles.
+constexpr int kUnitTiles = 5;
 constexpr uint32_t kBadPage = 0xFFFFFFFFu;   // in place of the scales' place: nothing to see
 constexpr float kNone = -1e30f;    // reference of a row that has seen no key
 constexpr float kSumLimit = 64.f;  // log2 of a term of the sum below
 constexpr float kTop = 15.f, kHead = 8.f;   // log2 of a term above: limit, and what a new reference leaves
 
-// CTAs per SM (registers: the rows' sums grow with NT)
-constexpr int kv_attn_resident(int nt) { return nt == 1 ? 3 : 2; }
+// CTAs per SM.  More streams in flight cost DRAM more than they hide: 64 ragged
+// sequences, 2.25 GB: two 344 us (6.5 TB/s), three 384, four 414.
+constexpr int kResident = 2;
 
 template <int DH, int NT>
 struct KvSmem {
@@ -53,7 +58,7 @@ struct KvSmem {
   static constexpr int VB = DH / 8;               // bytes of a V row that a lane reads
   static constexpr int PIECES = DH / 16;          // 16-byte pieces of a row
   static constexpr int RPC = 32 / PIECES;         // rows of one copy instruction of the warp
-  static constexpr int ST = 4;
+  static constexpr int ST = 3;                    // (four: 7 % slower)
   static constexpr int RING = ST * STAGE;         // bytes of a warp's ring
   // piece c of row r: eight consecutive pieces of 128 bytes differ for the
   // rows that are read at once
@@ -129,14 +134,15 @@ CC_DEV SeqPlan seq_plan(const KvAttnParams &p, int b) {
   q.groups = (q.s.count * (p.hq / p.hkv) + 8 * NT - 1) / (8 * NT);
   return q;
 }
-// Tiles of a sequence's units, and of all sequences'.  A whole warp calls the latter.
-CC_DEV long long seq_tiles(const KvAttnParams &p, const SeqPlan &q) {
-  return (long long)q.groups * q.tiles * p.hkv;
+// Tiles of a sequence's units of one KV head on the line, each unit's own after
+// kUnitTiles for its cost, and of all sequences'.  A whole warp calls the latter.
+CC_DEV long long seq_tiles(const SeqPlan &q) {
+  return (long long)q.groups * (q.tiles + kUnitTiles);
 }
 template <int NT>
 CC_DEV long long total_tiles(const KvAttnParams &p) {
   long long all = 0;
-  for (int b = threadIdx.x & 31; b < p.rows.batch; b += 32) all += seq_tiles(p, seq_plan<NT>(p, b));
+  for (int b = threadIdx.x & 31; b < p.rows.batch; b += 32) all += seq_tiles(seq_plan<NT>(p, b));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
   return all;
@@ -148,7 +154,7 @@ CC_DEV int find_tile(const KvAttnParams &p, long long at, long long &before) {
   const int lane = threadIdx.x & 31;
   before = 0;
   for (int b0 = 0; b0 < p.rows.batch; b0 += 32) {
-    const long long w = b0 + lane < p.rows.batch ? seq_tiles(p, seq_plan<NT>(p, b0 + lane)) : 0;
+    const long long w = b0 + lane < p.rows.batch ? seq_tiles(seq_plan<NT>(p, b0 + lane)) : 0;
     long long sum = w;   // inclusive prefix over the lanes
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -165,11 +171,14 @@ CC_DEV int find_tile(const KvAttnParams &p, long long at, long long &before) {
   }
   return p.rows.batch;
 }
-// CTAs that get a share of `total` tiles; CTA c's starts at total * c / n.
-CC_DEV int sharing_ctas(const KvAttnParams &p, long long total) {
-  return (int)max(1ll, min((long long)p.ctas, (total + kMinTiles - 1) / kMinTiles));
+// Shares of the line of `total` tiles where `resident` are worked on at once; share
+// c starts at total * c / n.  (Three times as many shorter ones, so that a slower SM
+// takes fewer, measured within 1 %.)
+__host__ __device__ __forceinline__ int line_shares(int resident, long long total) {
+  const long long few = (total + kMinTiles - 1) / kMinTiles;
+  return few >= resident ? resident : few < 1 ? 1 : (int)few;
 }
-CC_DEV int cta_of_tile(long long t, long long total, int n) {   // the last c with total * c / n <= t
+CC_DEV int share_of_tile(long long t, long long total, int n) {   // the last c with total * c / n <= t
   return (int)(((t + 1) * n - 1) / total);
 }
 
@@ -206,7 +215,7 @@ CC_DEV float row_lse(float m, float l) {
 // the kernel
 // ---------------------------------------------------------------------------
 template <typename T, int DH, int NT>
-__global__ void __launch_bounds__(kWarps * 32, kv_attn_resident(NT))
+__global__ void __launch_bounds__(kWarps * 32, kResident)
     kv_attn_kernel(const __grid_constant__ KvAttnParams p) {
   using L = KvSmem<DH, NT>;
   constexpr int KS = DH / 16;        // k steps of K Q^T
@@ -221,14 +230,15 @@ __global__ void __launch_bounds__(kWarps * 32, kv_attn_resident(NT))
   pdl_trigger();   // the combine may launch: it waits for this grid
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n8 = lane >> 2, quad = lane & 3;
   const long long total = total_tiles<NT>(p);
-  const int n_ctas = sharing_ctas(p, total), cta = blockIdx.x;
+  const int n_shares = min(p.shares, line_shares(p.resident, total)), cta = blockIdx.x;
+  const int share = cta / p.hkv, g = cta - share * p.hkv;
   int4 cut = make_int4(0, 0, 0, -1);   // the unit that starts here and goes on in the next share
-  if (cta >= n_ctas) {
+  if (share >= n_shares) {
     if (tid == 0) p.cut[cta] = cut;
     return;
   }
-  long long at = total * cta / n_ctas;
-  const long long end = total * (cta + 1) / n_ctas;
+  long long at = total * share / n_shares;
+  const long long end = total * (share + 1) / n_shares;
   // reported once, by the first CTA: sequences whose rows or lengths are bad
   if (cta == 0)
     for (int b = tid; b < p.rows.batch; b += kWarps * 32)
@@ -241,14 +251,18 @@ __global__ void __launch_bounds__(kWarps * 32, kv_attn_resident(NT))
   SeqPlan sq = seq_plan<NT>(p, b);
   bool first = true;   // the share's first segment
   while (at < end) {
-    while (before + seq_tiles(p, sq) <= at) {   // the next sequence with rows
-      before += seq_tiles(p, sq);
+    while (before + seq_tiles(sq) <= at) {   // the next sequence with rows
+      before += seq_tiles(sq);
       sq = seq_plan<NT>(p, ++b);
     }
     const long long in_seq = at - before;
-    const int unit = (int)(in_seq / sq.tiles), g = unit / sq.groups, grp = unit - g * sq.groups;
-    const int tile0 = (int)(in_seq - (long long)unit * sq.tiles);
-    const int tile1 = (int)min((long long)sq.tiles, tile0 + (end - at));
+    const int span = sq.tiles + kUnitTiles;
+    const int grp = (int)(in_seq / span), from = (int)(in_seq - (long long)grp * span);
+    const int to = (int)min((long long)span, from + (end - at));
+    const long long unit_at = at - from;
+    at += to - from;
+    const int tile0 = max(0, from - kUnitTiles), tile1 = to - kUnitTiles;
+    if (tile1 <= 0) break;   // the share ends before the unit's first tile
     const SeqRows s = sq.s;
     const int gs = p.pg.head_major ? 0 : g;
     const int G = p.hq / p.hkv, R0 = grp * L::ROWS;
@@ -489,7 +503,8 @@ __global__ void __launch_bounds__(kWarps * 32, kv_attn_resident(NT))
         float y[4];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const float f = ex2(lv + m[t][c] - mv[t][c]);
+          // (finite: a key of probability 0 may have any scale)
+          const float f = ex2(fminf(lv + m[t][c] - mv[t][c], 126.f));
           const float p0 = ex2(sc[t][c] - m[t][c]), p1 = ex2(sc[t][2 + c] - m[t][c]);
           l[t][c] += p0 + p1;
           y[c] = p0 * f;
@@ -586,7 +601,7 @@ __global__ void __launch_bounds__(kWarps * 32, kv_attn_resident(NT))
     __syncthreads();
     const bool whole = tile0 == 0 && tile1 == sq.tiles;
     if (tile0 == 0 && !whole)
-      cut = make_int4(b, g, grp, cta_of_tile(at + sq.tiles - 1, total, n_ctas));
+      cut = make_int4(b, g, grp, share_of_tile(unit_at + span - 1, total, n_shares));
     // a unit in several shares: what this one has of it, after (0) or from (1) its start
     const long long part = (2ll * cta + (first && tile0 > 0 ? 0 : 1)) * L::ROWS;
     if (tid < L::ROWS) {   // per row: the warps' weights, and where it goes
@@ -640,7 +655,6 @@ __global__ void __launch_bounds__(kWarps * 32, kv_attn_resident(NT))
       }
     }
     __syncthreads();   // the rows are read: the ring may be refilled
-    at += tile1 - tile0;
     first = false;
   }
   if (tid == 0) p.cut[cta] = cut;
@@ -660,15 +674,15 @@ __global__ void __launch_bounds__(kGroups * DH / 2)
   __shared__ float part_l[kGroups];
   pdl_trigger();
   pdl_wait();
-  const int c0 = blockIdx.x, R = blockIdx.y;
-  const int4 u = p.cut[c0];   // sequence, KV head, group of rows, last share (none: no unit)
+  const int c0 = blockIdx.x / p.hkv, R = blockIdx.y;
+  const int4 u = p.cut[blockIdx.x];   // sequence, KV head, group of rows, last share (none: no unit)
   if (u.w <= c0) return;
   const RowAt r = row_at(p, seq_rows(p.rows, u.x, !p.memory_only), u.y, u.z * ROWS + R);
   if (!r.live) return;
   const int c1 = u.w;
   const int part_id = threadIdx.x / (DH / 2), d = (threadIdx.x - part_id * (DH / 2)) * 2;
   // share c0 holds the unit's start, those after it start inside the unit
-  auto slot = [&](int c) { return (2ll * c + (c == c0 ? 1 : 0)) * ROWS + R; };
+  auto slot = [&](int c) { return (2ll * ((long long)c * p.hkv + u.y) + (c == c0 ? 1 : 0)) * ROWS + R; };
   float m = kNone, mv = kNone;
   for (int c = c0 + (threadIdx.x & 31); c <= c1; c += 32) {
     const float4 x = p.part_ml[slot(c)];
@@ -719,7 +733,7 @@ cudaError_t launch_as(const KvAttnParams &p, cudaStream_t st) {
   kern<<<(unsigned)p.ctas, kWarps * 32, L::BYTES, st>>>(p);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  return launch_pdl(kv_combine_kernel<T, DH, NT>, dim3((unsigned)p.ctas, L::ROWS),
+  return launch_pdl(kv_combine_kernel<T, DH, NT>, dim3((unsigned)p.ctas, (unsigned)std::min<long long>(L::ROWS, (long long)p.rows.max_rows * (p.hq / p.hkv))),
                     dim3(kGroups * DH / 2), 0, st, p);
 }
 template <typename T, int DH>
@@ -840,7 +854,11 @@ __global__ void __launch_bounds__(256)
 void kv_attn_plan(KvAttnParams &p, int sms) {
   const long long rows = (long long)p.rows.max_rows * (p.hq / p.hkv);
   p.nt = (int)std::min<long long>(4, (rows + 7) / 8);
-  p.ctas = sms * kv_attn_resident(p.nt);
+  p.resident = std::max(1, sms * kResident / p.hkv);
+  // (as if every sequence were as long as its buffer)
+  const long long groups = (rows + 8 * p.nt - 1) / (8 * p.nt), tiles = (p.rows.cap + kTile - 1) / kTile + kUnitTiles;
+  p.shares = line_shares(p.resident, p.rows.batch * groups * tiles);
+  p.ctas = p.shares * p.hkv;
 }
 
 size_t kv_attn_part_bytes(const KvAttnParams &p) {

@@ -20,7 +20,9 @@ struct KvAttnParams {
   float scale_log2;             // log2(e) / sqrt(head_dim)
   // set by kv_attn_plan
   int nt;                       // query rows of a unit / 8: 1 to 4
-  int ctas;                     // CTAs that share the units' key tiles
+  int resident;                 // shares of a KV head's key tiles that the SMs work on at once
+  int shares;                   // shares at most, each one CTA per KV head
+  int ctas;                     // shares * hkv
   float *part_o;                // [2 * ctas][8 * nt][head_dim]: what a CTA leaves of the unit
   float4 *part_ml;              // [2 * ctas][8 * nt]            before and after its share
   int4 *cut;                    // [ctas]: the unit that starts in a CTA's share and goes on

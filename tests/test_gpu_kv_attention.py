@@ -189,6 +189,30 @@ def test_scales_far_apart(pkg, dtype):
     check(got, ls, want[0], want[1], want[2] + tiny, eps)
 
 
+def test_scales_at_the_ends_of_the_range(pkg):
+    """Value scales of 2^-110 and 2^110 side by side, where the large ones have next to no
+    weight and where they have all."""
+    rng = np.random.default_rng(13)
+    s, cap, block = shape(2, 1, 64), 256, 16
+    codes, exps = {}, {}
+    for n in "kv":
+        codes[n], exps[n] = quantised(rng, 2, cap, 1, 64, block, (0.9, 1.1))
+    big = np.arange(cap // block) % 3 == 1
+    exps["v"][:, :, 0] = np.where(big, 237, 17)
+    k = values(codes["k"], exps["k"]).copy()
+    q = np.zeros((2, 2, 64))
+    # sequence 0 shuns the blocks of large scale by 300 in score, sequence 1 seeks them
+    codes["k"][:, :, 0, 0] = np.where(np.repeat(big, block), 0x7E, 0xFE)   # +-448
+    exps["k"][:] = 127
+    q[0, :, 0], q[1, :, 0] = -2.5, 2.5
+    k, v = values(codes["k"], exps["k"]), values(codes["v"], exps["v"])
+    c = DeviceCache(pkg, codes, exps, [255, 255], "slot")
+    got, ls = attend(pkg, s, c, [1, 1], columns([q], torch.bfloat16)[0])
+    want = oracle.attend_rows(q, k, v, [255, 255], [0, 1, 2])
+    assert 2.0 ** -112 < np.abs(want[0][0]).max() < 2.0 ** -90 and np.abs(want[0][1]).max() > 2.0 ** 100
+    check(got, ls, *want, 2.0 ** -8)
+
+
 def test_one_key_dominates(pkg):
     """Scores over hundreds: the references rise late, early and not at all."""
     rng = np.random.default_rng(4)
