@@ -1,10 +1,14 @@
 // logprob.cu -- log-probability of a given token, entropy and the largest
 // alternatives of each row of logits, in one pass over the logits.
 //
-//   S = sum e^(z - m), W = sum e^(z - m) (z - m) with a running maximum m;
-//   ln p_t = (z_t - m) - ln S,  H = ln S - W / S.
-// m is kept exact (every 2 vectors), not raised lazily: with a reference well
-// below the maximum the two terms of H would cancel.
+// With c = log2(e) and a running maximum m, t = z c - m c:
+//   S = sum 2^t, W = sum 2^t t;  ln p_k = (z_k c - m c - log2 S) / c,
+//   H = (log2 S - W / S) / c.
+// m is exact after every four vectors, not raised lazily: with a reference well
+// below the maximum the two terms of H would cancel.  A forbidden logit (-inf, or
+// any below -2^20) is raised to -2^20, whose term is 0 in both sums; a row whose
+// maximum lies near there or past 2^20 (nothing allowed, the type's lowest value
+// everywhere) is done again from t = (z - m) c.
 //
 // Alternatives without a second pass: each thread keeps its largest logit and
 // where that is.  The top-th largest of the CTA's thread maxima is a lower bound
@@ -12,12 +16,11 @@
 // candidates, and their few dozen vectors are read again (from L2).  Keys
 // of (value, lower position first) are all distinct, so ties change nothing.
 //
-// Bound by HBM.  A CTA takes a row; with few rows a cluster of up to 8 CTAs
-// does, a contiguous segment each, and rank 0 joins their sums and sorted lists
-// through distributed shared memory.
+// Bound by HBM, and close behind by issue slots: 16-bit maxima and fp32 sums in pairs
+// keep it under 6 instructions per logit.  A CTA takes a row; with few rows a
+// cluster of up to 8 CTAs does, a contiguous segment each, and rank 0 joins their
+// sums and sorted lists through distributed shared memory.
 #include "logprob.cuh"
-
-#include <float.h>
 
 #include <type_traits>
 
@@ -25,13 +28,20 @@ namespace cc {
 
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kFar = -200.f;   // e^x is 0 in fp32 below
+constexpr float kC = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+// A forbidden logit.  A power of two, so that kLow c is no rounding away from itself
+// (at the maxima that the sums take, up to 2^20, z c and m c are 0.1 apart at most).
+constexpr float kLow = -0x1p20f;
+constexpr float kFar = -200.f;   // 2^x is 0 in fp32 below
 
 CC_DEV float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+CC_DEV float max_nan(float a, float b) {   // NaN if either is
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
   return y;
 }
 CC_DEV uint4 load_once(const void *p) {
@@ -41,6 +51,10 @@ CC_DEV uint4 load_once(const void *p) {
   return v;
 }
 
+CC_DEV void copy16(uint32_t dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
 template <typename T>
 CC_DEV float to_float(T x) {
   if constexpr (std::is_same_v<T, float>) return x;
@@ -48,43 +62,68 @@ CC_DEV float to_float(T x) {
   else return __bfloat162float(x);
 }
 
-// One row as 16-byte vectors: vector v holds elements v * N - skip + [0, N), of
-// which those outside [0, vocab) do not exist.
+// Two logits of a vector's word (one, fp32) as fp32.
+template <typename T>
+CC_DEV float2 widen_word(uint32_t w) {
+  if constexpr (std::is_same_v<T, __half>) return __half22float2(*reinterpret_cast<const __half2 *>(&w));
+  else return make_float2(bf16_lo(w), bf16_hi(w));
+}
+// Larger of the logits, word by word (NaN drops out).
+template <typename T>
+CC_DEV uint32_t max_word(uint32_t a, uint32_t b) {
+  if constexpr (std::is_same_v<T, float>) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  } else {
+    using V = std::conditional_t<std::is_same_v<T, __half>, __half2, __nv_bfloat162>;
+    const V r = __hmax2(*reinterpret_cast<const V *>(&a), *reinterpret_cast<const V *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+  }
+}
+template <typename T>
+CC_DEV uint32_t max_vec(uint4 u) {
+  return max_word<T>(max_word<T>(u.x, u.y), max_word<T>(u.z, u.w));
+}
+template <typename T>
+CC_DEV float max_of_word(uint32_t w) {
+  if constexpr (std::is_same_v<T, float>) {
+    return __uint_as_float(w);
+  } else {
+    const float2 f = widen_word<T>(w);
+    return fmaxf(f.x, f.y);
+  }
+}
+
+// One row as 16-byte vectors: vector v holds elements v * N - skip + [0, N).
+// Vectors [lo, hi) lie in the row as a whole; the few elements before and after
+// them are its edges.
 template <typename T>
 struct Row {
   static constexpr int N = 16 / sizeof(T);
   const T *base;   // 16-byte aligned, `skip` elements before the row
-  int skip, vocab;
+  int skip, vocab, lo, hi;
   CC_DEV Row(const T *row, int n) : vocab(n) {
     skip = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
     base = row - skip;
+    lo = skip ? 1 : 0;
+    hi = max(lo, (int)(((long long)vocab + skip) / N));
   }
-  CC_DEV int vectors() const { return (int)(((long long)vocab + skip + N - 1) / N); }
   CC_DEV int first(int v) const { return v * N - skip; }
-  CC_DEV bool whole(int v) const { return first(v) >= 0 && (long long)first(v) + N <= vocab; }
+  CC_DEV const T *at(int v) const { return base + (long long)v * N; }
+  // Edge element i, in ascending position (or -1).
+  CC_DEV int edge(int i) const {
+    const int before = min(vocab, lo * N - skip);
+    const int e = i < before ? i : max(first(hi), before) + i - before;
+    return e < vocab ? e : -1;
+  }
   CC_DEV void widen(uint4 u, float (&x)[N]) const {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (std::is_same_v<T, float>) {
         x[i] = __uint_as_float(w[i]);
-      } else if constexpr (std::is_same_v<T, __half>) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
-        x[2 * i] = f.x, x[2 * i + 1] = f.y;
       } else {
-        x[2 * i] = bf16_lo(w[i]), x[2 * i + 1] = bf16_hi(w[i]);
-      }
-    }
-  }
-  // (a vector at the row's ends: what lies outside reads as -inf)
-  CC_DEV void load(int v, float (&x)[N]) const {
-    if (whole(v)) {
-      widen(load_once(base + (long long)v * N), x);
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int e = first(v) + i;
-        x[i] = e >= 0 && e < vocab ? to_float(base[(long long)v * N + i]) : -INFINITY;
+        const float2 f = widen_word<T>(w[i]);
+        x[2 * i] = f.x, x[2 * i + 1] = f.y;
       }
     }
   }
@@ -131,14 +170,29 @@ CC_DEV Key insert_key(Key list, Key k) {
   return lane < at ? list : lane == at ? k : up;
 }
 
+CC_DEV float scaled(float m) { return __fmul_rn(m, kC); }   // (rounded, whatever it is added to)
+
+// Merges the first n lists into lists[0].  The whole CTA calls; they are written
+// and every thread has seen it.
+CC_DEV void merge_tree(Key (*lists)[32], int n, int warp, int lane) {
+#pragma unroll 1
+  while (n > 1) {
+    const int half = (n + 1) / 2;
+    if (warp + half < n) lists[warp][lane] = merge_lists(lists[warp][lane], lists[warp + half][lane]);
+    __syncthreads();
+    n = half;
+  }
+}
+
+// m: the maximum, at least kLow; s, w: the sums against scaled(m).
 struct Sums {
   float m, s, w;
 };
 CC_DEV Sums join(Sums a, Sums b) {
   const float m = fmaxf(a.m, b.m);
-  const float da = fmaxf(a.m - m, kFar), db = fmaxf(b.m - m, kFar);
-  // a maximum of +inf: its own sum is NaN already
-  const float fa = ex2(da * kLog2e), fb = ex2(db * kLog2e);
+  // (a maximum of +inf: the sums are NaN already)
+  const float mc = scaled(m), da = fmaxf(scaled(a.m) - mc, kFar), db = fmaxf(scaled(b.m) - mc, kFar);
+  const float fa = ex2(da), fb = ex2(db);
   return {m, a.s * fa + b.s * fb, fa * (a.w + a.s * da) + fb * (b.w + b.s * db)};
 }
 CC_DEV Sums warp_join(Sums x) {
@@ -149,10 +203,35 @@ CC_DEV Sums warp_join(Sums x) {
   return x;
 }
 
+// The sums of a word's one or two logits against mc (pairs where there are two).
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 2)
+CC_DEV void add_word(uint32_t w, float2 mc, float2 &s, float2 &ws) {
+  float2 z;
+  if constexpr (std::is_same_v<T, float>) {
+    z = make_float2(__uint_as_float(w), 0.f);
+    const float t = fmaf(max_nan(z.x, kLow), kC, mc.x), e = ex2(t);
+    s.x += e;
+    ws.x = fmaf(e, t, ws.x);
+  } else {
+    if constexpr (std::is_same_v<T, __half>) {
+      z = widen_word<T>(w);
+      z = make_float2(max_nan(z.x, kLow), max_nan(z.y, kLow));
+    } else {   // both at once
+      const __nv_bfloat162 low = __floats2bfloat162_rn(kLow, kLow);
+      const __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162 *>(&w), low);
+      z = widen_word<T>(*reinterpret_cast<const uint32_t *>(&r));
+    }
+    const float2 t = __ffma2_rn(z, make_float2(kC, kC), mc), e = make_float2(ex2(t.x), ex2(t.y));
+    s = __fadd2_rn(s, e);
+    ws = __ffma2_rn(e, t, ws);
+  }
+}
+
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS)
     token_logprob_kernel(const __grid_constant__ LogprobParams p) {
-  constexpr int N = Row<T>::N;
+  constexpr int N = Row<T>::N, kWarps = THREADS / 32;
+  extern __shared__ __align__(16) uint8_t stage_mem[];   // two batches: [2][4][THREADS] vectors
   __shared__ Key lists[kWarps][32];
   __shared__ float sums[kWarps][3];
   __shared__ Key part_list[8][32];   // rank 0: the cluster's
@@ -165,69 +244,80 @@ __global__ void __launch_bounds__(kThreads, 2)
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   const T *row_ptr = reinterpret_cast<const T *>(p.logits) + (long long)r * p.ld;
   const Row<T> row(row_ptr, p.vocab);
-  const int nv = row.vectors();
-  const int v0 = (int)((long long)nv * rank / cl), v1 = (int)((long long)nv * (rank + 1) / cl);
+  const int nv = row.hi - row.lo;
+  const int v0 = row.lo + (int)((long long)nv * rank / cl), v1 = row.lo + (int)((long long)nv * (rank + 1) / cl);
 
-  // ---- one pass: sums, and the thread's largest logit
-  Sums a{-FLT_MAX, 0.f, 0.f};
+  // ---- one pass: sums, and the thread's largest logit.  Batches of four vectors
+  // (the last one of fewer); a thread copies ahead what it will read itself: no barrier
+  Sums a{kLow, 0.f, 0.f};
   float best = -INFINITY;
-  int best_v = -1;
-  auto add = [&](const float (&x)[N], const float (&y)[N], int vx, int vy) {
-    float mx = -INFINITY, my = -INFINITY;   // (NaN drops out)
+  const int mine_n = max(0, (v1 - v0 - tid + THREADS - 1) / THREADS);   // this thread's vectors
+  const int full = mine_n / 4, rest = mine_n % 4;
+  int best_v = mine_n > 0 ? v0 + tid : -1, v = v0 + tid;
+  const uint8_t *src = reinterpret_cast<const uint8_t *>(row.at(v));
+  const uint32_t ring = smem_u32(stage_mem) + tid * 16;
+  auto issue = [&](int i, int st) {   // batch i
+    const uint32_t to = ring + st * (4 * THREADS * 16);
+    if (i < full) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) mx = fmaxf(mx, x[i]), my = fmaxf(my, y[i]);
-    if (mx > best || best_v < 0) best = mx, best_v = vx;
-    if (my > best) best = my, best_v = vy;
-    const float m = fmaxf(a.m, fmaxf(mx, my));
-    const float d = fmaxf(a.m - m, kFar), f = ex2(d * kLog2e);
-    float s = 0.f, w = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float dx = x[i] - m, dy = y[i] - m;
-      const float ex = ex2(dx * kLog2e), ey = ex2(dy * kLog2e);
-      s += ex + ey;
-      w = fmaf(ex, fmaxf(dx, kFar), w);   // (0 times -inf would be NaN)
-      w = fmaf(ey, fmaxf(dy, kFar), w);
+      for (int k = 0; k < 4; ++k) copy16(to + k * THREADS * 16, src + k * THREADS * 16);
+      src += 4 * THREADS * 16;
+    } else if (i == full) {
+      for (int k = 0; k < rest; ++k) copy16(to + k * THREADS * 16, src + k * THREADS * 16);
     }
-    a.w = fmaf(f, fmaf(a.s, d, a.w), w);
-    a.s = fmaf(a.s, f, s);
-    a.m = m;
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  int v = v0 + tid;
-  for (; v + 3 * kThreads < v1; v += 4 * kThreads) {
-    uint4 u[4];
-    if (row.whole(v) && row.whole(v + 3 * kThreads)) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) u[k] = load_once(row.base + (long long)(v + k * kThreads) * N);
-      float x[N], y[N];
-      row.widen(u[0], x);
-      row.widen(u[1], y);
-      add(x, y, v, v + kThreads);
-      row.widen(u[2], x);
-      row.widen(u[3], y);
-      add(x, y, v + 2 * kThreads, v + 3 * kThreads);
-    } else {
+  issue(0, 0);
 #pragma unroll 1
-      for (int k = 0; k < 4; k += 2) {
-        float x[N], y[N];
-        row.load(v + k * kThreads, x);
-        row.load(v + (k + 1) * kThreads, y);
-        add(x, y, v + k * kThreads, v + (k + 1) * kThreads);
+  for (int i = 0; i < full + (rest ? 1 : 0); ++i, v += 4 * THREADS) {
+    issue(i + 1, (i + 1) & 1);
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    const uint4 *here = reinterpret_cast<const uint4 *>(stage_mem) + (i & 1) * 4 * THREADS + tid;
+    uint4 u[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) u[k] = here[k * THREADS];
+    if (i == full) {
+      constexpr uint32_t kInf = std::is_same_v<T, float> ? 0xFF800000u
+                                : std::is_same_v<T, __half> ? 0xFC00FC00u : 0xFF80FF80u;
+#pragma unroll
+      for (int k = 1; k < 4; ++k)
+        if (k >= rest) u[k] = make_uint4(kInf, kInf, kInf, kInf);
+    }
+    uint32_t mw[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mw[k] = max_vec<T>(u[k]);
+    const float top = max_of_word<T>(max_word<T>(max_word<T>(mw[0], mw[1]), max_word<T>(mw[2], mw[3])));
+    if (top > best) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float x = max_of_word<T>(mw[k]);
+        if (x > best) best = x, best_v = v + k * THREADS;
       }
     }
-  }
-#pragma unroll 1
-  for (; v < v1; v += 2 * kThreads) {
-    float x[N], y[N];
-    row.load(v, x);
-    const bool two = v + kThreads < v1;
-    if (two) {
-      row.load(v + kThreads, y);
-    } else {
+    const float m = fmaxf(a.m, top), mc = scaled(m);
+    const float d = fmaxf(scaled(a.m) - mc, kFar), f = ex2(d);
+    const float2 nmc = make_float2(-mc, -mc);
+    float2 s = make_float2(0.f, 0.f), ws = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int i = 0; i < N; ++i) y[i] = -INFINITY;
+    for (int k = 0; k < 4; ++k) {
+      add_word<T>(u[k].x, nmc, s, ws);
+      add_word<T>(u[k].y, nmc, s, ws);
+      add_word<T>(u[k].z, nmc, s, ws);
+      add_word<T>(u[k].w, nmc, s, ws);
     }
-    add(x, y, v, v + kThreads);
+    a.w = fmaf(f, fmaf(a.s, d, a.w), ws.x + ws.y);
+    a.s = fmaf(a.s, f, s.x + s.y);
+    a.m = m;
+  }
+  // the edges: up to 2 N - 2 elements, a lane each
+  int edge = -1;
+  if (rank == 0 && warp == 0) {
+    edge = row.edge(lane);
+    if (edge >= 0) {
+      const float z = to_float(row_ptr[edge]), m = fmaxf(z, kLow);
+      const float t = fmaf(max_nan(z, kLow), kC, -scaled(m)), e = ex2(t);
+      a = join(a, {m, e, e * t});
+    }
   }
   a = warp_join(a);
   if (lane == 0) sums[warp][0] = a.m, sums[warp][1] = a.s, sums[warp][2] = a.w;
@@ -239,11 +329,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     const Key mine = best_v < 0 ? 0 : make_key(ordered(best), (uint32_t)best_v);
     lists[warp][lane] = sort_list(mine);
     __syncthreads();
-#pragma unroll 1
-    for (int w = kWarps / 2; w > 0; w >>= 1) {
-      if (warp < w) lists[warp][lane] = merge_lists(lists[warp][lane], lists[warp + w][lane]);
-      __syncthreads();
-    }
+    merge_tree(lists, kWarps, warp, lane);
     const Key least = lists[0][p.top - 1];   // the top-th largest thread maximum
     if (mine != 0 && mine >= least) marked[atomicAdd(&n_marked, 1)] = tid;
     __syncthreads();
@@ -251,16 +337,15 @@ __global__ void __launch_bounds__(kThreads, 2)
 #pragma unroll 1
     for (int k = warp; k < n_marked; k += kWarps) {
 #pragma unroll 1
-      for (int u0 = v0 + marked[k]; u0 < v1; u0 += 32 * kThreads) {
-        const int u = u0 + lane * kThreads;
+      for (int u0 = v0 + marked[k]; u0 < v1; u0 += 32 * THREADS) {
+        const int u = u0 + lane * THREADS;
         float x[N];
-        if (u < v1) row.load(u, x);
+        row.widen(u < v1 ? load_once(row.at(u)) : make_uint4(0, 0, 0, 0), x);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           const int e = row.first(u) + i;
-          const bool in = u < v1 && e >= 0 && e < p.vocab;
-          const uint32_t o = in ? ordered(x[i]) : 0u;
-          unsigned cand = __ballot_sync(0xFFFFFFFFu, in && make_key(o, (uint32_t)u) >= least);
+          const uint32_t o = ordered(x[i]);
+          unsigned cand = __ballot_sync(0xFFFFFFFFu, u < v1 && make_key(o, (uint32_t)u) >= least);
           while (cand) {
             const int src = __ffs(cand) - 1;
             cand &= cand - 1;
@@ -269,17 +354,20 @@ __global__ void __launch_bounds__(kThreads, 2)
         }
       }
     }
+    for (unsigned cand = __ballot_sync(0xFFFFFFFFu, edge >= 0); cand; cand &= cand - 1) {
+      const Key k = edge >= 0 ? make_key(ordered(to_float(row_ptr[edge])), (uint32_t)edge) : 0;
+      list = insert_key(list, __shfl_sync(0xFFFFFFFFu, k, __ffs(cand) - 1));
+    }
     __syncthreads();   // every thread has read `least`
     lists[warp][lane] = list;
+    __syncthreads();
+    merge_tree(lists, min(kWarps, max(n_marked, 1)), warp, lane);
+    list = lists[0][lane];
+  } else {
+    __syncthreads();
   }
-  __syncthreads();
   if (warp == 0) {
-    if (p.top > 0) {
-      const int used = min(kWarps, max(n_marked, 1));
-      list = lists[0][lane];
-      for (int w = 1; w < used; ++w) list = merge_lists(list, lists[w][lane]);
-    }
-    a = lane < kWarps ? Sums{sums[lane][0], sums[lane][1], sums[lane][2]} : Sums{-FLT_MAX, 0.f, 0.f};
+    a = lane < kWarps ? Sums{sums[lane][0], sums[lane][1], sums[lane][2]} : Sums{kLow, 0.f, 0.f};
     a = warp_join(a);
   }
 
@@ -296,46 +384,65 @@ __global__ void __launch_bounds__(kThreads, 2)
       }
     }
     cluster_sync();
-    if (rank != 0 || warp != 0) return;
-    for (int c = 1; c < cl; ++c) {
-      if (p.top > 0) list = merge_lists(list, part_list[c][lane]);
-      a = join(a, {part_sums[c][0], part_sums[c][1], part_sums[c][2]});
+    if (rank != 0) return;
+    if (p.top > 0) {
+      merge_tree(part_list, cl, warp, lane);
+      list = part_list[0][lane];
+    }
+    if (warp == 0) {
+      a = lane < cl ? Sums{part_sums[lane][0], part_sums[lane][1], part_sums[lane][2]} : Sums{kLow, 0.f, 0.f};
+      a = warp_join(a);
     }
   }
   if (warp != 0) return;
-  const float ln_s = logf(a.s);
+  // ---- a row without a maximum that the sums can stand on: again, from differences
+  float largest = a.m;
+  const bool odd = a.m <= 0.5f * kLow || a.m >= -kLow;
+  if (odd) {
+    largest = -INFINITY;
+    for (int e = lane; e < p.vocab; e += 32) largest = fmaxf(largest, to_float(row_ptr[e]));
+    largest = warp_max(largest);
+    float s = 0.f, w = 0.f;
+    for (int e = lane; e < p.vocab; e += 32) {
+      const float z = to_float(row_ptr[e]);
+      if (z == -INFINITY) continue;
+      const float t = (z - largest) * kC, x = ex2(t);
+      s += x;
+      w = fmaf(x, max_nan(t, kFar), w);
+    }
+    a.s = warp_sum(s);
+    a.w = warp_sum(w);
+  }
+  // a row that allows nothing has no distribution
+  const float log_s = a.s > 0.f ? log2f(a.s) : NAN;
+  auto log_prob = [&](float z) {
+    // (z c of a logit far below would be coarse, or infinite)
+    return odd || fabsf(z) >= -kLow ? (z - largest) - log_s * kLn2
+                                    : (fmaf(z, kC, -scaled(a.m)) - log_s) * kLn2;
+  };
   if (lane == 0) {
-    // a row that allows nothing has no distribution
-    const float none = a.s > 0.f ? 0.f : NAN;
     if (p.logprob) {
       const int t = p.targets[r];
-      float lp = 0.f;
-      if (t >= 0 && t < p.vocab) lp = to_float(row_ptr[t]) - a.m - ln_s + none;
-      else if (t != -1) set_status(p.status, CC_ERR_DEVICE_ARG);
-      p.logprob[r] = lp;
+      const bool in = t >= 0 && t < p.vocab;
+      if (!in && t != -1) set_status(p.status, CC_ERR_DEVICE_ARG);
+      p.logprob[r] = in ? log_prob(to_float(row_ptr[t])) : 0.f;
     }
-    if (p.entropy) p.entropy[r] = ln_s - a.w / a.s;
+    if (p.entropy) p.entropy[r] = (log_s - a.w / a.s) * kLn2;
   }
   if (lane < p.top) {
     if (p.top_ids) p.top_ids[(long long)r * p.top + lane] = (int32_t)key_at(list);
     if (p.top_logprob)
-      p.top_logprob[(long long)r * p.top + lane] =
-          from_ordered((uint32_t)(list >> 32)) - a.m - ln_s + (a.s > 0.f ? 0.f : NAN);
+      p.top_logprob[(long long)r * p.top + lane] = log_prob(from_ordered((uint32_t)(list >> 32)));
   }
 }
 
-template <typename T>
-cudaError_t launch_as(const LogprobParams &p, int sms, cudaStream_t st) {
-  // CTAs of a row: until two waves of the SMs' CTAs are in flight, each with a
-  // few vectors per thread
-  int cl = 1;
-  while (cl < 8 && (long long)p.rows * cl * 2 <= 2 * sms &&
-         (long long)p.vocab >= 4LL * cl * kThreads * (16 / (int)sizeof(T)))
-    cl *= 2;
+template <typename T, int THREADS>
+cudaError_t launch_as(const LogprobParams &p, int cl, cudaStream_t st) {
   if ((long long)p.rows * cl > 0x7FFFFFFFll) return cudaErrorInvalidValue;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(p.rows * cl));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = 2 * 4 * THREADS * 16;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -343,16 +450,39 @@ cudaError_t launch_as(const LogprobParams &p, int sms, cudaStream_t st) {
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, token_logprob_kernel<T>, p);
+  static bool attr_set[64] = {};
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (dev < 64 && !attr_set[dev]) {
+    const cudaError_t e = cudaFuncSetAttribute(token_logprob_kernel<T, THREADS>,
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               (int)cfg.dynamicSmemBytes);
+    if (e != cudaSuccess) return e;
+    attr_set[dev] = true;
+  }
+  return cudaLaunchKernelEx(&cfg, token_logprob_kernel<T, THREADS>, p);
+}
+
+template <typename T>
+cudaError_t launch_rows(const LogprobParams &p, int sms, cudaStream_t st) {
+  // Few rows: clusters, until two CTAs of 512 threads per SM are in flight, each
+  // thread with a few vectors.  Many: CTAs of 256 threads, so that the rows on an SM
+  // are at different points of their work.
+  if (p.rows > 2 * sms) return launch_as<T, 256>(p, 1, st);
+  int cl = 1;
+  while (cl < 8 && (long long)p.rows * cl * 2 <= 2 * sms &&
+         (long long)p.vocab >= 4LL * cl * 512 * (16 / (int)sizeof(T)))
+    cl *= 2;
+  return launch_as<T, 512>(p, cl, st);
 }
 
 }  // namespace
 
 cudaError_t launch_token_logprobs(const LogprobParams &p, int sms, cudaStream_t st) {
   switch (p.dtype) {
-    case CC_BF16: return launch_as<__nv_bfloat16>(p, sms, st);
-    case CC_F16: return launch_as<__half>(p, sms, st);
-    case CC_F32: return launch_as<float>(p, sms, st);
+    case CC_BF16: return launch_rows<__nv_bfloat16>(p, sms, st);
+    case CC_F16: return launch_rows<__half>(p, sms, st);
+    case CC_F32: return launch_rows<float>(p, sms, st);
     default: return cudaErrorInvalidValue;
   }
 }
