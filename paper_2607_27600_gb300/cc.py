@@ -216,8 +216,14 @@ def _dev_ptr(t, name):
     return t.data_ptr()
 
 
+# The current stream's handle without building a Stream object, where torch has it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
@@ -625,17 +631,26 @@ def _row_ptr(t, name, n_rows, width, dtype):
         return None, 0
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} is {t.dtype}, not {dtype}")
     shape, stride = t.shape, t.stride()
     inner = 1
-    for i in range(t.dim() - 1, 0, -1):
-        if shape[i] != 1 and stride[i] != inner:
+    for n, st in zip(shape[:0:-1], stride[:0:-1]):
+        if n != 1 and st != inner:
             raise ValueError(f"{name}: the elements of a row must be contiguous")
-        inner *= shape[i]
+        inner *= n
     if shape[0] != n_rows or inner != width:
         raise ValueError(f"{name} has shape {tuple(shape)}; {n_rows} rows of {width} elements expected")
     return t.data_ptr(), (stride[0] if n_rows > 1 else width)
+
+
+def _vec_ptr(t, name, n, dtype):
+    """Pointer of a contiguous CUDA tensor of n elements of dtype, or None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n:
+        raise ValueError(f"{name} must be {dtype} of {n} elements")
+    return _dev_ptr(t, name)
 
 
 def _dtype(t, name):
@@ -670,21 +685,18 @@ def cc_kv_attention(cfg, cache: Cache, layer: int, rows: Rows, q, out, ws, lse=N
     see the slots up to their own, or with memory_only the seq_len slots alone."""
     c, n = _cfg(cfg), rows.c.n_rows
     hq = c.n_q_heads * c.head_dim
-    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != n * c.n_q_heads):
-        raise ValueError("lse must be fp32 [n_rows, Hq]")
     _check(load_library().cc_kv_attention(
         c, cache.c, layer, rows.c, _dtype(q, "q"), 1 if memory_only else 0,
         *_row_ptr(q, "q", n, hq, q.dtype), *_row_ptr(out, "out", n, hq, q.dtype),
-        _dev_ptr(lse, "lse"), _dev_ptr(ws, "ws"), ws.numel() * ws.element_size(),
-        _stream(stream)), "cc_kv_attention")
+        _vec_ptr(lse, "lse", n * c.n_q_heads, torch.float32), _dev_ptr(ws, "ws"),
+        ws.numel() * ws.element_size(), _stream(stream)), "cc_kv_attention")
 
 
 def cc_kv_advance(cache: Cache, rows: Rows, tokens=None, stream=None):
     """Ends a step: positions and tokens (int32 [n_rows] or None) of the rows
     into the cache, and seq_len grows."""
-    if tokens is not None and (tokens.dtype != torch.int32 or tokens.numel() != rows.c.n_rows):
-        raise ValueError(f"tokens must be int32 of {rows.c.n_rows} elements")
-    _check(load_library().cc_kv_advance(cache.c, rows.c, _dev_ptr(tokens, "tokens"),
+    _check(load_library().cc_kv_advance(cache.c, rows.c,
+                                        _vec_ptr(tokens, "tokens", rows.c.n_rows, torch.int32),
                                         _stream(stream)), "cc_kv_advance")
 
 
@@ -694,27 +706,23 @@ def cc_token_logprobs(logits, targets=None, logprob=None, entropy=None, top_ids=
     log-probability of targets (int32 [rows]) into logprob, the entropy, and the
     most likely ids [rows, top] with their log-probabilities.  Outputs are fp32
     but the int32 ids; any may be None."""
-    if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
-        raise TypeError("logits must be a CUDA tensor")
-    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
-        raise ValueError("logits must be [rows, vocab] with contiguous rows")
-    n, vocab = logits.shape
+    if not isinstance(logits, torch.Tensor) or not logits.is_cuda or logits.dim() != 2:
+        raise TypeError("logits must be a CUDA tensor [rows, vocab]")
+    (n, vocab), (ld, inner) = logits.shape, logits.stride()
+    if vocab > 1 and inner != 1:
+        raise ValueError("the logits of a row must be contiguous")
     top = 0
-    for t, name, dtype in ((targets, "targets", torch.int32), (logprob, "logprob", torch.float32),
-                           (entropy, "entropy", torch.float32)):
-        if t is not None and (t.dtype != dtype or t.numel() != n):
-            raise ValueError(f"{name} must be {dtype} of {n} elements")
-    for t, name, dtype in ((top_ids, "top_ids", torch.int32), (top_logprob, "top_logprob", torch.float32)):
-        if t is None:
-            continue
-        if t.dtype != dtype or t.dim() != 2 or t.shape[0] != n or (top and t.shape[1] != top):
-            raise ValueError(f"{name} must be {dtype} [{n}, top]")
-        top = t.shape[1]
+    for t, name in ((top_ids, "top_ids"), (top_logprob, "top_logprob")):
+        if t is not None:
+            if t.dim() != 2 or (top and t.shape[1] != top):
+                raise ValueError(f"{name} must be [{n}, top]")
+            top = t.shape[1]
+    f32, i32 = torch.float32, torch.int32
     _check(load_library().cc_token_logprobs(
-        logits.data_ptr(), _dtype(logits, "logits"), n, vocab, logits.stride(0) if n > 1 else vocab,
-        _dev_ptr(targets, "targets"), _dev_ptr(logprob, "logprob"), _dev_ptr(entropy, "entropy"), top,
-        _dev_ptr(top_ids, "top_ids"), _dev_ptr(top_logprob, "top_logprob"), _stream(stream)),
-        "cc_token_logprobs")
+        logits.data_ptr(), _dtype(logits, "logits"), n, vocab, ld if n > 1 else vocab,
+        _vec_ptr(targets, "targets", n, i32), _vec_ptr(logprob, "logprob", n, f32),
+        _vec_ptr(entropy, "entropy", n, f32), top, _vec_ptr(top_ids, "top_ids", n * top, i32),
+        _vec_ptr(top_logprob, "top_logprob", n * top, f32), _stream(stream)), "cc_token_logprobs")
 
 
 def cc_timing_enable(on: bool):

@@ -465,14 +465,16 @@ cudaError_t launch_as(const LogprobParams &p, int cl, cudaStream_t st) {
 
 template <typename T>
 cudaError_t launch_rows(const LogprobParams &p, int sms, cudaStream_t st) {
-  // Few rows: clusters, until two CTAs of 512 threads per SM are in flight, each
-  // thread with a few vectors.  Many: CTAs of 256 threads, so that the rows on an SM
-  // are at different points of their work.
+  // Few rows: the largest clusters of which all rows' are resident (two CTAs of 512
+  // threads per SM; of 152 SMs, clusters of 8 hold 120 and of 4 hold 144), each thread
+  // with a few vectors.  Many: CTAs of 256 threads, so that the rows on an SM are
+  // at different points of their work.
   if (p.rows > 2 * sms) return launch_as<T, 256>(p, 1, st);
-  int cl = 1;
-  while (cl < 8 && (long long)p.rows * cl * 2 <= 2 * sms &&
-         (long long)p.vocab >= 4LL * cl * 512 * (16 / (int)sizeof(T)))
-    cl *= 2;
+  int cl = 8;
+  const int hold[9] = {0, 2 * sms, sms, 0, 2 * sms * 36 / 152, 0, 0, 0, 2 * sms * 15 / 152};
+  while (cl > 1 && (p.rows > hold[cl] ||
+                    (long long)p.vocab < 2LL * cl * 512 * (16 / (int)sizeof(T))))
+    cl /= 2;
   return launch_as<T, 512>(p, cl, st);
 }
 
