@@ -11,10 +11,10 @@
 // everywhere) is done again from t = (z - m) c.
 //
 // Alternatives without a second pass: each thread keeps its largest logit and
-// where that is.  The top-th largest of the CTA's thread maxima is a lower bound
-// of the top-th largest logit, so only the `top` threads at or above it hold
-// candidates, and their few dozen vectors are read again (from L2).  Keys
-// of (value, lower position first) are all distinct, so ties change nothing.
+// where that is.  The top-th largest maximum of 64 groups of threads is a lower
+// bound of the top-th largest logit, so only the threads that reach it (hardly more
+// than `top`) hold candidates, and their few dozen vectors are read again (from L2).
+// Keys of (value, lower position first) are all distinct, so ties change nothing.
 //
 // Bound by HBM, and close behind by issue slots: 16-bit maxima and fp32 sums in pairs
 // keep it under 6 instructions per logit.  A CTA takes a row; with few rows a
@@ -33,6 +33,8 @@ constexpr float kC = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 // (at the maxima that the sums take, up to 2^20, z c and m c are 0.1 apart at most).
 constexpr float kLow = -0x1p20f;
 constexpr float kFar = -200.f;   // 2^x is 0 in fp32 below
+constexpr int kManyRows = 2;     // per SM, past which a row has 256 threads
+constexpr int kCand = 256;       // candidates of a segment that are sorted at once
 
 CC_DEV float ex2(float x) {
   float y;
@@ -236,7 +238,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
   __shared__ float sums[kWarps][3];
   __shared__ Key part_list[8][32];   // rank 0: the cluster's
   __shared__ float part_sums[8][3];
-  __shared__ int marked[kMaxTop], n_marked;
+  __shared__ Key groups[64], cand[kCand];
+  __shared__ int marked[THREADS], n_marked, n_cand;
   const int cl = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int r = blockIdx.x / cl;
@@ -325,47 +328,65 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
   // ---- the segment's largest `top` as a sorted list in warp 0
   Key list = 0;
   if (p.top > 0) {
-    if (tid == 0) n_marked = 0;
+    if (tid == 0) n_marked = n_cand = 0;
     const Key mine = best_v < 0 ? 0 : make_key(ordered(best), (uint32_t)best_v);
-    lists[warp][lane] = sort_list(mine);
+    // the top-th largest of 64 groups' maxima bounds the top-th largest logit from
+    // below, and hardly more threads than `top` reach it
+    Key group = mine;
+#pragma unroll
+    for (int o = 1; o < THREADS / 64; o <<= 1) {
+      const Key k = __shfl_xor_sync(0xFFFFFFFFu, group, o);
+      group = k > group ? k : group;
+    }
+    if (tid % (THREADS / 64) == 0) groups[tid / (THREADS / 64)] = group;
     __syncthreads();
-    merge_tree(lists, kWarps, warp, lane);
-    const Key least = lists[0][p.top - 1];   // the top-th largest thread maximum
+    const Key least = __shfl_sync(
+        0xFFFFFFFFu, merge_lists(sort_list(groups[lane]), sort_list(groups[32 + lane])), p.top - 1);
     if (mine != 0 && mine >= least) marked[atomicAdd(&n_marked, 1)] = tid;
     __syncthreads();
-    // the marked threads' vectors again, a warp at a time
+    // their vectors again, a warp per thread; `take` gets the elements that reach the bound
+    auto scan = [&](auto &&take) {
 #pragma unroll 1
-    for (int k = warp; k < n_marked; k += kWarps) {
+      for (int k = warp; k < n_marked; k += kWarps) {
 #pragma unroll 1
-      for (int u0 = v0 + marked[k]; u0 < v1; u0 += 32 * THREADS) {
-        const int u = u0 + lane * THREADS;
-        float x[N];
-        row.widen(u < v1 ? load_once(row.at(u)) : make_uint4(0, 0, 0, 0), x);
+        for (int u0 = v0 + marked[k]; u0 < v1; u0 += 32 * THREADS) {
+          const int u = u0 + lane * THREADS;
+          float x[N];
+          row.widen(u < v1 ? load_once(row.at(u)) : make_uint4(0, 0, 0, 0), x);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int e = row.first(u) + i;
-          const uint32_t o = ordered(x[i]);
-          unsigned cand = __ballot_sync(0xFFFFFFFFu, u < v1 && make_key(o, (uint32_t)u) >= least);
-          while (cand) {
-            const int src = __ffs(cand) - 1;
-            cand &= cand - 1;
-            list = insert_key(list, __shfl_sync(0xFFFFFFFFu, make_key(o, (uint32_t)e), src));
+          for (int i = 0; i < N; ++i) {
+            const uint32_t o = ordered(x[i]);
+            take(u < v1 && make_key(o, (uint32_t)u) >= least, make_key(o, (uint32_t)(row.first(u) + i)));
           }
         }
       }
-    }
-    for (unsigned cand = __ballot_sync(0xFFFFFFFFu, edge >= 0); cand; cand &= cand - 1) {
-      const Key k = edge >= 0 ? make_key(ordered(to_float(row_ptr[edge])), (uint32_t)edge) : 0;
-      list = insert_key(list, __shfl_sync(0xFFFFFFFFu, k, __ffs(cand) - 1));
-    }
-    __syncthreads();   // every thread has read `least`
-    lists[warp][lane] = list;
+      if (warp == 0)
+        take(edge >= 0, edge >= 0 ? make_key(ordered(to_float(row_ptr[edge])), (uint32_t)edge) : 0);
+    };
+    scan([&](bool in, Key k) {
+      if (!in) return;
+      const int at = atomicAdd(&n_cand, 1);
+      if (at < kCand) cand[at] = k;
+    });
     __syncthreads();
-    merge_tree(lists, min(kWarps, max(n_marked, 1)), warp, lane);
-    list = lists[0][lane];
-  } else {
-    __syncthreads();
+    if (n_cand <= kCand) {
+      if (warp == 0)
+        for (int c = 0; c < n_cand; c += 32) {
+          const Key k = sort_list(c + lane < n_cand ? cand[c + lane] : 0);
+          list = c ? merge_lists(list, k) : k;
+        }
+    } else {   // many equal logits at the bound: each warp's largest, then all warps'
+      scan([&](bool in, Key k) {
+        for (unsigned some = __ballot_sync(0xFFFFFFFFu, in); some; some &= some - 1)
+          list = insert_key(list, __shfl_sync(0xFFFFFFFFu, k, __ffs(some) - 1));
+      });
+      lists[warp][lane] = list;
+      __syncthreads();
+      merge_tree(lists, kWarps, warp, lane);
+      list = lists[0][lane];
+    }
   }
+  __syncthreads();
   if (warp == 0) {
     a = lane < kWarps ? Sums{sums[lane][0], sums[lane][1], sums[lane][2]} : Sums{kLow, 0.f, 0.f};
     a = warp_join(a);
@@ -465,13 +486,14 @@ cudaError_t launch_as(const LogprobParams &p, int cl, cudaStream_t st) {
 
 template <typename T>
 cudaError_t launch_rows(const LogprobParams &p, int sms, cudaStream_t st) {
-  // Few rows: the largest clusters of which all rows' are resident (two CTAs of 512
-  // threads per SM; of 152 SMs, clusters of 8 hold 120 and of 4 hold 144), each thread
-  // with a few vectors.  Many: CTAs of 256 threads, so that the rows on an SM are
-  // at different points of their work.
-  if (p.rows > 2 * sms) return launch_as<T, 256>(p, 1, st);
+  // Few rows: the largest clusters of which all rows' are resident at one CTA of 512
+  // threads per SM (152 SMs hold 15 clusters of 8, 36 of 4 and 76 of 2), each thread
+  // with a few vectors: 64 rows of 152064 bf16 logits in pairs 10.4 us, in fours 12.8.
+  // Many: CTAs of 256 threads, so that the rows on an SM are at different points of
+  // their work.
+  if (p.rows > kManyRows * sms) return launch_as<T, 256>(p, 1, st);
   int cl = 8;
-  const int hold[9] = {0, 2 * sms, sms, 0, 2 * sms * 36 / 152, 0, 0, 0, 2 * sms * 15 / 152};
+  const int hold[9] = {0, 0, sms / 2, 0, sms * 36 / 152, 0, 0, 0, sms * 15 / 152};
   while (cl > 1 && (p.rows > hold[cl] ||
                     (long long)p.vocab < 2LL * cl * 512 * (16 / (int)sizeof(T))))
     cl /= 2;
