@@ -3,47 +3,61 @@
 // step.
 //
 // A unit of work is a block of `block` cache slots of one sequence that new
-// rows fall into (block format: the slots that share a scale).  A CTA takes one
-// unit, or with few units a share of its heads: it tabulates cos and sin of its
-// rows' angles once for all heads; then a warp takes one KV head's keys or
-// values of the unit, and teams of head_dim / 16 lanes take one query head of
-// one row.  A lane holds 8 elements and the 8 that they rotate with.
+// rows fall into (block format: the slots that share a scale), a CTA's is a unit
+// and a share of the heads.  Block format: first a warp per KV head bounds the
+// magnitudes of the unit's keys or values and settles the scale.  For keys it
+// bounds the radius of each rotated pair, sqrt(a^2 + b^2) <= max + min / 2, so that
+// the scale needs no angle and is the same bits however cos and sin are rounded;
+// it is at most 1.12 times the largest magnitude that any rotation gives.  Then
+// teams of head_dim / 16 lanes take a row each, or where there are few rows some of
+// its heads: a lane holds 8 elements of a head and the 8 that they rotate with, and
+// cos and sin of its angles stay in registers from head to head.
 //
-// Block format: a KV head's warp reads its rows twice, first for the bound of
-// their magnitudes.  For keys it bounds the radius of each rotated pair,
-// sqrt(a^2 + b^2) <= max + min / 2, so that the scale needs no angle and is the
-// same bits however cos and sin are rounded; it is at most 1.12 times the
-// largest magnitude that any rotation gives.  The second read hits L1.
+// Bound by HBM; keys and values are read twice, the second time from L2.  A lane
+// copies what it will read a few heads (rows, for the bound) ahead into slots of its
+// own (cp.async, no barrier): loops unrolled over loads instead held as much in
+// flight but half of the time nothing, and their code was a single token's latency.
 #include "kvappend.cuh"
 
 #include <algorithm>
+#include <atomic>
+#include <type_traits>
 
 namespace cc {
 
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kSplitCtas = 2;   // CTAs per SM to split the heads for
 constexpr int kLeastExp = 10, kMostExp = 247, kUnitExp = 127;   // scale exponents written
 
+// 8 elements as they lie in memory.
 template <typename T>
-CC_DEV void load8(const T *src, float (&x)[8]) {
-  if constexpr (sizeof(T) == 4) {
-    const float4 a = reinterpret_cast<const float4 *>(src)[0], b = reinterpret_cast<const float4 *>(src)[1];
-    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-  } else {
-    const uint4 u = *reinterpret_cast<const uint4 *>(src);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+struct Raw8 {
+  uint4 w[sizeof(T) / 2];
+  CC_DEV void load(const T *src) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (std::is_same_v<T, __half>) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
-        x[2 * i] = f.x, x[2 * i + 1] = f.y;
-      } else {
-        x[2 * i] = bf16_lo(w[i]), x[2 * i + 1] = bf16_hi(w[i]);
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const uint4 *>(src)[i];
+  }
+  CC_DEV void widen(float (&x)[8]) const {
+    const uint32_t u[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+    if constexpr (sizeof(T) == 4) {
+      const uint32_t v[4] = {w[1].x, w[1].y, w[1].z, w[1].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(u[i]), x[4 + i] = __uint_as_float(v[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (std::is_same_v<T, __half>) {
+          const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&u[i]));
+          x[2 * i] = f.x, x[2 * i + 1] = f.y;
+        } else {
+          x[2 * i] = bf16_lo(u[i]), x[2 * i + 1] = bf16_hi(u[i]);
+        }
       }
     }
   }
-}
+};
 template <typename T>
 CC_DEV void store8(T *dst, const float (&x)[8]) {
   if constexpr (sizeof(T) == 4) {
@@ -78,22 +92,81 @@ CC_DEV int scale_exp(float bound) {
 }
 CC_DEV float pow2_biased(int e) { return e > 0 ? __uint_as_float((uint32_t)e << 23) : 0.f; }
 
-// (a, b) of 8 rotated pairs with their (cos, sin)
-CC_DEV void rotate8(float (&a)[8], float (&b)[8], const float2 *cs) {
+// 8 pairs: cos, sin, and minus sin, two to a register pair.
+struct Turn {
+  float2 c[4], s[4], n[4];
+};
+CC_DEV void rotate8(float (&a)[8], float (&b)[8], const Turn &t) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float2 t = cs[i];
-    const float x = a[i], y = b[i];
-    a[i] = x * t.x - y * t.y;
-    b[i] = y * t.x + x * t.y;
+  for (int i = 0; i < 4; ++i) {
+    const float2 x = make_float2(a[2 * i], a[2 * i + 1]), y = make_float2(b[2 * i], b[2 * i + 1]);
+    const float2 u = __ffma2_rn(y, t.n[i], __fmul2_rn(x, t.c[i]));
+    const float2 v = __ffma2_rn(x, t.s[i], __fmul2_rn(y, t.c[i]));
+    a[2 * i] = u.x, a[2 * i + 1] = u.y;
+    b[2 * i] = v.x, b[2 * i + 1] = v.y;
   }
 }
 
+// cos and sin of a fraction of a turn: those of the nearest 256th from a table,
+// turned by what is left (|d| <= pi / 256: the Taylor series to d^4 and d^3 are good to
+// 2^-40 and 2^-38), an eighth of the instructions of sincospif.
+constexpr int kTable = 256;
+CC_DEV void table_entry(float2 *table, int i) {
+  float sn, cs;
+  sincospif((float)i * (2.f / kTable), &sn, &cs);
+  table[i] = make_float2(cs, sn);
+}
+CC_DEV void turn_cs(const float2 *table, uint32_t frac, float &c, float &s) {   // frac / 2^32 of a turn
+  const uint32_t at = frac + (1u << 23);   // to the nearest entry
+  const float2 t = table[at >> 24];
+  const float d = (float)((int)(at & 0xFFFFFFu) - (1 << 23)) * 1.4629180792671596e-09f;   // 2 pi / 2^32
+  const float d2 = d * d;
+  const float cd = fmaf(d2, fmaf(d2, 1.f / 24.f, -0.5f), 1.f), sd = fmaf(d * d2, -1.f / 6.f, d);
+  c = fmaf(t.x, cd, -t.y * sd);
+  s = fmaf(t.y, cd, t.x * sd);
+}
+
+// A lane's items ahead: 8 + 8 elements each.
+template <typename T>
+struct Ahead {
+  static constexpr int PIECES = sizeof(T) / 2;              // 16-byte pieces of 8 elements
+  static constexpr int SLOTS = 256 / (2 * PIECES * 16);     // 256 bytes a lane
+  static constexpr int BYTES = kThreads * 256;
+  uint8_t *mem;   // of the lane
+  CC_DEV void issue(int slot, const T *a, const T *c) {
+    const uint32_t to = smem_u32(mem) + slot * (2 * PIECES * 16 * kThreads);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      copy16(to + i * 16 * kThreads, reinterpret_cast<const uint4 *>(a) + i);
+      copy16(to + (PIECES + i) * 16 * kThreads, reinterpret_cast<const uint4 *>(c) + i);
+    }
+  }
+  CC_DEV void get(int slot, float (&a)[8], float (&c)[8]) const {
+    const uint4 *from = reinterpret_cast<const uint4 *>(mem + slot * (2 * PIECES * 16 * kThreads));
+    Raw8<T> ra, rc;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      ra.w[i] = from[i * kThreads];
+      rc.w[i] = from[(PIECES + i) * kThreads];
+    }
+    ra.widen(a);
+    rc.widen(c);
+  }
+  CC_DEV static void copy16(uint32_t dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  }
+  CC_DEV static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+  CC_DEV static void wait_oldest() {   // of SLOTS - 1 in flight before the last one was issued
+    asm volatile("cp.async.wait_group %0;" ::"n"(SLOTS - 1) : "memory");
+  }
+};
+
 template <typename T, int DH>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 3)
     kv_append_kernel(const __grid_constant__ KvAppendParams p) {
   constexpr int HALF = DH / 2, TPR = DH / 16, RPI = 32 / TPR;   // lanes per row, rows per warp
-  extern __shared__ float2 trig[];   // [rows of the unit][HALF]
+  constexpr int TEAMS = kThreads / TPR, SLOTS = Ahead<T>::SLOTS;
+  extern __shared__ __align__(16) uint8_t smem[];
   const int B = p.block, per_seq = (p.rows.max_rows + B - 2) / B + 1;
   const int b = blockIdx.x / per_seq;
   const SeqRows s = seq_rows(p.rows, b, true);
@@ -109,70 +182,67 @@ __global__ void __launch_bounds__(kThreads)
   const int n = min(base + B, s.seq + s.count) - (base + old);
   if (n <= 0) return;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int at8 = (lane % TPR) * 8;
+  Ahead<T> ahead{smem + tid * 16};
+  float2 *table = reinterpret_cast<float2 *>(smem + Ahead<T>::BYTES);
+  float *scale = reinterpret_cast<float *>(table + kTable);   // 1 / scale: K heads, V heads
+  // this CTA's heads
+  const int ny = gridDim.y, y = blockIdx.y;
+  const int k0 = p.hkv * y / ny, nk = p.hkv * (y + 1) / ny - k0;
+  const int q0 = p.hq * y / ny, nq = p.q ? p.hq * (y + 1) / ny - q0 : 0;
+  const bool by_block = p.format == CC_KV_E4M3_BLOCK;
+  // the unit lies in one page: vector of KV head g and slot base + i
+  const long long row0 = p.pg.head_major ? 0 : kv_row(p.pg, p.rows.cap, b, base);
+  const int vstep = p.pg.head_major ? 1 : p.hkv;
+  auto vec_at = [&](int g) {
+    return p.pg.head_major ? ((long long)b * p.hkv + g) * p.rows.cap + base : row0 * p.hkv + g;
+  };
+  if (row0 < 0 && tid == 0) set_status(p.status, CC_ERR_DEVICE_ARG);
 
-  if (p.rotate) {
-    const int follow = p.pos || s.seq == 0
-                           ? 0 : p.cache_pos[(size_t)b * p.rows.cap + s.seq - 1] + 1;
-    for (int i = tid; i < n * HALF; i += kThreads) {
-      const int r = i / HALF, k = i - r * HALF;
-      int at = p.pos ? p.pos[r0 + r] : follow + (base + old - s.seq) + r;
-      if (at < 0) {
-        if (k == 0) set_status(p.status, CC_ERR_DEVICE_ARG);
-        at = 0;
-      }
-      // pos * turns mod 2^64 is a fraction of a turn; its top 32 bits as a
-      // signed fraction times 2 are the angle in units of pi
-      const int32_t frac = (int32_t)(((unsigned long long)at * p.turns[k]) >> 32);
-      float sn, cs;
-      sincospif((float)frac * 0x1p-31f, &sn, &cs);
-      trig[i] = make_float2(cs, sn);
-    }
-    __syncthreads();
-  }
-
-  const int stride = gridDim.y * (kThreads / 32);
-  const int team = lane / TPR, at8 = (lane % TPR) * 8;
-  for (int job = blockIdx.y * (kThreads / 32) + warp; job < 2 * p.hkv; job += stride) {
-    const bool is_k = job < p.hkv;
-    const int g = is_k ? job : job - p.hkv;
-    const long long vec0 = kv_vec(p.pg, p.rows.cap, b, g, base);
-    if (vec0 < 0) {
-      if (lane == 0) set_status(p.status, CC_ERR_DEVICE_ARG);
-      continue;
-    }
-    const int vstep = p.pg.head_major ? 1 : p.hkv;
-    const long long ld = is_k ? p.k_ld : p.v_ld;
-    const T *src = reinterpret_cast<const T *>(is_k ? p.k : p.v) + r0 * ld + g * DH + at8;
-    const bool turn = is_k && p.rotate;
-    float inv = is_k ? p.k_qscale : p.v_qscale;
-    const bool by_block = p.format == CC_KV_E4M3_BLOCK;
-    uint8_t *codes = reinterpret_cast<uint8_t *>(is_k ? p.kc : p.vc);
-    if (by_block) {
-      // a block lies in one page: its scale is the one of its first slot
-      const long long ei = p.pg.head_major ? vec0 / B : (vec0 / p.hkv) / B * p.hkv + g;
+  if (p.rotate) table_entry(table, tid);
+  static_assert(kTable == kThreads, "a thread an entry");
+  if (by_block && row0 >= 0) {
+    const int team = lane / TPR;
+    for (int job = warp; job < 2 * nk; job += kThreads / 32) {
+      const bool is_k = job < nk;
+      const int g = k0 + (is_k ? job : job - nk);
+      const long long vec0 = vec_at(g), ld = is_k ? p.k_ld : p.v_ld;
+      const T *src = reinterpret_cast<const T *>(is_k ? p.k : p.v) + r0 * ld + g * DH + at8;
+      const long long ei = p.pg.head_major ? vec0 / B : row0 / B * p.hkv + g;
       uint8_t *ep = (is_k ? p.ke : p.ve) + ei;
       const int e_old = old ? *ep : 0;
+      auto issue = [&](int r, int slot) {
+        if (r < n) ahead.issue(slot, src + r * ld, src + r * ld + HALF);
+        ahead.commit();
+      };
+#pragma unroll 1
+      for (int i = 0; i < SLOTS - 1; ++i) issue(team + i * RPI, i);
       float bound = 0.f;
-#pragma unroll 2
+      int slot = 0;
+#pragma unroll 1
       for (int r = team; r < n; r += RPI) {
+        issue(r + (SLOTS - 1) * RPI, slot == 0 ? SLOTS - 1 : slot - 1);
+        ahead.wait_oldest();
         float a[8], c[8];
-        load8(src + r * ld, a);
-        load8(src + r * ld + HALF, c);
+        ahead.get(slot, a, c);
+        slot = slot + 1 == SLOTS ? 0 : slot + 1;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float x = finite_abs(a[i]), y = finite_abs(c[i]);
-          const float hi = fmaxf(x, y);
-          bound = fmaxf(bound, is_k ? __fadd_rn(hi, 0.5f * fminf(x, y)) : hi);
+          const float u = finite_abs(a[i]), w = finite_abs(c[i]);
+          const float hi = fmaxf(u, w);
+          bound = fmaxf(bound, is_k ? __fadd_rn(hi, 0.5f * fminf(u, w)) : hi);
         }
       }
       int e = max(scale_exp(warp_max(bound)), e_old);
       if (e == 0) e = kUnitExp;   // zeros alone
-      if (old && e > e_old) {
+      if (old && e > e_old) {     // the older codes by a power of two
         const float f = pow2_biased(127 + e_old - e);
+        uint8_t *codes = reinterpret_cast<uint8_t *>(is_k ? p.kc : p.vc);
+#pragma unroll 1
         for (int r = team; r < old; r += RPI) {
-          uint8_t *at = codes + (vec0 + (long long)r * vstep) * DH + at8 * 2;
-          uint4 u = *reinterpret_cast<const uint4 *>(at);
-          uint32_t *w = &u.x;
+          uint4 *at = reinterpret_cast<uint4 *>(codes + (vec0 + (long long)r * vstep) * DH + at8 * 2);
+          const uint4 u = *at;
+          uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             uint32_t r2[2];
@@ -185,48 +255,107 @@ __global__ void __launch_bounds__(kThreads)
             }
             w[i] = r2[0] | (r2[1] << 16);
           }
-          *reinterpret_cast<uint4 *>(at) = u;
+          *at = make_uint4(w[0], w[1], w[2], w[3]);
         }
       }
-      if (lane == 0) *ep = (uint8_t)e;
-      inv = pow2_biased(254 - e);
-    }
-#pragma unroll 2
-    for (int r = team; r < n; r += RPI) {
-      float a[8], c[8];
-      load8(src + r * ld, a);
-      load8(src + r * ld + HALF, c);
-      if (turn) rotate8(a, c, trig + r * HALF + at8);
-      const long long el = (vec0 + (long long)(old + r) * vstep) * DH + at8;
-      if (p.format == CC_KV_BF16) {
-        __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(codes) + el;
-        store8(dst, a);
-        store8(dst + HALF, c);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          // one scale a layer saturates infinities, as the appends do
-          a[i] = by_block && fabsf(a[i]) == INFINITY ? NAN : a[i] * inv;
-          c[i] = by_block && fabsf(c[i]) == INFINITY ? NAN : c[i] * inv;
-        }
-        store_codes8(codes + el, a);
-        store_codes8(codes + el + HALF, c);
+      if (lane == 0) {
+        *ep = (uint8_t)e;
+        scale[job] = pow2_biased(254 - e);
       }
     }
   }
-  if (!p.q) return;
-  const int teams = gridDim.y * (kThreads / TPR);
-#pragma unroll 2
-  for (int i = blockIdx.y * (kThreads / TPR) + tid / TPR; i < n * p.hq; i += teams) {
-    const int r = i / p.hq, h = i - r * p.hq;
-    const T *src = reinterpret_cast<const T *>(p.q) + (r0 + r) * p.q_ld + h * DH + at8;
-    T *dst = reinterpret_cast<T *>(p.q_out) + (r0 + r) * p.q_out_ld + h * DH + at8;
-    float a[8], c[8];
-    load8(src, a);
-    load8(src + HALF, c);
-    if (p.rotate) rotate8(a, c, trig + r * HALF + at8);
-    store8(dst, a);
-    store8(dst + HALF, c);
+  __syncthreads();
+
+  // ---- rows by heads: rt rows at a time, TEAMS / rt teams to a row, each taking
+  // every ht-th of the row's K, V and Q heads
+  int rt = 1;
+  while (rt < TEAMS && rt < n) rt *= 2;
+  const int team = tid / TPR, ht = TEAMS / rt, h0 = team / rt, heads = 2 * nk + nq;
+  if (h0 >= heads || team % rt >= n) return;
+  const int follow = !p.rotate || p.pos || s.seq == 0
+                         ? 0 : p.cache_pos[(size_t)b * p.rows.cap + s.seq - 1] + 1;
+  auto position = [&](int r) {
+    return !p.rotate ? 0 : p.pos ? (r < n ? p.pos[r0 + r] : 0) : follow + (base + old - s.seq) + r;
+  };
+  int ri = team % rt, hi = h0;   // the next item to copy, and its row's K, V and Q
+  const T *ki, *vi, *qi;
+  auto enter = [&]() {
+    const long long r = r0 + ri;
+    ki = reinterpret_cast<const T *>(p.k) + r * p.k_ld + k0 * DH + at8;
+    vi = reinterpret_cast<const T *>(p.v) + r * p.v_ld + (k0 - nk) * DH + at8;
+    qi = reinterpret_cast<const T *>(p.q) + r * p.q_ld + (q0 - 2 * nk) * DH + at8;
+  };
+  enter();
+  auto issue = [&](int slot) {
+    if (ri < n) {
+      const T *src = (hi < nk ? ki : hi < 2 * nk ? vi : qi) + hi * DH;
+      ahead.issue(slot, src, src + HALF);
+      hi += ht;
+      if (hi >= heads) {
+        hi = h0;
+        ri += rt;
+        enter();
+      }
+    }
+    ahead.commit();
+  };
+#pragma unroll 1
+  for (int i = 0; i < SLOTS - 1; ++i) issue(i);
+  int slot = 0, next_pos = position(team % rt);
+#pragma unroll 1
+  for (int r = team % rt; r < n; r += rt) {
+    Turn t;
+    if (p.rotate) {
+      int at = next_pos;
+      next_pos = position(r + rt);
+      if (at < 0) {
+        set_status(p.status, CC_ERR_DEVICE_ARG);
+        at = 0;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        // pos * turns mod 2^64 is a fraction of a turn
+        float sn, cs;
+        turn_cs(table, (uint32_t)(((unsigned long long)at * p.turns[at8 + i]) >> 32), cs, sn);
+        (i & 1 ? t.c[i / 2].y : t.c[i / 2].x) = cs;
+        (i & 1 ? t.s[i / 2].y : t.s[i / 2].x) = sn;
+        (i & 1 ? t.n[i / 2].y : t.n[i / 2].x) = -sn;
+      }
+    }
+#pragma unroll 1
+    for (int h = h0; h < heads; h += ht) {
+      issue(slot == 0 ? SLOTS - 1 : slot - 1);
+      ahead.wait_oldest();
+      float a[8], c[8];
+      ahead.get(slot, a, c);
+      slot = slot + 1 == SLOTS ? 0 : slot + 1;
+      const bool is_k = h < nk, is_q = h >= 2 * nk;
+      if (p.rotate && (is_k || is_q)) rotate8(a, c, t);
+      if (is_q) {
+        T *out = reinterpret_cast<T *>(p.q_out) + (r0 + r) * p.q_out_ld + (q0 + h - 2 * nk) * DH + at8;
+        store8(out, a);
+        store8(out + HALF, c);
+        continue;
+      }
+      if (row0 < 0) continue;
+      const long long el = (vec_at(k0 + (is_k ? h : h - nk)) + (long long)(old + r) * vstep) * DH + at8;
+      void *buf = is_k ? p.kc : p.vc;
+      if (p.format == CC_KV_BF16) {
+        store8(reinterpret_cast<__nv_bfloat16 *>(buf) + el, a);
+        store8(reinterpret_cast<__nv_bfloat16 *>(buf) + el + HALF, c);
+        continue;
+      }
+      const float inv = by_block ? scale[h] : is_k ? p.k_qscale : p.v_qscale;
+      if (by_block) {   // 0 times an infinity: NaN (one scale a layer saturates it, as the appends do)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = fmaf(a[i], 0.f, a[i] * inv), c[i] = fmaf(c[i], 0.f, c[i] * inv);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] *= inv, c[i] *= inv;
+      }
+      store_codes8(reinterpret_cast<uint8_t *>(buf) + el, a);
+      store_codes8(reinterpret_cast<uint8_t *>(buf) + el + HALF, c);
+    }
   }
 }
 
@@ -254,15 +383,19 @@ cudaError_t launch_append_as(const KvAppendParams &p, int sms, cudaStream_t st) 
   const int per_seq = (p.rows.max_rows + p.block - 2) / p.block + 1;
   const long long units = (long long)p.rows.batch * per_seq;
   if (units > 0x7FFFFFFFll) return cudaErrorInvalidValue;
-  const size_t smem = p.rotate ? (size_t)std::min(p.block, p.rows.max_rows) * (DH / 2) * sizeof(float2) : 0;
   auto kern = kv_append_kernel<T, DH>;
-  if (smem > 48 * 1024) {   // (a block of 128 rows of 128: 64 KB)
+  // a unit's heads over several CTAs until they fill the SMs
+  const long long busy = std::min(units, (long long)p.rows.n_rows / p.block + p.rows.batch);   // (about)
+  const int split = (int)std::min<long long>(p.hkv, std::max<long long>(1, (kSplitCtas * sms + busy - 1) / busy));
+  const size_t smem = Ahead<T>::BYTES + kTable * sizeof(float2) + 2 * ((size_t)p.hkv / split + 1) * sizeof(float);
+  static std::atomic<size_t> allowed[64] = {};   // (the few floats grow with hkv)
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (dev >= 64 || allowed[dev] < smem) {
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
+    if (dev < 64) allowed[dev] = smem;
   }
-  // a unit's heads over several CTAs until they fill the SMs
-  const int most = std::max(1, (2 * p.hkv + p.hq) / 8);
-  const int split = (int)std::min<long long>(most, std::max<long long>(1, 6LL * sms / units));
   kern<<<dim3((unsigned)units, (unsigned)split), kThreads, smem, st>>>(p);
   return cudaGetLastError();
 }
