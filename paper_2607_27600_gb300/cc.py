@@ -634,6 +634,9 @@ def _row_ptr(t, name, n_rows, width, dtype):
     if t.dtype is not dtype:
         raise ValueError(f"{name} is {t.dtype}, not {dtype}")
     shape, stride = t.shape, t.stride()
+    if len(shape) == 3 and stride[2] == 1 and stride[1] == shape[2] and shape[0] == n_rows \
+            and shape[1] * shape[2] == width:   # the usual form
+        return t.data_ptr(), (stride[0] if n_rows > 1 else width)
     inner = 1
     for n, st in zip(shape[:0:-1], stride[:0:-1]):
         if n != 1 and st != inner:

@@ -1849,9 +1849,20 @@ bool step_on_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *
 // queries as pairs, and the partial rows of key splits.
 struct StepTileWs {
   size_t k, v, lo, hi, base, pairs, part_o, part_ml, total;
+  long long units;   // of the launch; most have no rows where sequences differ
+  int splits;        // key splits of a unit
 };
-StepTileWs step_tile_layout(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows) {
+StepTileWs step_tile_layout(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows, int sms) {
   StepTileWs w{};
+  // Units with rows, at most: whole ones of n_rows and a part-filled one per
+  // sequence.  Splits until they fill the SMs, of four key tiles at least, while the
+  // partial rows of all units stay below 1024.
+  const int P = attn_positions_per_unit(c->n_q_heads / c->n_kv_heads);
+  w.units = (long long)kv->batch * c->n_kv_heads * ((rows->max_rows + P - 1) / P);
+  const long long busy = std::min(w.units, (long long)c->n_kv_heads * (rows->n_rows / P + kv->batch));
+  const long long tiles = ((long long)kv->cap + 127) / 128;
+  w.splits = (int)std::max(1LL, std::min({sms / std::max(1LL, busy), tiles / kAttnMinSplitTiles,
+                                          1024 / std::max(1LL, w.units)}));
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = align256(off + bytes); return o; };
   const size_t copy = (size_t)kv->batch * kv->cap * c->n_kv_heads * c->head_dim * 2;
@@ -1861,8 +1872,10 @@ StepTileWs step_tile_layout(const cc_model_cfg *c, const cc_kv_cache *kv, const 
   w.hi = take((size_t)kv->batch * 4);
   w.base = take((size_t)kv->batch * 4);
   w.pairs = take((size_t)rows->n_rows * c->n_q_heads * c->head_dim * 4);
-  w.part_o = take((size_t)kAttnMaxSplitSlots * 256 * c->head_dim * 4);
-  w.part_ml = take((size_t)kAttnMaxSplitSlots * 256 * 8);
+  if (w.splits > 1) {
+    w.part_o = take((size_t)w.units * w.splits * 256 * c->head_dim * 4);
+    w.part_ml = take((size_t)w.units * w.splits * 256 * 8);
+  }
   w.total = off;
   return w;
 }
@@ -1871,7 +1884,7 @@ StepTileWs step_tile_layout(const cc_model_cfg *c, const cc_kv_cache *kv, const 
 // the layer; fp16 rows as bf16 pairs, P as pairs too (twice the products).
 cc_status run_step_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows,
                          const KvAttnParams &kp, void *ws, int sms, cudaStream_t st) {
-  const StepTileWs L = step_tile_layout(c, kv, rows);
+  const StepTileWs L = step_tile_layout(c, kv, rows, std::min(sms, kStepMaxSms));
   uint8_t *w = reinterpret_cast<uint8_t *>(ws);
   auto ints = [&](size_t o) { return reinterpret_cast<int32_t *>(w + o); };
   const KvTileRows tr{ints(L.lo), ints(L.hi), ints(L.base)};
@@ -1919,7 +1932,7 @@ cc_status run_step_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_
   p.key_end = kp.memory_only ? tr.lo : nullptr;
   p.lse = kp.lse;
   p.q_span = rows->max_rows;
-  p.kv_splits = attn_key_splits(attn_units(p), kv->cap, sms);
+  p.kv_splits = L.splits;
   p.part_o = reinterpret_cast<float *>(w + L.part_o);
   p.part_ml = reinterpret_cast<float2 *>(w + L.part_ml);
   CC_TRY(launch_attention(tq, tk, tv, p, st));
@@ -1991,7 +2004,7 @@ cc_status cc_kv_append(const cc_model_cfg *cfg, const cc_kv_cache *kv, int32_t l
 size_t cc_kv_attention_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *kv,
                                       const cc_rows *rows) {
   if (check_cfg(cfg) != CC_OK || check_step(kv, rows) != CC_OK || rows->n_rows == 0) return 0;
-  if (step_on_tiles(cfg, kv, rows)) return step_tile_layout(cfg, kv, rows).total;
+  if (step_on_tiles(cfg, kv, rows)) return step_tile_layout(cfg, kv, rows, kStepMaxSms).total;
   return align256(kv_attn_part_bytes(kv_attn_params(cfg, kv, rows, kStepMaxSms)));
 }
 

@@ -656,9 +656,11 @@ __global__ void __launch_bounds__(kCombineWarps * 32)
     float2 ml[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const size_t row = base + (size_t)min(s0 + k, S - 1) * 256;
+      ml[k] = make_float2(-INFINITY, 0.f);
+      v[k] = Vec{};
+      if (s0 + k >= S) continue;
+      const size_t row = base + (size_t)(s0 + k) * 256;
       ml[k] = p.part_ml[row];
-      if (s0 + k >= S) ml[k] = make_float2(-INFINITY, 0.f);
       v[k] = *reinterpret_cast<const Vec *>(p.part_o + row * DH + lane * DPL);
     }
     float mx = m;   // reference max over the splits that saw keys

@@ -38,7 +38,8 @@ namespace {
 
 constexpr int kWarps = 4;          // of a CTA, each every fourth 16 keys of a tile
 constexpr int kTile = 16 * kWarps; // keys of a tile
-constexpr int kMinTiles = 2;       // of a share at least
+constexpr int kMinTiles = 4;       // of a share at least
+constexpr int kGroups = 8, kJoin = 8;   // of the join
 // What a unit costs besides its tiles (its queries, the first loads' latency, its
 // rows at the end: 5 to 6 us where a tile takes 1), in tiles.
 constexpr int kUnitTiles = 5;
@@ -232,9 +233,9 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
   const long long total = total_tiles<NT>(p);
   const int n_shares = min(p.shares, line_shares(p.resident, total)), cta = blockIdx.x;
   const int share = cta / p.hkv, g = cta - share * p.hkv;
-  int4 cut = make_int4(0, 0, 0, -1);   // the unit that starts here and goes on in the next share
+  int4 cut = make_int4(0, -1, 0, 0);   // the unit that starts here and goes on in the next share
   if (share >= n_shares) {
-    if (tid == 0) p.cut[cta] = cut;
+    if (tid == 0 && !p.spread) p.cut[cta] = cut;
     return;
   }
   long long at = total * share / n_shares;
@@ -600,8 +601,10 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
       }
     __syncthreads();
     const bool whole = tile0 == 0 && tile1 == sq.tiles;
-    if (tile0 == 0 && !whole)
-      cut = make_int4(b, g, grp, share_of_tile(unit_at + span - 1, total, n_shares));
+    if (tile0 == 0 && (!whole || p.spread)) {
+      cut = make_int4(share, share_of_tile(unit_at + span - 1, total, n_shares), b, grp);
+      if (p.spread && tid == 0) p.cut[((long long)b * p.most_groups + grp) * p.hkv + g] = cut;
+    }
     // a unit in several shares: what this one has of it, after (0) or from (1) its start
     const long long part = (2ll * cta + (first && tile0 > 0 ? 0 : 1)) * L::ROWS;
     if (tid < L::ROWS) {   // per row: the warps' weights, and where it goes
@@ -657,60 +660,71 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
     __syncthreads();   // the rows are read: the ring may be refilled
     first = false;
   }
-  if (tid == 0) p.cut[cta] = cut;
+  if (tid == 0 && !p.spread) p.cut[cta] = cut;
 }
 
-// Joins the shares of a unit, one row of it per CTA, in share order: kGroups
-// groups of DH / 2 threads take every kGroups-th share.  CTA (c, row) joins the
-// unit that starts in share c and goes on past it, as that share's CTA wrote it
-// down.
-constexpr int kGroups = 4;
-
-template <typename T, int DH, int NT>
+// Joins the shares of a unit that starts in share c0 and goes on past it, as that
+// share's CTA wrote it down, in share order.  SPREAD (few units, of many shares): a CTA
+// per unit and row, its kGroups groups of DH / 2 threads each take every kGroups-th
+// share; else CTAs per share, a group per row.  A group loads eight shares at a time.
+template <typename T, int DH, int NT, bool SPREAD>
 __global__ void __launch_bounds__(kGroups * DH / 2)
     kv_combine_kernel(const __grid_constant__ KvAttnParams p) {
   constexpr int ROWS = 8 * NT;
-  __shared__ float2 part[kGroups][DH / 2];
+  __shared__ float4 part[SPREAD ? kGroups : 1][DH / 2];   // m, mv and the two sums
   __shared__ float part_l[kGroups];
+  const int group = threadIdx.x / (DH / 2), d = (threadIdx.x - group * (DH / 2)) * 2;
+  const int R = SPREAD ? blockIdx.y : blockIdx.y * kGroups + group;
+  const int unit = blockIdx.x / p.hkv, g = blockIdx.x - unit * p.hkv;
   pdl_trigger();
   pdl_wait();
-  const int c0 = blockIdx.x / p.hkv, R = blockIdx.y;
-  const int4 u = p.cut[blockIdx.x];   // sequence, KV head, group of rows, last share (none: no unit)
-  if (u.w <= c0) return;
-  const RowAt r = row_at(p, seq_rows(p.rows, u.x, !p.memory_only), u.y, u.z * ROWS + R);
+  // (SPREAD: a unit without rows was not written down)
+  const int b = SPREAD ? unit / p.most_groups : 0, grp = unit - b * p.most_groups;
+  RowAt r{0, 0, false};
+  if (SPREAD && R < ROWS) r = row_at(p, seq_rows(p.rows, b, !p.memory_only), g, grp * ROWS + R);
+  if (SPREAD && !r.live) return;
+  const int4 u = p.cut[blockIdx.x];   // first and last share; sequence and group of rows
+  const int c0 = u.x, c1 = u.y;
+  if (c1 <= c0 || R >= ROWS) return;
+  if (!SPREAD) r = row_at(p, seq_rows(p.rows, u.z, !p.memory_only), g, u.w * ROWS + R);
   if (!r.live) return;
-  const int c1 = u.w;
-  const int part_id = threadIdx.x / (DH / 2), d = (threadIdx.x - part_id * (DH / 2)) * 2;
   // share c0 holds the unit's start, those after it start inside the unit
-  auto slot = [&](int c) { return (2ll * ((long long)c * p.hkv + u.y) + (c == c0 ? 1 : 0)) * ROWS + R; };
-  float m = kNone, mv = kNone;
-  for (int c = c0 + (threadIdx.x & 31); c <= c1; c += 32) {
-    const float4 x = p.part_ml[slot(c)];
-    m = fmaxf(m, x.x);
-    mv = fmaxf(mv, x.y);
-  }
-  m = warp_max(m);
-  mv = warp_max(mv);
-  float l = 0.f, o0 = 0.f, o1 = 0.f;
-#pragma unroll 4
-  for (int c = c0 + part_id; c <= c1; c += kGroups) {
-    const float4 x = p.part_ml[slot(c)];
-    const float2 v = *reinterpret_cast<const float2 *>(p.part_o + slot(c) * DH + d);
-    l += x.z * ex2(x.x - m);
-    const float f = ex2(x.y - mv);
-    o0 = fmaf(f, v.x, o0);
-    o1 = fmaf(f, v.y, o1);
-  }
-  part[part_id][d / 2] = make_float2(o0, o1);
-  if (d == 0) part_l[part_id] = l;
-  __syncthreads();
-  if (part_id > 0) return;
-  l = o0 = o1 = 0.f;
+  auto slot = [&](int c) { return (2ll * ((long long)c * p.hkv + g) + (c == c0 ? 1 : 0)) * ROWS + R; };
+  constexpr int STEP = SPREAD ? kGroups : 1;
+  float m = kNone, mv = kNone, l = 0.f, o0 = 0.f, o1 = 0.f;
+  auto join = [&](float xm, float xmv, float xl, float x0, float x1) {
+    const float m1 = fmaxf(m, xm), mv1 = fmaxf(mv, xmv);
+    l = l * ex2(m - m1) + xl * ex2(xm - m1);
+    const float f = ex2(mv - mv1), g = ex2(xmv - mv1);
+    o0 = o0 * f + x0 * g;
+    o1 = o1 * f + x1 * g;
+    m = m1;
+    mv = mv1;
+  };
+#pragma unroll 1
+  for (int c = c0 + (SPREAD ? group : 0); c <= c1; c += kJoin * STEP) {
+    float4 x[kJoin];
+    float2 v[kJoin];
 #pragma unroll
-  for (int k = 0; k < kGroups; ++k) {
-    l += part_l[k];
-    o0 += part[k][d / 2].x;
-    o1 += part[k][d / 2].y;
+    for (int k = 0; k < kJoin; ++k)
+      if (c + k * STEP <= c1) {
+        x[k] = p.part_ml[slot(c + k * STEP)];
+        v[k] = *reinterpret_cast<const float2 *>(p.part_o + slot(c + k * STEP) * DH + d);
+      }
+#pragma unroll
+    for (int k = 0; k < kJoin; ++k)
+      if (c + k * STEP <= c1) join(x[k].x, x[k].y, x[k].z, v[k].x, v[k].y);
+  }
+  if constexpr (SPREAD) {
+    part[group][d / 2] = make_float4(m, mv, o0, o1);
+    if (d == 0) part_l[group] = l;
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int k = 1; k < kGroups; ++k) {
+      const float4 x = part[k][d / 2];
+      join(x.x, x.y, part_l[k], x.z, x.w);
+    }
   }
   const OutScale k = out_scale(m, mv, l);
   *reinterpret_cast<uint32_t *>(reinterpret_cast<T *>(p.out) + r.row * p.out_ld + (long long)r.head * DH + d) =
@@ -733,7 +747,12 @@ cudaError_t launch_as(const KvAttnParams &p, cudaStream_t st) {
   kern<<<(unsigned)p.ctas, kWarps * 32, L::BYTES, st>>>(p);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  return launch_pdl(kv_combine_kernel<T, DH, NT>, dim3((unsigned)p.ctas, (unsigned)std::min<long long>(L::ROWS, (long long)p.rows.max_rows * (p.hq / p.hkv))),
+  const unsigned rows = (unsigned)std::min<long long>(L::ROWS, (long long)p.rows.max_rows * (p.hq / p.hkv));
+  if (p.spread)
+    return launch_pdl(kv_combine_kernel<T, DH, NT, true>,
+                      dim3((unsigned)(p.rows.batch * p.most_groups * p.hkv), rows), dim3(kGroups * DH / 2),
+                      0, st, p);
+  return launch_pdl(kv_combine_kernel<T, DH, NT, false>, dim3((unsigned)p.ctas, (rows + kGroups - 1) / kGroups),
                     dim3(kGroups * DH / 2), 0, st, p);
 }
 template <typename T, int DH>
@@ -756,13 +775,13 @@ cudaError_t launch_dh(const KvAttnParams &p, cudaStream_t st) {
 // ---------------------------------------------------------------------------
 // 16 elements of K and of V per thread.
 __global__ void __launch_bounds__(256)
-    kv_block_copy_kernel(const __grid_constant__ KvAttnParams p, uint16_t *ko, uint16_t *vo, KvTileRows t) {
+    kv_block_copy_kernel(const __grid_constant__ KvAttnParams p, uint16_t *ko, uint16_t *vo, KvTileRows t,
+                         int per_seq) {
   const int dh = p.head_dim, chunks = p.hkv * dh / 16, cap = p.rows.cap;
-  const long long idx = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-  if (idx >= (long long)p.rows.batch * cap * chunks) return;
-  const long long row = idx / chunks;
-  const int c = (int)(idx - row * chunks);
-  const int b = (int)(row / cap), i = (int)(row - (long long)b * cap);
+  const int b = blockIdx.x / per_seq;
+  const uint32_t idx = (uint32_t)(blockIdx.x - b * per_seq) * 256u + threadIdx.x;   // in the sequence
+  const int i = (int)(idx / chunks), c = (int)(idx - (uint32_t)i * chunks);
+  const long long row = (long long)b * cap + i;
   const SeqRows s = seq_rows(p.rows, b, !p.memory_only);
   if (i == 0 && c == 0) {
     t.lo[b] = s.ok ? s.seq : 0;
@@ -770,7 +789,7 @@ __global__ void __launch_bounds__(256)
     t.base[b] = s.r0;
     if (!s.ok) set_status(p.status, CC_ERR_DEVICE_ARG);
   }
-  if (s.count == 0 || i >= s.seq + (p.memory_only ? 0 : s.count)) return;
+  if (s.count == 0 || i >= s.seq + (p.memory_only ? 0 : s.count)) return;   // (at most cap)
   const int h = c * 16 / dh, e = c * 16 - h * dh;
   const long long vec = kv_vec(p.pg, cap, b, h, i);
   const size_t dst = (size_t)row * p.hkv * dh + (size_t)h * dh + e;
@@ -801,12 +820,13 @@ __global__ void __launch_bounds__(256)
   convert(p.v + at * dh + e, vec < 0 ? 0 : p.ve[ei], i >= s.seq || vec < 0, vo + dst);
 }
 
-// A warp per new token and KV head: where its values hold NaN codes, the
-// outputs of its own and the later rows of its sequence get NaN there.
+// 16 values of a new token and KV head per thread: where they hold NaN codes, the
+// outputs of the token's own and the later rows of its sequence get NaN.
 template <typename T>
 __global__ void __launch_bounds__(256) kv_restore_nan_kernel(const __grid_constant__ KvAttnParams p) {
-  const long long w = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-  const int lane = threadIdx.x & 31, r = (int)(w / p.hkv), g = (int)(w - (long long)r * p.hkv);
+  const int dh = p.head_dim, chunks = p.hkv * dh / 16, G = p.hq / p.hkv;
+  const long long idx = (long long)blockIdx.x * 256 + threadIdx.x;
+  const int r = (int)(idx / chunks), c = (int)(idx - (long long)r * chunks);
   if (r >= p.rows.n_rows) return;
   int b = 0;   // the last sequence that starts at or before row r
   for (int hi = p.rows.batch - 1; b < hi;) {
@@ -815,15 +835,17 @@ __global__ void __launch_bounds__(256) kv_restore_nan_kernel(const __grid_consta
   }
   const SeqRows s = seq_rows(p.rows, b, true);
   if (r < s.r0 || r >= s.r0 + s.count) return;
+  const int g = c * 16 / dh, e = c * 16 - g * dh;
   const long long vec = kv_vec(p.pg, p.rows.cap, b, g, s.seq + r - s.r0);
   if (vec < 0) return;
-  const int dh = p.head_dim, G = p.hq / p.hkv;
-  for (int d = lane; d < dh; d += 32) {
-    if ((p.v[vec * dh + d] & 0x7F) != 0x7F) continue;
-    const T nan = std::is_same_v<T, __half> ? T(__ushort_as_half(0x7FFF)) : T(__ushort_as_bfloat16(0x7FFF));
+  const uint4 u = *reinterpret_cast<const uint4 *>(p.v + vec * dh + e);
+  if (!(nan_bytes(u.x) | nan_bytes(u.y) | nan_bytes(u.z) | nan_bytes(u.w))) return;
+  const T nan = std::is_same_v<T, __half> ? T(__ushort_as_half(0x7FFF)) : T(__ushort_as_bfloat16(0x7FFF));
+  for (int d = 0; d < 16; ++d) {
+    if ((p.v[vec * dh + e + d] & 0x7F) != 0x7F) continue;
     for (int i = r; i < s.r0 + s.count; ++i)
       for (int h = 0; h < G; ++h)
-        reinterpret_cast<T *>(p.out)[i * p.out_ld + (long long)(g * G + h) * dh + d] = nan;
+        reinterpret_cast<T *>(p.out)[i * p.out_ld + (long long)(g * G + h) * dh + e + d] = nan;
   }
 }
 
@@ -859,6 +881,8 @@ void kv_attn_plan(KvAttnParams &p, int sms) {
   const long long groups = (rows + 8 * p.nt - 1) / (8 * p.nt), tiles = (p.rows.cap + kTile - 1) / kTile + kUnitTiles;
   p.shares = line_shares(p.resident, p.rows.batch * groups * tiles);
   p.ctas = p.shares * p.hkv;
+  p.spread = p.shares >= kGroups * p.rows.batch * groups;
+  p.most_groups = (int)groups;
 }
 
 size_t kv_attn_part_bytes(const KvAttnParams &p) {
@@ -879,16 +903,16 @@ cudaError_t launch_kv_attn(const KvAttnParams &p, cudaStream_t st) {
 
 cudaError_t launch_kv_block_copy(const KvAttnParams &p, void *ko, void *vo, const KvTileRows &t,
                                  cudaStream_t st) {
-  const long long n = (long long)p.rows.batch * p.rows.cap * (p.hkv * p.head_dim / 16);
-  const long long blocks = (n + 255) / 256;
-  if (blocks > 0x7FFFFFFFll) return cudaErrorInvalidValue;
+  const long long n = (long long)p.rows.cap * (p.hkv * p.head_dim / 16), per_seq = (n + 255) / 256;
+  const long long blocks = per_seq * p.rows.batch;
+  if (blocks > 0x7FFFFFFFll || n > 0xFFFFFF00ll) return cudaErrorInvalidValue;
   kv_block_copy_kernel<<<(unsigned)blocks, 256, 0, st>>>(
-      p, reinterpret_cast<uint16_t *>(ko), reinterpret_cast<uint16_t *>(vo), t);
+      p, reinterpret_cast<uint16_t *>(ko), reinterpret_cast<uint16_t *>(vo), t, (int)per_seq);
   return cudaGetLastError();
 }
 
 cudaError_t launch_kv_restore_nan(const KvAttnParams &p, cudaStream_t st) {
-  const long long blocks = ((long long)p.rows.n_rows * p.hkv + 7) / 8;
+  const long long blocks = ((long long)p.rows.n_rows * (p.hkv * p.head_dim / 16) + 255) / 256;
   if (blocks > 0x7FFFFFFFll) return cudaErrorInvalidValue;
   if (p.f16) kv_restore_nan_kernel<__half><<<(unsigned)blocks, 256, 0, st>>>(p);
   else kv_restore_nan_kernel<__nv_bfloat16><<<(unsigned)blocks, 256, 0, st>>>(p);

@@ -23,9 +23,12 @@ struct KvAttnParams {
   int resident;                 // shares of a KV head's key tiles that the SMs work on at once
   int shares;                   // shares at most, each one CTA per KV head
   int ctas;                     // shares * hkv
+  int most_groups;              // units of a KV head and sequence at most
+  int spread;                   // few units, of many shares each
   float *part_o;                // [2 * ctas][8 * nt][head_dim]: what a CTA leaves of the unit
   float4 *part_ml;              // [2 * ctas][8 * nt]            before and after its share
-  int4 *cut;                    // [ctas]: the unit that starts in a CTA's share and goes on
+  int4 *cut;                    // [ctas]: the unit that starts in a CTA's share and goes on;
+                                // spread: the shares of each unit
   unsigned *status;
 };
 
