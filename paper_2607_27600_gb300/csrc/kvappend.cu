@@ -31,52 +31,63 @@ constexpr int kThreads = 256;
 constexpr int kSplitCtas = 2;   // CTAs per SM to split the heads for
 constexpr int kLeastExp = 10, kMostExp = 247, kUnitExp = 127;   // scale exponents written
 
-// 8 elements as they lie in memory.
-template <typename T>
-struct Raw8 {
-  uint4 w[sizeof(T) / 2];
-  CC_DEV void load(const T *src) {
+// The 8 elements of half a head that a lane holds: pieces of 16 bytes which lie side
+// by side across the team's lanes, so that a load or store takes whole sectors.
+template <typename T, int DH>
+struct Lane {
+  static constexpr int GRP = 16 / sizeof(T), PIECES = 8 / GRP, APART = DH / 2 / PIECES;
+  int first;   // of piece 0
+  CC_DEV explicit Lane(int lane) : first(lane % (DH / 16) * GRP) {}
+  CC_DEV int element(int i) const { return first + i / GRP * APART + i % GRP; }
+  CC_DEV void store(T *dst, const float (&x)[8]) const {   // dst: the half's first element
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const uint4 *>(src)[i];
-  }
-  CC_DEV void widen(float (&x)[8]) const {
-    const uint32_t u[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
-    if constexpr (sizeof(T) == 4) {
-      const uint32_t v[4] = {w[1].x, w[1].y, w[1].z, w[1].w};
+    for (int j = 0; j < PIECES; ++j) {
+      if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<float4 *>(dst + first + j * APART) =
+            make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+      } else {
+        uint32_t w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(u[i]), x[4 + i] = __uint_as_float(v[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (std::is_same_v<T, __half>) {
-          const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&u[i]));
-          x[2 * i] = f.x, x[2 * i + 1] = f.y;
-        } else {
-          x[2 * i] = bf16_lo(u[i]), x[2 * i + 1] = bf16_hi(u[i]);
-        }
+        for (int i = 0; i < 4; ++i)
+          w[i] = std::is_same_v<T, __half> ? pack_f16x2(x[2 * i], x[2 * i + 1])
+                                           : pack_bf16x2(x[2 * i], x[2 * i + 1]);
+        *reinterpret_cast<uint4 *>(dst + first) = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
   }
-};
-template <typename T>
-CC_DEV void store8(T *dst, const float (&x)[8]) {
-  if constexpr (sizeof(T) == 4) {
-    reinterpret_cast<float4 *>(dst)[0] = make_float4(x[0], x[1], x[2], x[3]);
-    reinterpret_cast<float4 *>(dst)[1] = make_float4(x[4], x[5], x[6], x[7]);
-  } else {
-    uint32_t w[4];
+  CC_DEV void store_bf16(__nv_bfloat16 *dst, const float (&x)[8]) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[i] = std::is_same_v<T, __half> ? pack_f16x2(x[2 * i], x[2 * i + 1])
-                                       : pack_bf16x2(x[2 * i], x[2 * i + 1]);
-    *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int i = 0; i < 8; i += 4)
+      *reinterpret_cast<uint2 *>(dst + element(i)) =
+          make_uint2(pack_bf16x2(x[i], x[i + 1]), pack_bf16x2(x[i + 2], x[i + 3]));
   }
-}
-CC_DEV void store_codes8(uint8_t *dst, const float (&x)[8]) {
-  *reinterpret_cast<uint2 *>(dst) =
-      make_uint2(pack_e4m3x2(x[0], x[1]) | (pack_e4m3x2(x[2], x[3]) << 16),
-                 pack_e4m3x2(x[4], x[5]) | (pack_e4m3x2(x[6], x[7]) << 16));
-}
+  CC_DEV void store_codes(uint8_t *dst, const float (&x)[8]) const {
+    const uint32_t lo = pack_e4m3x2(x[0], x[1]) | (pack_e4m3x2(x[2], x[3]) << 16);
+    const uint32_t hi = pack_e4m3x2(x[4], x[5]) | (pack_e4m3x2(x[6], x[7]) << 16);
+    if constexpr (PIECES == 1) {
+      *reinterpret_cast<uint2 *>(dst + first) = make_uint2(lo, hi);
+    } else {
+      *reinterpret_cast<uint32_t *>(dst + element(0)) = lo;
+      *reinterpret_cast<uint32_t *>(dst + element(4)) = hi;
+    }
+  }
+};
+
+// 8 elements as they lie in memory, in words.
+template <typename T>
+struct Raw8 {
+  uint32_t w[2 * sizeof(T)];
+  CC_DEV void widen(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(w[i]);
+      else if constexpr (std::is_same_v<T, __half>)
+        x[i] = i & 1 ? __high2float(*reinterpret_cast<const __half2 *>(&w[i / 2]))
+                     : __low2float(*reinterpret_cast<const __half2 *>(&w[i / 2]));
+      else x[i] = i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
+    }
+  }
+};
 
 CC_DEV float finite_abs(float x) {
   const float a = fabsf(x);
@@ -126,34 +137,70 @@ CC_DEV void turn_cs(const float2 *table, uint32_t frac, float &c, float &s) {   
   s = fmaf(t.y, cd, t.x * sd);
 }
 
-// A lane's items ahead: 8 + 8 elements each.
+// What magnitudes a lane has seen of one head's keys or values.
 template <typename T>
+struct Bound {
+  float top = 0.f;     // keys: of max + min / 2; fp32 values too
+  uint32_t seen = 0;   // 16-bit types: the largest magnitudes' bits, two at a time
+  CC_DEV static float of(uint32_t bits) {
+    return std::is_same_v<T, __half> ? __half2float(__ushort_as_half((unsigned short)bits))
+                                     : __uint_as_float(bits << 16);
+  }
+  // Infinities and NaN take no part: with `careful` one by one, else they are seen
+  // and `odd` tells.
+  CC_DEV void add(const Raw8<T> &ra, const Raw8<T> &rc, bool is_k, bool careful) {
+    if (sizeof(T) == 4 || careful) {
+      float a[8], c[8];
+      ra.widen(a);
+      rc.widen(c);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float u = finite_abs(a[i]), w = finite_abs(c[i]), hi = fmaxf(u, w);
+        top = fmaxf(top, is_k ? __fadd_rn(hi, 0.5f * fminf(u, w)) : hi);
+      }
+    } else {
+      float2 m = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {   // magnitudes order as their bits do
+        const uint32_t u = ra.w[i] & 0x7FFF7FFFu, w = rc.w[i] & 0x7FFF7FFFu, hi = __vmaxu2(u, w);
+        seen = __vmaxu2(seen, hi);
+        if (is_k) {
+          const uint32_t lo = __vminu2(u, w);
+          m.x = fmaxf(m.x, __fadd_rn(of(hi & 0xFFFFu), 0.5f * of(lo & 0xFFFFu)));
+          m.y = fmaxf(m.y, __fadd_rn(of(hi >> 16), 0.5f * of(lo >> 16)));
+        }
+      }
+      top = fmaxf(top, fmaxf(m.x, m.y));
+    }
+  }
+  CC_DEV bool odd() const {
+    const uint32_t inf = std::is_same_v<T, __half> ? 0x7C00u : 0x7F80u;
+    return max(seen & 0xFFFFu, seen >> 16) >= inf;
+  }
+  CC_DEV float get(bool is_k) const { return is_k ? top : fmaxf(top, of(max(seen & 0xFFFFu, seen >> 16))); }
+};
+
+// A lane's items ahead: 8 + 8 elements each.
+template <typename T, int DH>
 struct Ahead {
-  static constexpr int PIECES = sizeof(T) / 2;              // 16-byte pieces of 8 elements
-  static constexpr int SLOTS = 256 / (2 * PIECES * 16);     // 256 bytes a lane
+  using L = Lane<T, DH>;
+  static constexpr int SLOTS = 256 / (2 * L::PIECES * 16);   // 256 bytes a lane
   static constexpr int BYTES = kThreads * 256;
   uint8_t *mem;   // of the lane
-  CC_DEV void issue(int slot, const T *a, const T *c) {
-    const uint32_t to = smem_u32(mem) + slot * (2 * PIECES * 16 * kThreads);
+  CC_DEV void issue(int slot, const T *half0) {   // this lane's first element of the head
+    const uint32_t to = smem_u32(mem) + slot * (2 * L::PIECES * 16 * kThreads);
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      copy16(to + i * 16 * kThreads, reinterpret_cast<const uint4 *>(a) + i);
-      copy16(to + (PIECES + i) * 16 * kThreads, reinterpret_cast<const uint4 *>(c) + i);
-    }
+    for (int i = 0; i < 2 * L::PIECES; ++i)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * 16 * kThreads),
+                   "l"(half0 + i * L::APART) : "memory");
   }
-  CC_DEV void get(int slot, float (&a)[8], float (&c)[8]) const {
-    const uint4 *from = reinterpret_cast<const uint4 *>(mem + slot * (2 * PIECES * 16 * kThreads));
-    Raw8<T> ra, rc;
+  CC_DEV void get(int slot, Raw8<T> &a, Raw8<T> &c) const {
+    const uint4 *from = reinterpret_cast<const uint4 *>(mem + slot * (2 * L::PIECES * 16 * kThreads));
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      ra.w[i] = from[i * kThreads];
-      rc.w[i] = from[(PIECES + i) * kThreads];
+    for (int i = 0; i < L::PIECES; ++i) {
+      *reinterpret_cast<uint4 *>(&a.w[4 * i]) = from[i * kThreads];
+      *reinterpret_cast<uint4 *>(&c.w[4 * i]) = from[(L::PIECES + i) * kThreads];
     }
-    ra.widen(a);
-    rc.widen(c);
-  }
-  CC_DEV static void copy16(uint32_t dst, const void *src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
   }
   CC_DEV static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
   CC_DEV static void wait_oldest() {   // of SLOTS - 1 in flight before the last one was issued
@@ -165,7 +212,7 @@ template <typename T, int DH>
 __global__ void __launch_bounds__(kThreads, 3)
     kv_append_kernel(const __grid_constant__ KvAppendParams p) {
   constexpr int HALF = DH / 2, TPR = DH / 16, RPI = 32 / TPR;   // lanes per row, rows per warp
-  constexpr int TEAMS = kThreads / TPR, SLOTS = Ahead<T>::SLOTS;
+  constexpr int TEAMS = kThreads / TPR, SLOTS = Ahead<T, DH>::SLOTS;
   extern __shared__ __align__(16) uint8_t smem[];
   const int B = p.block, per_seq = (p.rows.max_rows + B - 2) / B + 1;
   const int b = blockIdx.x / per_seq;
@@ -182,10 +229,11 @@ __global__ void __launch_bounds__(kThreads, 3)
   const int n = min(base + B, s.seq + s.count) - (base + old);
   if (n <= 0) return;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int at8 = (lane % TPR) * 8;
-  Ahead<T> ahead{smem + tid * 16};
-  float2 *table = reinterpret_cast<float2 *>(smem + Ahead<T>::BYTES);
-  float *scale = reinterpret_cast<float *>(table + kTable);   // 1 / scale: K heads, V heads
+  const Lane<T, DH> mine(lane);
+  Ahead<T, DH> ahead{smem + tid * 16};
+  float2 *table = reinterpret_cast<float2 *>(smem + Ahead<T, DH>::BYTES);
+  // of K heads, then of V heads: the bound, then 1 / scale
+  float *scale = reinterpret_cast<float *>(table + kTable);
   // this CTA's heads
   const int ny = gridDim.y, y = blockIdx.y;
   const int k0 = p.hkv * y / ny, nk = p.hkv * (y + 1) / ny - k0;
@@ -194,6 +242,7 @@ __global__ void __launch_bounds__(kThreads, 3)
   // the unit lies in one page: vector of KV head g and slot base + i
   const long long row0 = p.pg.head_major ? 0 : kv_row(p.pg, p.rows.cap, b, base);
   const int vstep = p.pg.head_major ? 1 : p.hkv;
+  const long long head_step = (p.pg.head_major ? (long long)p.rows.cap : 1) * DH;   // elements
   auto vec_at = [&](int g) {
     return p.pg.head_major ? ((long long)b * p.hkv + g) * p.rows.cap + base : row0 * p.hkv + g;
   };
@@ -202,45 +251,63 @@ __global__ void __launch_bounds__(kThreads, 3)
   if (p.rotate) table_entry(table, tid);
   static_assert(kTable == kThreads, "a thread an entry");
   if (by_block && row0 >= 0) {
-    const int team = lane / TPR;
-    for (int job = warp; job < 2 * nk; job += kThreads / 32) {
+    constexpr int kWarps = kThreads / 32;
+    // bounds: a job (K or V of a head) to as many warps as there are for it
+    const int jobs = 2 * nk;
+    int parts = 1;
+    while (parts * 2 * jobs <= kWarps) parts *= 2;
+    for (int i = tid; i < jobs; i += kThreads) scale[i] = 0.f;
+    __syncthreads();
+    const int team = lane / TPR + warp % parts * RPI;
+    for (int job = warp / parts; job < jobs; job += kWarps / parts) {
+      const bool is_k = job < nk;
+      const long long ld = is_k ? p.k_ld : p.v_ld;
+      const T *src = reinterpret_cast<const T *>(is_k ? p.k : p.v) + r0 * ld +
+                     (k0 + (is_k ? job : job - nk)) * DH + mine.first;
+      Bound<T> bound;
+      auto sweep = [&](bool careful) {
+        auto issue = [&](int r, int slot) {
+          if (r < n) ahead.issue(slot, src + r * ld);
+          ahead.commit();
+        };
+#pragma unroll 1
+        for (int i = 0; i < SLOTS - 1; ++i) issue(team + i * RPI * parts, i);
+        int slot = 0;
+#pragma unroll 1
+        for (int r = team; r < n; r += RPI * parts) {
+          issue(r + (SLOTS - 1) * RPI * parts, slot == 0 ? SLOTS - 1 : slot - 1);
+          ahead.wait_oldest();
+          Raw8<T> a, c;
+          ahead.get(slot, a, c);
+          slot = slot + 1 == SLOTS ? 0 : slot + 1;
+          bound.add(a, c, is_k, careful);
+        }
+      };
+      sweep(false);
+      if (__any_sync(0xFFFFFFFFu, bound.odd())) {
+        bound = Bound<T>();
+        sweep(true);
+      }
+      const float top = warp_max(bound.get(is_k));
+      // (magnitudes order as their bits do)
+      if (lane == 0) atomicMax(reinterpret_cast<int *>(scale) + job, __float_as_int(top));
+    }
+    __syncthreads();
+    for (int job = warp; job < jobs; job += kWarps) {
       const bool is_k = job < nk;
       const int g = k0 + (is_k ? job : job - nk);
-      const long long vec0 = vec_at(g), ld = is_k ? p.k_ld : p.v_ld;
-      const T *src = reinterpret_cast<const T *>(is_k ? p.k : p.v) + r0 * ld + g * DH + at8;
+      const long long vec0 = vec_at(g);
       const long long ei = p.pg.head_major ? vec0 / B : row0 / B * p.hkv + g;
       uint8_t *ep = (is_k ? p.ke : p.ve) + ei;
       const int e_old = old ? *ep : 0;
-      auto issue = [&](int r, int slot) {
-        if (r < n) ahead.issue(slot, src + r * ld, src + r * ld + HALF);
-        ahead.commit();
-      };
-#pragma unroll 1
-      for (int i = 0; i < SLOTS - 1; ++i) issue(team + i * RPI, i);
-      float bound = 0.f;
-      int slot = 0;
-#pragma unroll 1
-      for (int r = team; r < n; r += RPI) {
-        issue(r + (SLOTS - 1) * RPI, slot == 0 ? SLOTS - 1 : slot - 1);
-        ahead.wait_oldest();
-        float a[8], c[8];
-        ahead.get(slot, a, c);
-        slot = slot + 1 == SLOTS ? 0 : slot + 1;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float u = finite_abs(a[i]), w = finite_abs(c[i]);
-          const float hi = fmaxf(u, w);
-          bound = fmaxf(bound, is_k ? __fadd_rn(hi, 0.5f * fminf(u, w)) : hi);
-        }
-      }
-      int e = max(scale_exp(warp_max(bound)), e_old);
+      int e = max(scale_exp(scale[job]), e_old);
       if (e == 0) e = kUnitExp;   // zeros alone
       if (old && e > e_old) {     // the older codes by a power of two
         const float f = pow2_biased(127 + e_old - e);
         uint8_t *codes = reinterpret_cast<uint8_t *>(is_k ? p.kc : p.vc);
 #pragma unroll 1
-        for (int r = team; r < old; r += RPI) {
-          uint4 *at = reinterpret_cast<uint4 *>(codes + (vec0 + (long long)r * vstep) * DH + at8 * 2);
+        for (int r = lane / TPR; r < old; r += RPI) {
+          uint4 *at = reinterpret_cast<uint4 *>(codes + (vec0 + (long long)r * vstep) * DH + lane % TPR * 16);
           const uint4 u = *at;
           uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -258,6 +325,7 @@ __global__ void __launch_bounds__(kThreads, 3)
           *at = make_uint4(w[0], w[1], w[2], w[3]);
         }
       }
+      __syncwarp();   // every lane has read the bound and the older exponent
       if (lane == 0) {
         *ep = (uint8_t)e;
         scale[job] = pow2_biased(254 - e);
@@ -281,15 +349,15 @@ __global__ void __launch_bounds__(kThreads, 3)
   const T *ki, *vi, *qi;
   auto enter = [&]() {
     const long long r = r0 + ri;
-    ki = reinterpret_cast<const T *>(p.k) + r * p.k_ld + k0 * DH + at8;
-    vi = reinterpret_cast<const T *>(p.v) + r * p.v_ld + (k0 - nk) * DH + at8;
-    qi = reinterpret_cast<const T *>(p.q) + r * p.q_ld + (q0 - 2 * nk) * DH + at8;
+    ki = reinterpret_cast<const T *>(p.k) + r * p.k_ld + k0 * DH + mine.first;
+    vi = reinterpret_cast<const T *>(p.v) + r * p.v_ld + (k0 - nk) * DH + mine.first;
+    qi = reinterpret_cast<const T *>(p.q) + r * p.q_ld + (q0 - 2 * nk) * DH + mine.first;
   };
   enter();
   auto issue = [&](int slot) {
     if (ri < n) {
       const T *src = (hi < nk ? ki : hi < 2 * nk ? vi : qi) + hi * DH;
-      ahead.issue(slot, src, src + HALF);
+      ahead.issue(slot, src);
       hi += ht;
       if (hi >= heads) {
         hi = h0;
@@ -316,45 +384,53 @@ __global__ void __launch_bounds__(kThreads, 3)
       for (int i = 0; i < 8; ++i) {
         // pos * turns mod 2^64 is a fraction of a turn
         float sn, cs;
-        turn_cs(table, (uint32_t)(((unsigned long long)at * p.turns[at8 + i]) >> 32), cs, sn);
+        turn_cs(table, (uint32_t)(((unsigned long long)at * p.turns[mine.element(i)]) >> 32), cs, sn);
         (i & 1 ? t.c[i / 2].y : t.c[i / 2].x) = cs;
         (i & 1 ? t.s[i / 2].y : t.s[i / 2].x) = sn;
         (i & 1 ? t.n[i / 2].y : t.n[i / 2].x) = -sn;
       }
     }
+    // where the row's K and V of head k0 go, and its Q of head q0
+    const long long el0 = row0 < 0 ? 0 : (vec_at(k0) + (long long)(old + r) * vstep) * DH;
+    T *out = reinterpret_cast<T *>(p.q_out) + (r0 + r) * p.q_out_ld + q0 * DH;
 #pragma unroll 1
     for (int h = h0; h < heads; h += ht) {
       issue(slot == 0 ? SLOTS - 1 : slot - 1);
       ahead.wait_oldest();
+      Raw8<T> ra, rc;
+      ahead.get(slot, ra, rc);
       float a[8], c[8];
-      ahead.get(slot, a, c);
+      ra.widen(a);
+      rc.widen(c);
       slot = slot + 1 == SLOTS ? 0 : slot + 1;
       const bool is_k = h < nk, is_q = h >= 2 * nk;
       if (p.rotate && (is_k || is_q)) rotate8(a, c, t);
       if (is_q) {
-        T *out = reinterpret_cast<T *>(p.q_out) + (r0 + r) * p.q_out_ld + (q0 + h - 2 * nk) * DH + at8;
-        store8(out, a);
-        store8(out + HALF, c);
+        mine.store(out + (h - 2 * nk) * DH, a);
+        mine.store(out + (h - 2 * nk) * DH + HALF, c);
         continue;
       }
       if (row0 < 0) continue;
-      const long long el = (vec_at(k0 + (is_k ? h : h - nk)) + (long long)(old + r) * vstep) * DH + at8;
+      const long long el = el0 + (is_k ? h : h - nk) * head_step;
       void *buf = is_k ? p.kc : p.vc;
       if (p.format == CC_KV_BF16) {
-        store8(reinterpret_cast<__nv_bfloat16 *>(buf) + el, a);
-        store8(reinterpret_cast<__nv_bfloat16 *>(buf) + el + HALF, c);
+        mine.store_bf16(reinterpret_cast<__nv_bfloat16 *>(buf) + el, a);
+        mine.store_bf16(reinterpret_cast<__nv_bfloat16 *>(buf) + el + HALF, c);
         continue;
       }
       const float inv = by_block ? scale[h] : is_k ? p.k_qscale : p.v_qscale;
-      if (by_block) {   // 0 times an infinity: NaN (one scale a layer saturates it, as the appends do)
+      // 0 times an infinity: NaN (one scale a layer saturates it, as the appends do)
+      const float2 inv2 = make_float2(inv, inv), zero = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) a[i] = fmaf(a[i], 0.f, a[i] * inv), c[i] = fmaf(c[i], 0.f, c[i] * inv);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) a[i] *= inv, c[i] *= inv;
+      for (int i = 0; i < 8; i += 2) {
+        float2 x = make_float2(a[i], a[i + 1]), z = make_float2(c[i], c[i + 1]);
+        const float2 xs = __fmul2_rn(x, inv2), zs = __fmul2_rn(z, inv2);
+        x = by_block ? __ffma2_rn(x, zero, xs) : xs;
+        z = by_block ? __ffma2_rn(z, zero, zs) : zs;
+        a[i] = x.x, a[i + 1] = x.y, c[i] = z.x, c[i + 1] = z.y;
       }
-      store_codes8(reinterpret_cast<uint8_t *>(buf) + el, a);
-      store_codes8(reinterpret_cast<uint8_t *>(buf) + el + HALF, c);
+      mine.store_codes(reinterpret_cast<uint8_t *>(buf) + el, a);
+      mine.store_codes(reinterpret_cast<uint8_t *>(buf) + el + HALF, c);
     }
   }
 }
@@ -387,7 +463,7 @@ cudaError_t launch_append_as(const KvAppendParams &p, int sms, cudaStream_t st) 
   // a unit's heads over several CTAs until they fill the SMs
   const long long busy = std::min(units, (long long)p.rows.n_rows / p.block + p.rows.batch);   // (about)
   const int split = (int)std::min<long long>(p.hkv, std::max<long long>(1, (kSplitCtas * sms + busy - 1) / busy));
-  const size_t smem = Ahead<T>::BYTES + kTable * sizeof(float2) + 2 * ((size_t)p.hkv / split + 1) * sizeof(float);
+  const size_t smem = Ahead<T, DH>::BYTES + kTable * sizeof(float2) + 2 * ((size_t)p.hkv / split + 1) * sizeof(float);
   static std::atomic<size_t> allowed[64] = {};   // (the few floats grow with hkv)
   int dev = 0;
   cudaGetDevice(&dev);
