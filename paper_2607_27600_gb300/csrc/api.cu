@@ -1836,13 +1836,16 @@ KvAttnParams kv_attn_params(const cc_model_cfg *c, const cc_kv_cache *kv, const 
   return p;
 }
 
-// Whether a step's rows take the tile attention: chunks, of so many query rows
-// per KV head and sequence on average.
-constexpr int kTileRows = 64, kTileMinRows = 16;
-bool step_on_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows) {
+// Whether a step's rows take the tile attention: chunks of more query rows per KV
+// head and sequence, on average, than two units of the direct kernel hold (fp16, whose
+// tiles multiply pairs: three).  Direct and tiles, 8 sequences of 8192 slots and 32/8
+// heads: 64 rows 114 and 142 us, 96 rows 161 and 143; fp16 96 rows 175 and 208, 128
+// rows 228 and 209; one Qwen2.5-7B sequence: 56 rows 23 and 30, 112 rows 32 and 30.
+constexpr int kTileRows = 64, kTileRowsF16 = 96, kTileMinRows = 4;
+bool step_on_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows, bool f16) {
   const long long group = c->n_q_heads / c->n_kv_heads;
   return rows->row_start && rows->max_rows >= kTileMinRows &&
-         rows->n_rows * group >= (long long)kTileRows * kv->batch;
+         rows->n_rows * group > (long long)(f16 ? kTileRowsF16 : kTileRows) * kv->batch;
 }
 
 // Workspace of the tile attention: the layer as bf16, the sequences' rows, fp16
@@ -2004,8 +2007,10 @@ cc_status cc_kv_append(const cc_model_cfg *cfg, const cc_kv_cache *kv, int32_t l
 size_t cc_kv_attention_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *kv,
                                       const cc_rows *rows) {
   if (check_cfg(cfg) != CC_OK || check_step(kv, rows) != CC_OK || rows->n_rows == 0) return 0;
-  if (step_on_tiles(cfg, kv, rows)) return step_tile_layout(cfg, kv, rows, kStepMaxSms).total;
-  return align256(kv_attn_part_bytes(kv_attn_params(cfg, kv, rows, kStepMaxSms)));
+  const size_t direct = align256(kv_attn_part_bytes(kv_attn_params(cfg, kv, rows, kStepMaxSms)));
+  // (for rows of either type)
+  return step_on_tiles(cfg, kv, rows, false)
+             ? std::max(direct, step_tile_layout(cfg, kv, rows, kStepMaxSms).total) : direct;
 }
 
 cc_status cc_kv_attention(const cc_model_cfg *cfg, const cc_kv_cache *kv, int32_t layer,
@@ -2040,7 +2045,7 @@ cc_status cc_kv_attention(const cc_model_cfg *cfg, const cc_kv_cache *kv, int32_
   p.ve = reinterpret_cast<const uint8_t *>(kv->v_exp[layer]);
   p.status = dev->status;
   CC_TRY(wait_kv_ready(kv, layer, layer + 1, st));
-  if (step_on_tiles(cfg, kv, rows)) {
+  if (step_on_tiles(cfg, kv, rows, p.f16 != 0)) {
     if (out_ld > 0x7FFFFFFF) return CC_ERR_UNSUPPORTED;
     TimedScope t(CC_KERNEL_KV_ATTENTION, st);
     return run_step_tiles(cfg, kv, rows, p, ws, dev->sms, st);
