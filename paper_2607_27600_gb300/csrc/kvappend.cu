@@ -4,9 +4,9 @@
 //
 // A unit of work is a block of `block` cache slots of one sequence that new
 // rows fall into (block format: the slots that share a scale), a CTA's is a unit
-// and a share of the heads.  Block format: first a warp per KV head bounds the
-// magnitudes of the unit's keys or values and settles the scale.  For keys it
-// bounds the radius of each rotated pair, sqrt(a^2 + b^2) <= max + min / 2, so that
+// and a share of the heads.  Block format: first the warps, shared evenly among the KV
+// heads' keys and values, bound the unit's magnitudes, and a warp settles each scale
+// and rescales what the block held.  For keys it bounds the radius of each rotated pair, sqrt(a^2 + b^2) <= max + min / 2, so that
 // the scale needs no angle and is the same bits however cos and sin are rounded;
 // it is at most 1.12 times the largest magnitude that any rotation gives.  Then
 // teams of head_dim / 16 lanes take a row each, or where there are few rows some of
@@ -17,6 +17,9 @@
 // copies what it will read a few heads (rows, for the bound) ahead into slots of its
 // own (cp.async, no barrier): loops unrolled over loads instead held as much in
 // flight but half of the time nothing, and their code was a single token's latency.
+// Four chunks of 4096 tokens, 32/8 heads of 128, bf16: 369 MB in 74.8 us (4.9 TB/s); 2957
+// tokens of five ragged sequences, 28/4 heads, fp32: 100 MB in 16.6 us (6.0 TB/s); a
+// token each of 64 sequences: 6.6 us, latency (launch, bound, rows one after another).
 #include "kvappend.cuh"
 
 #include <algorithm>

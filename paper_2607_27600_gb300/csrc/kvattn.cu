@@ -27,6 +27,10 @@
 // permute of two rows' words before they are widened.  The 16 keys are taken in an
 // order (row_of) in which, with the rows' pieces swizzled, neither product's reads
 // meet in a bank.
+//
+// 64 ragged sequences of 1500 to 32767 slots, a row each, 32/8 heads: 2.25 GB in 339 us
+// (6.6 TB/s); one of 8192 slots, 28/4 heads: 11.3 us, of which the stream is 1.3.  Units
+// of 24 rows are bound by issue: 16 sequences' 5 rows of fp16, 153 MB in 59 us.
 #include "kvattn.cuh"
 
 #include <algorithm>
@@ -319,7 +323,7 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
         }
         if (!ok && lane == 0) set_status(p.status, CC_ERR_DEVICE_ARG);
         // the block's scale exponents: the aligned words that hold them
-        const long long eo = e0 + (off >> log_block) * hs;
+        const long long eo = e0 + (long long)(off >> log_block) * hs;
         if (ok && lane < 2)
           copy4(dst + 2 * L::HALF + lane * 4, (lane ? p.ve : p.ke) + (eo & ~3ll),
                 (int)min(4ll, p.exp_bytes - (eo & ~3ll)));

@@ -20,6 +20,9 @@
 // keep it under 6 instructions per logit.  A CTA takes a row; with few rows a
 // cluster of up to 8 CTAs does, a contiguous segment each, and rank 0 joins their
 // sums and sorted lists through distributed shared memory.
+//
+// 4096 rows of 128256 bf16 logits, 8 alternatives: 1.05 GB in 181 us (5.8 TB/s); 64 rows
+// of 152064: 10 us; one fp32 row: 7.3 us, launch, cluster and sort one after another.
 #include "logprob.cuh"
 
 #include <type_traits>
