@@ -135,9 +135,9 @@ CC_DEV void turn_cs(const float2 *table, uint32_t frac, float &c, float &s) {   
   const float2 t = table[at >> 24];
   const float d = (float)((int)(at & 0xFFFFFFu) - (1 << 23)) * 1.4629180792671596e-09f;   // 2 pi / 2^32
   const float d2 = d * d;
-  const float cd = fmaf(d2, fmaf(d2, 1.f / 24.f, -0.5f), 1.f), sd = fmaf(d * d2, -1.f / 6.f, d);
-  c = fmaf(t.x, cd, -t.y * sd);
-  s = fmaf(t.y, cd, t.x * sd);
+  const float cd1 = d2 * fmaf(d2, 1.f / 24.f, -0.5f), sd = fmaf(d * d2, -1.f / 6.f, d);   // cos d - 1, sin d
+  c = t.x + fmaf(t.x, cd1, -t.y * sd);   // (the small terms' roundings do not count)
+  s = t.y + fmaf(t.y, cd1, t.x * sd);
 }
 
 // What magnitudes a lane has seen of one head's keys or values.
