@@ -1849,23 +1849,27 @@ bool step_on_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *
 }
 
 // Workspace of the tile attention: the layer as bf16, the sequences' rows, fp16
-// queries as pairs, and the partial rows of key splits.
+// queries as pairs, and how the SMs share the units (kvattn.cu) with the partial rows.
+// The plan's single CTA takes up to kPlanUnits units; more are waves enough.
+constexpr int kPlanUnits = 1024;
 struct StepTileWs {
-  size_t k, v, lo, hi, base, pairs, part_o, part_ml, total;
-  long long units;   // of the launch; most have no rows where sequences differ
-  int splits;        // key splits of a unit
+  size_t k, v, lo, hi, base, pairs, pieces, joins, part_o, part_ml, total;
+  KvTilePlan plan;   // (units = 0: none)
 };
 StepTileWs step_tile_layout(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows, int sms) {
   StepTileWs w{};
-  // Units with rows, at most: whole ones of n_rows and a part-filled one per
-  // sequence.  Splits until they fill the SMs, of four key tiles at least, while the
-  // partial rows of all units stay below 1024.
+  // Units with rows, at most: whole ones of n_rows and a part-filled one per sequence.
   const int P = attn_positions_per_unit(c->n_q_heads / c->n_kv_heads);
-  w.units = (long long)kv->batch * c->n_kv_heads * ((rows->max_rows + P - 1) / P);
-  const long long busy = std::min(w.units, (long long)c->n_kv_heads * (rows->n_rows / P + kv->batch));
-  const long long tiles = ((long long)kv->cap + 127) / 128;
-  w.splits = (int)std::max(1LL, std::min({sms / std::max(1LL, busy), tiles / kAttnMinSplitTiles,
-                                          1024 / std::max(1LL, w.units)}));
+  const long long units = std::min((long long)kv->batch * c->n_kv_heads * ((rows->max_rows + P - 1) / P),
+                                   (long long)c->n_kv_heads * (rows->n_rows / P + kv->batch));
+  if (units <= kPlanUnits && kv->batch <= kTilePlanBatch &&
+      units * ((long long)kv->cap / 128 + 8) < (1ll << 30)) {   // (the plan counts in 32 bits)
+    w.plan.P = P;
+    w.plan.sms = sms;
+    w.plan.units = (int)units;
+    w.plan.n_pieces = (int)units + sms;
+    w.plan.n_joins = (int)std::min<long long>(units, sms);
+  }
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = align256(off + bytes); return o; };
   const size_t copy = (size_t)kv->batch * kv->cap * c->n_kv_heads * c->head_dim * 2;
@@ -1875,9 +1879,11 @@ StepTileWs step_tile_layout(const cc_model_cfg *c, const cc_kv_cache *kv, const 
   w.hi = take((size_t)kv->batch * 4);
   w.base = take((size_t)kv->batch * 4);
   w.pairs = take((size_t)rows->n_rows * c->n_q_heads * c->head_dim * 4);
-  if (w.splits > 1) {
-    w.part_o = take((size_t)w.units * w.splits * 256 * c->head_dim * 4);
-    w.part_ml = take((size_t)w.units * w.splits * 256 * 8);
+  if (w.plan.units) {
+    w.pieces = take((size_t)w.plan.n_pieces * 2 * sizeof(int4));
+    w.joins = take((size_t)w.plan.n_joins * sizeof(int4));
+    w.part_o = take((size_t)2 * sms * kAttnPartRowFloats * c->head_dim * 4);
+    w.part_ml = take((size_t)2 * sms * kAttnPartRowFloats * 8);
   }
   w.total = off;
   return w;
@@ -1887,15 +1893,19 @@ StepTileWs step_tile_layout(const cc_model_cfg *c, const cc_kv_cache *kv, const 
 // the layer; fp16 rows as bf16 pairs, P as pairs too (twice the products).
 cc_status run_step_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows,
                          const KvAttnParams &kp, void *ws, int sms, cudaStream_t st) {
-  const StepTileWs L = step_tile_layout(c, kv, rows, std::min(sms, kStepMaxSms));
+  StepTileWs L = step_tile_layout(c, kv, rows, std::min(sms, kStepMaxSms));
   uint8_t *w = reinterpret_cast<uint8_t *>(ws);
   auto ints = [&](size_t o) { return reinterpret_cast<int32_t *>(w + o); };
   const KvTileRows tr{ints(L.lo), ints(L.hi), ints(L.base)};
+  if (L.plan.units) {
+    L.plan.pieces = reinterpret_cast<int4 *>(w + L.pieces);
+    L.plan.joins = reinterpret_cast<int4 *>(w + L.joins);
+  }
   const int dh = c->head_dim, G = c->n_q_heads / c->n_kv_heads, P = attn_positions_per_unit(G);
   const uint64_t R = (uint64_t)kv->batch * kv->cap;
   {
     TimedScope t(CC_KERNEL_KV_DEQUANT, st);
-    CC_TRY(launch_kv_block_copy(kp, w + L.k, w + L.v, tr, st));
+    CC_TRY(launch_kv_block_copy(kp, w + L.k, w + L.v, tr, L.plan, st));
     if (kp.f16) CC_TRY(launch_kv_split_rows(kp, w + L.pairs, st));
   }
   CUtensorMap tq, tk, tv;
@@ -1935,9 +1945,15 @@ cc_status run_step_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_
   p.key_end = kp.memory_only ? tr.lo : nullptr;
   p.lse = kp.lse;
   p.q_span = rows->max_rows;
-  p.kv_splits = L.splits;
-  p.part_o = reinterpret_cast<float *>(w + L.part_o);
-  p.part_ml = reinterpret_cast<float2 *>(w + L.part_ml);
+  p.kv_splits = 1;
+  if (L.plan.units) {
+    p.pieces = L.plan.pieces;
+    p.joins = L.plan.joins;
+    p.n_pieces = L.plan.n_pieces;
+    p.n_joins = L.plan.n_joins;
+    p.part_o = reinterpret_cast<float *>(w + L.part_o);
+    p.part_ml = reinterpret_cast<float2 *>(w + L.part_ml);
+  }
   CC_TRY(launch_attention(tq, tk, tv, p, st));
   if (!kp.memory_only) CC_TRY(launch_kv_restore_nan(kp, st));
   return CC_OK;

@@ -187,7 +187,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int G = p.group, P = p.P;
   // Key splits (few units): the splits of a unit are consecutive CTAs.
   const int S = p.kv_splits > 1 ? p.kv_splits : 1;
-  const int unit_id = blockIdx.x / S, split = blockIdx.x - unit_id * S;
+  int unit_id = blockIdx.x / S, split = blockIdx.x - unit_id * S;
+  int4 piece = make_int4(0, 0, 0, -1);
+  if (CAUSAL && p.pieces) {
+    piece = p.pieces[blockIdx.x];
+    unit_id = piece.x;
+    if (unit_id < 0) return;
+  }
+  const bool cut = CAUSAL && p.pieces ? piece.w >= 0 : S > 1;   // the unit's rows are partial here
   const UnitInfo u = decode_unit(p, unit_id, CAUSAL);
   if (u.bad) {
     if (threadIdx.x == 0) set_status(p.status, CC_ERR_DEVICE_ARG);
@@ -204,10 +211,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   // this CTA's share of the unit's key tiles (all of them without splits):
   // local iteration `it` handles tile t_hi - it; the tail tile is t_top
   const int t_top = t1;
-  const int it_off = S > 1 ? split * max(ntiles_unit, 0) / S : 0;
-  const int ntiles = S > 1 ? (split + 1) * max(ntiles_unit, 0) / S - it_off : ntiles_unit;
+  int it_off = S > 1 ? split * max(ntiles_unit, 0) / S : 0;
+  int ntiles = S > 1 ? (split + 1) * max(ntiles_unit, 0) / S - it_off : ntiles_unit;
+  if (CAUSAL && p.pieces) {
+    it_off = piece.y;
+    ntiles = min(piece.z, ntiles_unit - piece.y);
+  }
   const int t_hi = t1 - it_off;
-  const size_t part_slot = ((size_t)unit_id * S + split) * 256;
+  const size_t part_slot = (CAUSAL && p.pieces ? (size_t)max(piece.w, 0) : (size_t)unit_id * S + split) * 256;
   // pool row of key tile t (paged) or b*cap + 128 t; a bad page reads zeros
   // (a coordinate past the maps) and is reported
   auto tile_row = [&](int t) -> int {
@@ -220,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     return (int)r;
   };
 
-  if (S > 1 && ntiles <= 0) {   // nothing for this split: an empty partial
+  if (cut && ntiles <= 0) {   // nothing for this split: an empty partial
     for (int R = threadIdx.x; R < 256; R += blockDim.x)
       p.part_ml[part_slot + R] = make_float2(-INFINITY, 0.f);
     return;
@@ -559,7 +570,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     // ---- epilogue: O / l -> bf16 -> out[row_base + pos][g*G + hl][:]
     if (ok) ok = mbar_wait(&o_done[h], 0, abort_flag, p.status);
-    if (ok && S > 1) {   // key split: this CTA's unnormalised O and (max, sum) per row
+    if (ok && cut) {   // key split: this CTA's unnormalised O and (max, sum) per row
       tc_fence_after();
       float *po = p.part_o + (part_slot + R) * DH;
 #pragma unroll 1
@@ -637,15 +648,19 @@ __global__ void __launch_bounds__(kCombineWarps * 32)
   pdl_trigger();
   pdl_wait();
   const int lane = threadIdx.x & 31;
-  const int R = blockIdx.x * kCombineWarps + (threadIdx.x >> 5), unit_id = blockIdx.y;
+  const int R = blockIdx.x * kCombineWarps + (threadIdx.x >> 5);
+  int4 join = make_int4(blockIdx.y, blockIdx.y * p.kv_splits, p.kv_splits, 0);
+  if (CAUSAL && p.joins) join = p.joins[blockIdx.y];
+  const int unit_id = join.x;
+  if (unit_id < 0) return;
   const UnitInfo u = decode_unit(p, unit_id, CAUSAL);
   const int G = p.group;
   if (!u.valid || R >= p.P * G) return;
   const int pos = u.p0 + R / G, hl = R % G;
   if (pos > u.p_last) return;
-  const int S = p.kv_splits;
+  const int S = join.z;
   const float c = p.scale_log2;
-  const size_t base = (size_t)unit_id * S * 256 + R;   // split s's row: base + s * 256
+  const size_t base = (size_t)join.y * 256 + R;   // split s's row: base + s * 256
   float m = -INFINITY, l = 0.f, o[DPL];
   bool nan = false;   // a split's row sum
 #pragma unroll
@@ -730,13 +745,17 @@ cudaError_t launch_dh(const CUtensorMap &q, const CUtensorMap &k, const CUtensor
   AttnParams pp = p;
   pp.streams_per_group = (int)fmax(1.0, fmin((double)n_streams, floor(sqrt(kReuseBytes / per_stream2))));
   const int S = pp.kv_splits > 1 ? pp.kv_splits : 1;
-  if (S > 1 && (!pp.part_o || !pp.part_ml)) return cudaErrorInvalidValue;
-  kern<<<(unsigned)(units * S), kThreads, L::BYTES, stream>>>(q, k, v, pp);
-  if (S > 1) {
+  if ((S > 1 || pp.pieces) && (!pp.part_o || !pp.part_ml)) return cudaErrorInvalidValue;
+  if (pp.pieces) {
+    if (!CAUSAL || S > 1 || !pp.joins) return cudaErrorInvalidValue;
+    pp.streams_per_group = n_streams;
+  }
+  kern<<<(unsigned)(pp.pieces ? pp.n_pieces : units * S), kThreads, L::BYTES, stream>>>(q, k, v, pp);
+  if (S > 1 || (pp.pieces && pp.n_joins > 0)) {
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     if (p.out_lo > 0 || F16) return cudaErrorInvalidValue;   // splits: an append's rows only
-    return launch_pdl(attn_combine_kernel<DH, CAUSAL, SPLIT && CAUSAL>, dim3(256 / kCombineWarps, (unsigned)units),
+    return launch_pdl(attn_combine_kernel<DH, CAUSAL, SPLIT && CAUSAL>, dim3(256 / kCombineWarps, (unsigned)(pp.pieces ? pp.n_joins : units)),
                       dim3(kCombineWarps * 32), 0, stream, pp);
   }
   return cudaGetLastError();

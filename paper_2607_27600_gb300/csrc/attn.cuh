@@ -37,6 +37,12 @@ struct AttnParams {
   float *part_o;            // kv_splits > 1: [unit][split][256 rows][head_dim] unnormalised O
   float2 *part_ml;          // kv_splits > 1: [unit][split][256 rows] (reference max, row sum)
                             // (the decode kernel: kDecMaxG rows instead of 256)
+  // causal: null, or the launch's CTAs, [n_pieces] of (unit, its key tiles left out from
+  // the end, key tiles, partial rows or -1: all of the unit is here; unit -1: nothing to
+  // do), and the units to join, [n_joins] of (unit or -1, first partial, partials).  Units
+  // are numbered as in one group of all streams.  Takes the place of kv_splits.
+  const int4 *pieces, *joins;
+  int n_pieces, n_joins;
   const __nv_bfloat16 *q;   // decode kernel: Q [rows][Hq][dh]
   int dec_ctas;             // decode kernel: CTAs the batch's keys are spread over
   long long q_lo_off;       // decode kernel: > 0: Q is hi + lo, lo at this element offset

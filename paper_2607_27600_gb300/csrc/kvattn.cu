@@ -790,13 +790,158 @@ cudaError_t launch_dh(const KvAttnParams &p, cudaStream_t st) {
 // ---------------------------------------------------------------------------
 // around the tile attention
 // ---------------------------------------------------------------------------
-// 16 elements of K and of V per thread.
-__global__ void __launch_bounds__(256)
+// How the tile attention's CTAs, one per SM at a time, share its units.  Nearly equal
+// units stay whole as far as they fill the SMs evenly; what is left of them, or all where
+// they differ, is left whole, cut into equal pieces while there are SMs for each, or
+// laid end to end as a line that is cut into one share per SM, whichever has the
+// least estimate: key tiles of 1.45 us and what pieces cost besides.  Units in step, on
+// the same key tiles, share them in L2, which only the line gives up.  Longest pieces
+// come first, so that the SMs, which take them in order, end at about one time.
+// Against as many equal pieces of every unit as SMs allow (none past one wave), 32/8
+// heads: 2048 rows after 14336 slots 407 -> 385 us, after 129024 3.10 -> 2.82 ms; eight
+// chunks of 1 to 2000 rows 315 -> 230; three of fp16, 100 to 30000 slots, 802 -> 250; four
+// equal ones 263 -> 269 and 128 rows after 2048 slots 36 -> 39 (the join's launch, the plan).
+constexpr int kPieceCost = 5;    // of a piece besides its key tiles, in tiles (7 us)
+constexpr int kPieceTiles = 4;   // of a piece at least
+constexpr int kJoinCost = 4, kJoinParts = 25;   // the join: its launch, and partial rows a tile
+constexpr int kLineCost = 2 * kPieceCost + 22;  // of the line: two pieces an SM, the join, uneven ends
+constexpr int kPlanThreads = 256, kPlanBins = 64;
+
+__device__ __noinline__ void plan_tiles(const KvAttnParams &p, const KvTilePlan &t) {
+  __shared__ int s_unit[kTilePlanBatch + 1], s_at[kTilePlanBatch + 1];   // a sequence's first, and the end
+  __shared__ int s_seq[kTilePlanBatch], s_count[kTilePlanBatch], s_bin[kPlanBins];
+  __shared__ int s_most, s_pieces, s_parts, s_joins;
+  const int tid = threadIdx.x, batch = p.rows.batch, P = t.P, heads = p.hkv, sms = t.sms;
+  // key tiles of position block i
+  auto tiles_of = [&](int seq, int count, int i) {
+    const int n = p.memory_only ? seq : seq + count, last = seq + min((i + 1) * P, count) - 1;
+    return n > 0 ? min(last, n - 1) / 128 + 1 : 0;
+  };
+  if (tid == 0) s_most = s_pieces = s_parts = s_joins = s_unit[0] = s_at[0] = 0;
+  if (tid < kPlanBins) s_bin[tid] = 0;
+  __syncthreads();
+  if (tid < batch) {
+    const SeqRows s = seq_rows(p.rows, tid, !p.memory_only);
+    s_seq[tid] = s.seq;
+    s_count[tid] = s.count;
+    const int blocks = (s.count + P - 1) / P;
+    int weight = 0;
+    for (int i = 0; i < blocks; ++i) weight += tiles_of(s.seq, s.count, i) + kPieceCost;
+    if (blocks) atomicMax(&s_most, tiles_of(s.seq, s.count, blocks - 1));
+    s_unit[tid + 1] = blocks * heads;
+    s_at[tid + 1] = weight * heads;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int o = 1; o < batch; o *= 2) {   // running sums
+    const int u = tid >= o && tid < batch ? s_unit[tid + 1 - o] : 0, w = tid >= o && tid < batch ? s_at[tid + 1 - o] : 0;
+    __syncthreads();
+    if (tid < batch) {
+      s_unit[tid + 1] += u;
+      s_at[tid + 1] += w;
+    }
+    __syncthreads();
+  }
+  // (more units than fit: sequences share rows, which is reported; no sum is used then)
+  const int units = min(s_unit[batch], t.units), all = s_at[batch], most = s_most;
+  struct Unit {
+    int id, tiles, at;
+  };
+  auto unit_at = [&](int j) {
+    int b = 0;
+#pragma unroll 1
+    for (int o = kTilePlanBatch / 2; o; o /= 2)
+      if (b + o < batch && s_unit[b + o] <= j) b += o;
+    const int seq = s_seq[b], count = s_count[b], blocks = (count + P - 1) / P;
+    const int r = j - s_unit[b], g = r / blocks, i = r - g * blocks;
+    Unit u{(i * batch + b) * heads + g, tiles_of(seq, count, i), s_at[b] + (s_at[b + 1] - s_at[b]) / heads * g};
+#pragma unroll 1
+    for (int k = 0; k < i; ++k) u.at += tiles_of(seq, count, k) + kPieceCost;
+    return u;
+  };
+  const int top = most + kPieceCost;
+  const bool even = 4ll * top * s_unit[batch] <= 5ll * all;   // none a quarter above the mean
+  const int whole = even ? units / sms * sms : 0, rest = units - whole;
+  const int from = rest > 0 ? unit_at(whole).at : all;
+  const int share = max((all - from + sms - 1) / sms, kPieceTiles);
+  // estimates
+  const int equal = even && rest > 0 ? min(sms / rest, most / kPieceTiles) : 1;
+  const int uncut = rest <= sms ? top : share + top / 2;
+  const int in_equal = most / max(equal, 1) + kPieceCost + kJoinCost + rest * equal / kJoinParts;
+  const int in_line = share + share / 16 + kLineCost;
+  const bool sound = rest > 0 && s_unit[batch] <= t.units;
+  const bool line = sound && in_line < uncut && (equal < 2 || in_line < in_equal);
+  const bool equally = sound && !line && equal > 1 && in_equal < uncut;
+  int4 *raw = t.pieces + t.n_pieces;
+  const float per_tile = (kPlanBins - 1) / (float)max(most, 1);
+  auto bin_of = [&](int tiles) { return max(0, kPlanBins - 1 - (int)((float)tiles * per_tile)); };
+#pragma unroll 1
+  for (int j = tid; j < units; j += kPlanThreads) {
+    const Unit u = unit_at(j);
+    auto walk = [&](auto piece) {
+      int last = 0, k = 0;
+      if (j >= whole && line) {
+        const int x = u.at - from;
+        for (int y = (x / share + 1) * share - x - kPieceCost; y <= u.tiles - kPieceTiles; y += share)
+          if (y >= last + kPieceTiles) {
+            piece(k++, last, y - last);
+            last = y;
+          }
+      } else if (j >= whole && equally) {
+        for (int to = 1; to < equal; ++to) {
+          const int y = (int)((long long)u.tiles * to / equal);
+          if (y - last >= kPieceTiles && u.tiles - y >= kPieceTiles) {
+            piece(k++, last, y - last);
+            last = y;
+          }
+        }
+      }
+      piece(k++, last, u.tiles - last);
+      return k;
+    };
+    const int n = walk([](int, int, int) {});
+    const int at = atomicAdd(&s_pieces, n), part = n > 1 ? atomicAdd(&s_parts, n) : -1;
+    if (at + n > t.n_pieces || part + n > 2 * sms) continue;   // (never: there are fewer cuts than SMs)
+    walk([&](int k, int off, int tiles) {
+      raw[at + k] = make_int4(u.id, off, tiles, n > 1 ? part + k : -1);
+      atomicAdd(&s_bin[bin_of(tiles)], 1);
+    });
+    if (n > 1) {
+      const int to = atomicAdd(&s_joins, 1);
+      if (to < t.n_joins) t.joins[to] = make_int4(u.id, part, n, 0);
+    }
+  }
+  __syncthreads();
+  const int pieces = min(s_pieces, t.n_pieces);
+  for (int i = s_joins + tid; i < t.n_joins; i += kPlanThreads) t.joins[i] = make_int4(-1, 0, 0, 0);
+  for (int i = pieces + tid; i < t.n_pieces; i += kPlanThreads) t.pieces[i] = make_int4(-1, 0, 0, -1);
+  int before = 0;   // pieces of longer bins
+  if (tid < kPlanBins)
+    for (int i = 0; i < tid; ++i) before += s_bin[i];
+  __syncthreads();
+  if (tid < kPlanBins) s_bin[tid] = before;
+  __syncthreads();
+  for (int i = tid; i < pieces; i += kPlanThreads) {
+    const int4 x = raw[i];
+    t.pieces[atomicAdd(&s_bin[bin_of(x.z)], 1)] = x;
+  }
+}
+static_assert(kTilePlanBatch <= kPlanThreads && kPlanBins <= kPlanThreads, "a thread a sequence, and a bin");
+
+// 16 elements of K and of V per thread (four, all loads ahead, changed no time by more
+// than 2 %).  Registers for eight CTAs per SM, which the plan alone exceeds: with five
+// the copy of 130000 slots took 13 us more.
+__global__ void __launch_bounds__(256, 8)
     kv_block_copy_kernel(const __grid_constant__ KvAttnParams p, uint16_t *ko, uint16_t *vo, KvTileRows t,
-                         int per_seq) {
+                         const __grid_constant__ KvTilePlan plan, int per_seq) {
+  int block = blockIdx.x;
+  if (plan.pieces && block-- == 0) {
+    plan_tiles(p, plan);
+    return;
+  }
   const int dh = p.head_dim, chunks = p.hkv * dh / 16, cap = p.rows.cap;
-  const int b = blockIdx.x / per_seq;
-  const uint32_t idx = (uint32_t)(blockIdx.x - b * per_seq) * 256u + threadIdx.x;   // in the sequence
+  const int b = block / per_seq;
+  const uint32_t idx = (uint32_t)(block - b * per_seq) * 256u + threadIdx.x;   // in the sequence
   const int i = (int)(idx / chunks), c = (int)(idx - (uint32_t)i * chunks);
   const long long row = (long long)b * cap + i;
   const SeqRows s = seq_rows(p.rows, b, !p.memory_only);
@@ -919,12 +1064,13 @@ cudaError_t launch_kv_attn(const KvAttnParams &p, cudaStream_t st) {
 }
 
 cudaError_t launch_kv_block_copy(const KvAttnParams &p, void *ko, void *vo, const KvTileRows &t,
-                                 cudaStream_t st) {
+                                 const KvTilePlan &plan, cudaStream_t st) {
   const long long n = (long long)p.rows.cap * (p.hkv * p.head_dim / 16), per_seq = (n + 255) / 256;
-  const long long blocks = per_seq * p.rows.batch;
+  const long long blocks = per_seq * p.rows.batch + (plan.pieces ? 1 : 0);
   if (blocks > 0x7FFFFFFFll || n > 0xFFFFFF00ll) return cudaErrorInvalidValue;
+  if (plan.pieces && p.rows.batch > kTilePlanBatch) return cudaErrorInvalidValue;
   kv_block_copy_kernel<<<(unsigned)blocks, 256, 0, st>>>(
-      p, reinterpret_cast<uint16_t *>(ko), reinterpret_cast<uint16_t *>(vo), t, (int)per_seq);
+      p, reinterpret_cast<uint16_t *>(ko), reinterpret_cast<uint16_t *>(vo), t, plan, (int)per_seq);
   return cudaGetLastError();
 }
 

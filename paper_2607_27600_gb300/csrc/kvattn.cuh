@@ -49,8 +49,19 @@ cudaError_t launch_kv_attn(const KvAttnParams &p, cudaStream_t st);
 struct KvTileRows {
   int32_t *lo, *hi, *base;   // device [batch]
 };
+//   (and, meanwhile, how the SMs share the tile attention's work: AttnParams' pieces and
+//   joins, where they are asked for)
+struct KvTilePlan {
+  int4 *pieces;     // device [n_pieces], then as many again of scratch; or null
+  int4 *joins;      // device [n_joins]
+  int n_pieces, n_joins;
+  int units;        // with rows, at most
+  int sms;          // partial rows of 2 * sms pieces at most
+  int P;            // positions of a unit
+};
+constexpr int kTilePlanBatch = 256;   // sequences of a plan at most
 cudaError_t launch_kv_block_copy(const KvAttnParams &p, void *ko, void *vo, const KvTileRows &t,
-                                 cudaStream_t st);
+                                 const KvTilePlan &plan, cudaStream_t st);
 //   ... and put into the rows that do, afterwards;
 cudaError_t launch_kv_restore_nan(const KvAttnParams &p, cudaStream_t st);
 //   fp16 rows as bf16 pairs (exact): [n_rows][hi: hq * head_dim | lo: hq * head_dim].
