@@ -472,29 +472,38 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
       const float kf = __uint_as_float(ek << 23);
       const float lv = (float)((int)ev - 127);
       const bool mask = slot + 16 > seen_lo;   // uniform over the warp
+      float qk[NT][2];   // what makes them scores: 1 where they are masked, and scores already
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) qk[t][c] = qf[t][c] * kf;
+      if (mask) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            sc[t][k] = slot + row_of(n8) + 8 * (k >> 1) >= seen[t][k & 1] ? -INFINITY : sc[t][k] * qk[t][k & 1];
+          qk[t][0] = qk[t][1] = 1.f;
+        }
+      }
+      const float room = kTop - lv;
       bool over = false;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          sc[t][k] *= qf[t][k & 1] * kf;
-          if (mask && slot + row_of(n8) + 8 * (k >> 1) >= seen[t][k & 1]) sc[t][k] = -INFINITY;
-        }
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int c = 0; c < 2; ++c)
-          over |= fmaxf(sc[t][c], sc[t][2 + c]) - m[t][c] > fminf(kSumLimit, kTop - (lv + m[t][c] - mv[t][c]));
-      }
+          over |= fmaxf(sc[t][c], sc[t][2 + c]) * qk[t][c] > fminf(m[t][c] + kSumLimit, mv[t][c] + room);
       if (__any_sync(0xFFFFFFFFu, over)) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            float x = fmaxf(sc[t][c], sc[t][2 + c]);
+            float x = fmaxf(sc[t][c], sc[t][2 + c]) * qk[t][c];
             x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 4));
             x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 8));
             x = ceilf(fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 16)));
             const float m1 = fmaxf(m[t][c], x), mv1 = fmaxf(mv[t][c], x + lv - kHead);
-            l[t][c] *= ex2(m[t][c] - m1);
+            l[t][c] = m1 < INFINITY ? l[t][c] * ex2(m[t][c] - m1) : NAN;   // (a score past fp32)
             const float f = ex2(mv[t][c] - mv1);
             m[t][c] = m1;
             mv[t][c] = mv1;
@@ -513,7 +522,7 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
         for (int c = 0; c < 2; ++c) {
           // (finite: a key of probability 0 may have any scale)
           const float f = ex2(fminf(lv + m[t][c] - mv[t][c], 126.f));
-          const float p0 = ex2(sc[t][c] - m[t][c]), p1 = ex2(sc[t][2 + c] - m[t][c]);
+          const float p0 = ex2(fmaf(sc[t][c], qk[t][c], -m[t][c])), p1 = ex2(fmaf(sc[t][2 + c], qk[t][c], -m[t][c]));
           l[t][c] += p0 + p1;
           y[c] = p0 * f;
           y[2 + c] = p1 * f;
