@@ -28,9 +28,9 @@
 // order (row_of) in which, with the rows' pieces swizzled, neither product's reads
 // meet in a bank.
 //
-// 64 ragged sequences of 1500 to 32767 slots, a row each, 32/8 heads: 2.25 GB in 339 us
-// (6.6 TB/s); one of 8192 slots, 28/4 heads: 11.3 us, of which the stream is 1.3.  Units
-// of 24 rows are bound by issue: 16 sequences' 5 rows of fp16, 153 MB in 59 us.
+// 64 ragged sequences of 1500 to 32767 slots, a row each, 32/8 heads: 2.25 GB in 337 us
+// (6.7 TB/s); one of 8192 slots, 28/4 heads: 11.3 us, of which the stream is 1.3.  Units
+// of 24 rows are bound by issue: 16 sequences' 5 rows of fp16, 153 MB in 60 us.
 #include "kvattn.cuh"
 
 #include <algorithm>
@@ -43,7 +43,7 @@ namespace {
 constexpr int kWarps = 4;          // of a CTA, each every fourth 16 keys of a tile
 constexpr int kTile = 16 * kWarps; // keys of a tile
 constexpr int kMinTiles = 4;       // of a share at least
-constexpr int kGroups = 8, kJoin = 8;   // of the join
+constexpr int kGroups = 8;         // of the join
 // What a unit costs besides its tiles (its queries, the first loads' latency, its
 // rows at the end: 5 to 6 us where a tile takes 1), in tiles.
 constexpr int kUnitTiles = 5;
@@ -692,11 +692,14 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
 // Joins the shares of a unit that starts in share c0 and goes on past it, as that
 // share's CTA wrote it down, in share order.  SPREAD (few units, of many shares): a CTA
 // per unit and row, its kGroups groups of DH / 2 threads each take every kGroups-th
-// share; else CTAs per share, a group per row.  A group loads eight shares at a time.
+// share; else CTAs per share, a group per row.  A group loads eight shares at a time; in
+// the second form, where a unit has a few and many CTAs find none, four, so that two
+// CTAs fit an SM (16 sequences' 5 rows: fp16 62.1 -> 60.1 us, bf16 57.0 -> 55.0; two at a
+// time and four CTAs: the same, and single rows 1 us slower).
 template <typename T, int DH, int NT, bool SPREAD>
-__global__ void __launch_bounds__(kGroups * DH / 2)
+__global__ void __launch_bounds__(kGroups * DH / 2, SPREAD ? 1 : 1024 / (kGroups * DH / 2))
     kv_combine_kernel(const __grid_constant__ KvAttnParams p) {
-  constexpr int ROWS = 8 * NT;
+  constexpr int ROWS = 8 * NT, kJoin = SPREAD ? 8 : 4;
   __shared__ float4 part[SPREAD ? kGroups : 1][DH / 2];   // m, mv and the two sums
   __shared__ float part_l[kGroups];
   const int group = threadIdx.x / (DH / 2), d = (threadIdx.x - group * (DH / 2)) * 2;
@@ -712,8 +715,8 @@ __global__ void __launch_bounds__(kGroups * DH / 2)
   const int4 u = p.cut[blockIdx.x];   // first and last share; sequence and group of rows
   const int c0 = u.x, c1 = u.y;
   if (c1 <= c0 || R >= ROWS) return;
+  // (the row is needed last: its lookup runs beside the loads)
   if (!SPREAD) r = row_at(p, seq_rows(p.rows, u.z, !p.memory_only), g, u.w * ROWS + R);
-  if (!r.live) return;
   // share c0 holds the unit's start, those after it start inside the unit
   auto slot = [&](int c) { return (2ll * ((long long)c * p.hkv + g) + (c == c0 ? 1 : 0)) * ROWS + R; };
   constexpr int STEP = SPREAD ? kGroups : 1;
@@ -752,6 +755,7 @@ __global__ void __launch_bounds__(kGroups * DH / 2)
       join(x.x, x.y, part_l[k], x.z, x.w);
     }
   }
+  if (!r.live) return;
   const OutScale k = out_scale(m, mv, l);
   *reinterpret_cast<uint32_t *>(reinterpret_cast<T *>(p.out) + r.row * p.out_ld + (long long)r.head * DH + d) =
       k.b == 0.f ? 0u : pack2<T>(o0 * k.a * k.b, o1 * k.a * k.b);
