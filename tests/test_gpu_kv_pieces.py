@@ -67,3 +67,39 @@ def test_pieces(hq, hkv, dh, layout, cap, lens, counts, dtype, memory):
     assert torch.equal(lse.isinf(), want_lse.isinf())
     f = want_lse.isfinite()
     assert ((lse - want_lse).abs()[f] <= 2.0 ** -12 + 2.0 ** -22 * want_lse[f].abs()).all()
+
+
+def test_a_captured_chunk_is_planned_again_at_each_replay():
+    import paper_2607_27600_gb300 as pkg
+    from paper_2607_27600_gb300 import cc
+    rng = np.random.default_rng(3)
+    s, cap = shape(8, 2, 64), 6144
+    codes, exps = {}, {}
+    for x in "kv":
+        codes[x], exps[x] = quantised(rng, 2, cap, 2, 64, 64)
+    c, rows = DeviceCache(pkg, codes, exps, [0, 0], "slot"), device_rows(pkg, [300, 100])
+    dq, = columns([rng.standard_normal((400, 8, 64))], torch.bfloat16)
+    out = torch.empty(400, 8, 64, dtype=torch.bfloat16, device="cuda")
+    ws = cc.alloc_workspace(cc.cc_kv_attention_workspace_size(s, c.cache, rows))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    lens = ([0, 0], [5500, 9], [3, 6000], [4000, 4000])
+    want = []
+    for n in lens:
+        with torch.cuda.stream(side):
+            c.d["seq_len"].copy_(torch.tensor(n, dtype=torch.int32))
+        cc.cc_kv_attention(s, c.cache, 0, rows, dq, out, ws, stream=side)
+        with torch.cuda.stream(side):
+            want.append(out.clone())
+    cc.cc_graph_begin(side)
+    cc.cc_kv_attention(s, c.cache, 0, rows, dq, out, ws, stream=side)
+    graph = cc.cc_graph_end(side)
+    for n, w in zip(lens, want):
+        with torch.cuda.stream(side):
+            c.d["seq_len"].copy_(torch.tensor(n, dtype=torch.int32))
+            out.zero_()
+        cc.cc_graph_launch(graph, side)
+        with torch.cuda.stream(side):
+            assert torch.equal(out, w)
+    assert cc.cc_get_status(side) == cc.CC_OK
+    cc.cc_graph_destroy(graph)
