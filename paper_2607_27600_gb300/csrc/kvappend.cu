@@ -17,7 +17,7 @@
 // copies what it will read a few heads (rows, for the bound) ahead into slots of its
 // own (cp.async, no barrier): loops unrolled over loads instead held as much in
 // flight but half of the time nothing, and their code was a single token's latency.
-// Four chunks of 4096 tokens, 32/8 heads of 128, bf16: 369 MB in 74.8 us (4.9 TB/s); 2957
+// Four chunks of 4096 tokens, 32/8 heads of 128, bf16: 369 MB in 69 us (5.3 TB/s); 2957
 // tokens of five ragged sequences, 28/4 heads, fp32: 100 MB in 16.6 us (6.0 TB/s); a
 // token each of 64 sequences: 6.6 us, latency (launch, bound, rows one after another).
 #include "kvappend.cuh"
@@ -31,7 +31,12 @@ namespace cc {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSplitCtas = 2;   // CTAs per SM to split the heads for
+// CTAs per SM to split the heads for, and where there are heads for so many (three are
+// resident: the last wave is a smaller part; four chunks of 4096 tokens, 32/8 heads, in
+// blocks of 128, 64 and 32 slots: 76.9 -> 71.1, 77.2 -> 70.8, 72.5 -> 67.6 us).  Short of
+// that one wave is better: 28/4 heads, three shares 58, four 63.
+constexpr int kSplitCtas = 2;
+constexpr int kManyCtas = 6;
 constexpr int kLeastExp = 10, kMostExp = 247, kUnitExp = 127;   // scale exponents written
 
 // The 8 elements of half a head that a lane holds: pieces of 16 bytes which lie side
@@ -465,7 +470,8 @@ cudaError_t launch_append_as(const KvAppendParams &p, int sms, cudaStream_t st) 
   auto kern = kv_append_kernel<T, DH>;
   // a unit's heads over several CTAs until they fill the SMs
   const long long busy = std::min(units, (long long)p.rows.n_rows / p.block + p.rows.batch);   // (about)
-  const int split = (int)std::min<long long>(p.hkv, std::max<long long>(1, (kSplitCtas * sms + busy - 1) / busy));
+  const long long ctas = (long long)sms * (busy * p.hkv >= kManyCtas * sms ? kManyCtas : kSplitCtas);
+  const int split = (int)std::min<long long>(p.hkv, std::max<long long>(1, (ctas + busy - 1) / busy));
   const size_t smem = Ahead<T, DH>::BYTES + kTable * sizeof(float2) + 2 * ((size_t)p.hkv / split + 1) * sizeof(float);
   static std::atomic<size_t> allowed[64] = {};   // (the few floats grow with hkv)
   int dev = 0;
