@@ -473,13 +473,16 @@ cudaError_t launch_append_as(const KvAppendParams &p, int sms, cudaStream_t st) 
   const long long ctas = (long long)sms * (busy * p.hkv >= kManyCtas * sms ? kManyCtas : kSplitCtas);
   const int split = (int)std::min<long long>(p.hkv, std::max<long long>(1, (ctas + busy - 1) / busy));
   const size_t smem = Ahead<T, DH>::BYTES + kTable * sizeof(float2) + 2 * ((size_t)p.hkv / split + 1) * sizeof(float);
-  static std::atomic<size_t> allowed[64] = {};   // (the few floats grow with hkv)
+  // one limit for every head count: a call must not lower what another thread's needs
+  constexpr size_t kMostSmem = 200 * 1024;
+  if (smem > kMostSmem) return cudaErrorInvalidValue;
+  static std::atomic<bool> attr_set[64] = {};
   int dev = 0;
   cudaGetDevice(&dev);
-  if (dev >= 64 || allowed[dev] < smem) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (dev >= 64 || !attr_set[dev]) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem);
     if (e != cudaSuccess) return e;
-    if (dev < 64) allowed[dev] = smem;
+    if (dev < 64) attr_set[dev] = true;
   }
   kern<<<dim3((unsigned)units, (unsigned)split), kThreads, smem, st>>>(p);
   return cudaGetLastError();
