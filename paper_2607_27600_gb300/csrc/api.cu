@@ -1943,6 +1943,7 @@ cc_status run_step_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_
   p.row_lo = tr.lo;
   p.pbase = tr.base;
   p.key_end = kp.memory_only ? tr.lo : nullptr;
+  p.none_zero = 1;
   p.lse = kp.lse;
   p.q_span = rows->max_rows;
   p.kv_splits = 1;

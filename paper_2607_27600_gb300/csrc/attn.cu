@@ -589,6 +589,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc_fence_after();
       const bool store = row_used && pos <= p_last;
       const float inv = l > 0.f ? p.v_scale / l : 0.f;   // V scale: e4m3 cache (else 1)
+      // (where P is NaN, O is too: such a row is not 0 by a factor of 0)
+      const bool zero = CAUSAL && p.none_zero && !(l > 0.f);
       if (CAUSAL && p.lse && store)
         p.lse[(row_base + pos) * p.n_q_heads + g * G + hl] = row_lse(m_used, l, sl2);
       __nv_bfloat16 *dst =
@@ -601,8 +603,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t pk[16];
 #pragma unroll
         for (int k = 0; k < 32; k += 2)
-          pk[k / 2] = OUT_F16 ? pack_f16x2(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv)
-                              : pack_bf16x2(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv);
+          pk[k / 2] = zero      ? 0u
+                      : OUT_F16 ? pack_f16x2(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv)
+                                : pack_bf16x2(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv);
         if (store) {
           uint4 *d = reinterpret_cast<uint4 *>(dst + c);
 #pragma unroll

@@ -31,6 +31,8 @@ struct AttnParams {
                             // pbase[b] + i - row_lo[b]
   const int32_t *key_end;   // causal: null, or device [batch]: every row sees the slots [0, key_end[b])
                             // and no others (its own slot, past them, only names its row)
+  int none_zero;            // causal: a row with a NaN or infinite score is 0 in whole units too (as a
+                            // join of a unit's parts stores it)
   float *lse;               // causal: null, or [row][n_q_heads]: ln of the sum of e^score
   int q_span;               // query slots per sequence at most (cap, or the chunk size)
   int kv_splits;            // > 1: each unit's key tiles split over kv_splits CTAs (few units)
