@@ -1849,11 +1849,11 @@ bool step_on_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *
 }
 
 // Workspace of the tile attention: the layer as bf16, the sequences' rows, fp16
-// queries as pairs, and how the SMs share the units (kvattn.cu) with the partial rows.
-// The plan's single CTA takes up to kPlanUnits units; more are waves enough.
+// queries as pairs, the rows' lse where the caller wants none, and how the SMs share the
+// units (kvattn.cu) with the partial rows.  The plan's single CTA takes up to kPlanUnits units; more are waves enough.
 constexpr int kPlanUnits = 1024;
 struct StepTileWs {
-  size_t k, v, lo, hi, base, pairs, pieces, joins, part_o, part_ml, total;
+  size_t k, v, lo, hi, base, pairs, lse, pieces, joins, part_o, part_ml, total;
   KvTilePlan plan;   // (units = 0: none)
 };
 StepTileWs step_tile_layout(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows, int sms) {
@@ -1879,6 +1879,7 @@ StepTileWs step_tile_layout(const cc_model_cfg *c, const cc_kv_cache *kv, const 
   w.hi = take((size_t)kv->batch * 4);
   w.base = take((size_t)kv->batch * 4);
   w.pairs = take((size_t)rows->n_rows * c->n_q_heads * c->head_dim * 4);
+  w.lse = take((size_t)rows->n_rows * c->n_q_heads * 4);
   if (w.plan.units) {
     w.pieces = take((size_t)w.plan.n_pieces * 2 * sizeof(int4));
     w.joins = take((size_t)w.plan.n_joins * sizeof(int4));
@@ -1892,7 +1893,7 @@ StepTileWs step_tile_layout(const cc_model_cfg *c, const cc_kv_cache *kv, const 
 // The rows' attention as tiles of 256 query rows (attn.cu) over a bf16 copy of
 // the layer; fp16 rows as bf16 pairs, P as pairs too (twice the products).
 cc_status run_step_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows,
-                         const KvAttnParams &kp, void *ws, int sms, cudaStream_t st) {
+                         KvAttnParams kp, void *ws, int sms, cudaStream_t st) {
   StepTileWs L = step_tile_layout(c, kv, rows, std::min(sms, kStepMaxSms));
   uint8_t *w = reinterpret_cast<uint8_t *>(ws);
   auto ints = [&](size_t o) { return reinterpret_cast<int32_t *>(w + o); };
@@ -1901,6 +1902,7 @@ cc_status run_step_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_
     L.plan.pieces = reinterpret_cast<int4 *>(w + L.pieces);
     L.plan.joins = reinterpret_cast<int4 *>(w + L.joins);
   }
+  if (!kp.lse) kp.lse = reinterpret_cast<float *>(w + L.lse);   // (the restored NaN values need it)
   const int dh = c->head_dim, G = c->n_q_heads / c->n_kv_heads, P = attn_positions_per_unit(G);
   const uint64_t R = (uint64_t)kv->batch * kv->cap;
   {

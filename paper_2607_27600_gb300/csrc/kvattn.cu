@@ -996,7 +996,8 @@ __global__ void __launch_bounds__(256, 8)
 }
 
 // 16 values of a new token and KV head per thread: where they hold NaN codes, the
-// outputs of the token's own and the later rows of its sequence get NaN.
+// outputs of the token's own and the later rows of its sequence get NaN, but for rows
+// that are 0 (a score that is no number: their lse is none either).
 template <typename T>
 __global__ void __launch_bounds__(256) kv_restore_nan_kernel(const __grid_constant__ KvAttnParams p) {
   const int dh = p.head_dim, chunks = p.hkv * dh / 16, G = p.hq / p.hkv;
@@ -1020,7 +1021,8 @@ __global__ void __launch_bounds__(256) kv_restore_nan_kernel(const __grid_consta
     if ((p.v[vec * dh + e + d] & 0x7F) != 0x7F) continue;
     for (int i = r; i < s.r0 + s.count; ++i)
       for (int h = 0; h < G; ++h)
-        reinterpret_cast<T *>(p.out)[i * p.out_ld + (long long)(g * G + h) * dh + e + d] = nan;
+        if (fabsf(p.lse[(long long)i * p.hq + g * G + h]) < INFINITY)
+          reinterpret_cast<T *>(p.out)[i * p.out_ld + (long long)(g * G + h) * dh + e + d] = nan;
   }
 }
 

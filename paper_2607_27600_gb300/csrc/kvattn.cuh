@@ -62,7 +62,7 @@ struct KvTilePlan {
 constexpr int kTilePlanBatch = 256;   // sequences of a plan at most
 cudaError_t launch_kv_block_copy(const KvAttnParams &p, void *ko, void *vo, const KvTileRows &t,
                                  const KvTilePlan &plan, cudaStream_t st);
-//   ... and put into the rows that do, afterwards;
+//   ... and put into the rows that do, afterwards (p.lse: of every row, by the tile attention);
 cudaError_t launch_kv_restore_nan(const KvAttnParams &p, cudaStream_t st);
 //   fp16 rows as bf16 pairs (exact): [n_rows][hi: hq * head_dim | lo: hq * head_dim].
 cudaError_t launch_kv_split_rows(const KvAttnParams &p, void *pairs, cudaStream_t st);

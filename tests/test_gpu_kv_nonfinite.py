@@ -127,3 +127,20 @@ def test_rows_that_see_a_bad_page(size, dtype):
     got, _, want = c.run(status=cc.CC_ERR_DEVICE_ARG, pages=[(0, 1)])
     assert (got[:c.start[1]] == 0).all()
     c.check(got, None, want, slice(c.start[1], None))
+
+
+@pytest.mark.parametrize("lse", [True, False])
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("size", list(SIZES))
+def test_a_token_that_is_no_number(size, dtype, lse):
+    """A new token whose keys, values and query are all NaN, as a diverged one's are: its own and
+    the later rows are 0, not NaN; a NaN among the values alone is NaN in its column."""
+    c = Case(*SIZES[size], dtype)
+    n, m = c.lens[0], c.start[1]
+    for x in "kv":
+        c.codes[x][0, n + m - 30] = 0x7F
+    c.q[m - 30] = np.nan
+    c.codes["v"][0, n + 11, 1, 6] = 0xFF
+    got, ls, want = c.run(lse=lse)
+    assert want[0][11:m - 30, 4:, 6].isnan().all() and (want[0][m - 30:m] == 0).all()
+    c.check(got, ls, want)
