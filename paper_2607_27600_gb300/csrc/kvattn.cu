@@ -1002,15 +1002,25 @@ template <typename T>
 __global__ void __launch_bounds__(256) kv_restore_nan_kernel(const __grid_constant__ KvAttnParams p) {
   const int dh = p.head_dim, chunks = p.hkv * dh / 16, G = p.hq / p.hkv;
   const long long idx = (long long)blockIdx.x * 256 + threadIdx.x;
-  const int r = (int)(idx / chunks), c = (int)(idx - (long long)r * chunks);
-  if (r >= p.rows.n_rows) return;
-  int b = 0;   // the last sequence that starts at or before row r
-  for (int hi = p.rows.batch - 1; b < hi;) {
-    const int mid = (b + hi + 1) >> 1;
-    if (p.rows.row_start[mid] <= r) b = mid; else hi = mid - 1;
-  }
+  const int r = (int)(idx / chunks), c = (int)(idx - (long long)r * chunks), lane = threadIdx.x & 31;
+  // Whose row it is: every sequence is looked at, a lane each, for the few rows of the warp in
+  // turn (where some are bad, row_start is not in order).
+  int b = -1;
+  const int last = min(__shfl_sync(0xFFFFFFFFu, r, 31), p.rows.n_rows - 1);
+  for (int row = __shfl_sync(0xFFFFFFFFu, r, 0); row <= last; ++row)
+    for (int b0 = 0; b0 < p.rows.batch; b0 += 32) {
+      bool in = false;
+      if (b0 + lane < p.rows.batch) {
+        const SeqRows s = seq_rows(p.rows, b0 + lane, true);
+        in = row >= s.r0 && row < s.r0 + s.count;
+      }
+      const unsigned hit = __ballot_sync(0xFFFFFFFFu, in);
+      if (!hit) continue;
+      if (row == r) b = b0 + __ffs(hit) - 1;
+      break;
+    }
+  if (b < 0) return;
   const SeqRows s = seq_rows(p.rows, b, true);
-  if (r < s.r0 || r >= s.r0 + s.count) return;
   const int g = c * 16 / dh, e = c * 16 - g * dh;
   const long long vec = kv_vec(p.pg, p.rows.cap, b, g, s.seq + r - s.r0);
   if (vec < 0) return;

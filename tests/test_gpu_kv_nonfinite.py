@@ -144,3 +144,15 @@ def test_a_token_that_is_no_number(size, dtype, lse):
     got, ls, want = c.run(lse=lse)
     assert want[0][11:m - 30, 4:, 6].isnan().all() and (want[0][m - 30:m] == 0).all()
     c.check(got, ls, want)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_not_a_number_beside_rows_out_of_order(dtype):
+    """Bad sequences (too many rows, and an end before the start) are reported; a NaN value of a
+    good one, whose rows lie before the end of a bad one's, is still NaN in its column."""
+    from paper_2607_27600_gb300 import cc
+    c = Case(8, 2, 64, "slot", 512, [100, 100, 100], [0, 290, 150, 300], 150, dtype)
+    c.codes["v"][2, 100 + 40, 0, 21] = 0x7F
+    got, ls, want = c.run(ok=[False, False, True], status=cc.CC_ERR_DEVICE_ARG)
+    assert want[0][190:, :4, 21].isnan().all()
+    c.check(got, ls, want, slice(150, 300))
