@@ -624,6 +624,16 @@ class Rows:
                          _dev_ptr(pos, "pos"))
 
 
+def _step_rows(cache, rows):
+    """The rows' struct; row_start has an entry more than the cache has sequences (or
+    further ones, which are not read)."""
+    start = rows.row_start
+    if start is not None and start.numel() <= cache.c.batch:
+        raise ValueError(f"row_start must have {cache.c.batch + 1} elements (the cache's sequences and one), "
+                         f"not {start.numel()}")
+    return rows.c
+
+
 def _row_ptr(t, name, n_rows, width, dtype):
     """(pointer, elements between rows) of a CUDA tensor [n_rows, heads, head_dim] (or
     [n_rows, heads * head_dim]) whose rows are contiguous."""
@@ -669,16 +679,18 @@ def cc_kv_append(cfg, cache: Cache, layer: int, rows: Rows, k, v, q=None, q_out=
     writes keys and values into layer `layer` of the cache, after each
     sequence's seq_len slots.  k, v: [n_rows, Hkv, dh], q, q_out: [n_rows, Hq, dh],
     of one type, any 16-byte aligned pitch."""
-    c, n = _cfg(cfg), rows.c.n_rows
+    c, r = _cfg(cfg), _step_rows(cache, rows)
+    n = r.n_rows
     kv, hq = c.n_kv_heads * c.head_dim, c.n_q_heads * c.head_dim
     args = (*_row_ptr(k, "k", n, kv, k.dtype), *_row_ptr(v, "v", n, kv, k.dtype),
             *_row_ptr(q, "q", n, hq, k.dtype), *_row_ptr(q_out, "q_out", n, hq, k.dtype))
-    _check(load_library().cc_kv_append(c, cache.c, layer, rows.c, _dtype(k, "k"), 1 if rotate else 0,
+    _check(load_library().cc_kv_append(c, cache.c, layer, r, _dtype(k, "k"), 1 if rotate else 0,
                                        *args, _stream(stream)), "cc_kv_append")
 
 
 def cc_kv_attention_workspace_size(cfg, cache: Cache, rows: Rows) -> int:
-    return int(load_library().cc_kv_attention_workspace_size(_cfg(cfg), cache.c, rows.c))
+    return int(load_library().cc_kv_attention_workspace_size(_cfg(cfg), cache.c,
+                                                             _step_rows(cache, rows)))
 
 
 def cc_kv_attention(cfg, cache: Cache, layer: int, rows: Rows, q, out, ws, lse=None,
@@ -686,10 +698,10 @@ def cc_kv_attention(cfg, cache: Cache, layer: int, rows: Rows, q, out, ws, lse=N
     """Attention of the rows (q [n_rows, Hq, dh], bf16 or fp16) over layer `layer`
     of a block-format cache into out; lse: fp32 [n_rows, Hq] or None.  The rows
     see the slots up to their own, or with memory_only the seq_len slots alone."""
-    c, n = _cfg(cfg), rows.c.n_rows
-    hq = c.n_q_heads * c.head_dim
+    c, r = _cfg(cfg), _step_rows(cache, rows)
+    n, hq = r.n_rows, c.n_q_heads * c.head_dim
     _check(load_library().cc_kv_attention(
-        c, cache.c, layer, rows.c, _dtype(q, "q"), 1 if memory_only else 0,
+        c, cache.c, layer, r, _dtype(q, "q"), 1 if memory_only else 0,
         *_row_ptr(q, "q", n, hq, q.dtype), *_row_ptr(out, "out", n, hq, q.dtype),
         _vec_ptr(lse, "lse", n * c.n_q_heads, torch.float32), _dev_ptr(ws, "ws"),
         ws.numel() * ws.element_size(), _stream(stream)), "cc_kv_attention")
@@ -698,8 +710,8 @@ def cc_kv_attention(cfg, cache: Cache, layer: int, rows: Rows, q, out, ws, lse=N
 def cc_kv_advance(cache: Cache, rows: Rows, tokens=None, stream=None):
     """Ends a step: positions and tokens (int32 [n_rows] or None) of the rows
     into the cache, and seq_len grows."""
-    _check(load_library().cc_kv_advance(cache.c, rows.c,
-                                        _vec_ptr(tokens, "tokens", rows.c.n_rows, torch.int32),
+    r = _step_rows(cache, rows)
+    _check(load_library().cc_kv_advance(cache.c, r, _vec_ptr(tokens, "tokens", r.n_rows, torch.int32),
                                         _stream(stream)), "cc_kv_advance")
 
 
