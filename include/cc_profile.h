@@ -36,9 +36,10 @@ typedef enum {
   CC_KERNEL_GEMM_QKV = 16,   /* fused q/k/v projections (+ RoPE) of the append    */
   CC_KERNEL_KEYATTN = 17,    /* comparison scorers: attention received per key    */
   CC_KERNEL_KV_DEQUANT = 18, /* a layer's K/V copied for the tile attention: e4m3
-                                as bf16 or fp16, bf16 as fp16 (CC_SCORE_F16)        */
+                                as bf16 or fp16, bf16 as fp16 (CC_SCORE_F16); in
+                                cc_kv_attention with fp16 rows as pairs             */
   CC_KERNEL_KV_APPEND = 19,  /* cc_kv_append, cc_kv_advance                       */
-  CC_KERNEL_KV_ATTENTION = 20,/* cc_kv_attention                                  */
+  CC_KERNEL_KV_ATTENTION = 20,/* cc_kv_attention but for a chunk's copy            */
   CC_KERNEL_TOKEN_LOGPROB = 21,/* cc_token_logprobs                               */
   CC_KERNEL_COUNT = 22
 } cc_kernel_kind;

@@ -1957,6 +1957,7 @@ cc_status run_step_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_
     p.part_o = reinterpret_cast<float *>(w + L.part_o);
     p.part_ml = reinterpret_cast<float2 *>(w + L.part_ml);
   }
+  TimedScope t(CC_KERNEL_KV_ATTENTION, st);   // (apart from the copy's)
   CC_TRY(launch_attention(tq, tk, tv, p, st));
   if (!kp.memory_only) CC_TRY(launch_kv_restore_nan(kp, st));
   return CC_OK;
@@ -2066,7 +2067,6 @@ cc_status cc_kv_attention(const cc_model_cfg *cfg, const cc_kv_cache *kv, int32_
   CC_TRY(wait_kv_ready(kv, layer, layer + 1, st));
   if (step_on_tiles(cfg, kv, rows, p.f16 != 0)) {
     if (out_ld > 0x7FFFFFFF) return CC_ERR_UNSUPPORTED;
-    TimedScope t(CC_KERNEL_KV_ATTENTION, st);
     return run_step_tiles(cfg, kv, rows, p, ws, dev->sms, st);
   }
   kv_attn_bind(p, ws);
