@@ -455,7 +455,9 @@ __global__ void __launch_bounds__(kThreads)
   const size_t at = (size_t)b * rows.cap + s.seq;
   const int follow = pos || s.seq == 0 ? 0 : cache_pos[at - 1] + 1;
   for (int i = threadIdx.x; i < s.count; i += kThreads) {
-    cache_pos[at + i] = pos ? max(pos[s.r0 + i], 0) : follow + i;
+    const int at_pos = pos ? pos[s.r0 + i] : follow + i;
+    if (at_pos < 0) set_status(status, CC_ERR_DEVICE_ARG);
+    cache_pos[at + i] = max(at_pos, 0);
     if (tokens) cache_tokens[at + i] = tokens[s.r0 + i];
   }
   __syncthreads();   // every thread has read seq_len
