@@ -110,6 +110,8 @@ CC_DEV int scale_exp(float bound) {
   return min(max(e, kLeastExp), kMostExp);
 }
 CC_DEV float pow2_biased(int e) { return e > 0 ? __uint_as_float((uint32_t)e << 23) : 0.f; }
+// 1 / 2^(e - 127), e from 1 on (of 2^127 a subnormal).
+CC_DEV float inverse_pow2(int e) { return e == 254 ? __uint_as_float(1u << 22) : pow2_biased(254 - e); }
 
 // 8 pairs: cos, sin, and minus sin, two to a register pair.
 struct Turn {
@@ -311,7 +313,7 @@ __global__ void __launch_bounds__(kThreads, 3)
       int e = max(scale_exp(scale[job]), e_old);
       if (e == 0) e = kUnitExp;   // zeros alone
       if (old && e > e_old) {     // the older codes by a power of two
-        const float f = pow2_biased(127 + e_old - e);
+        const float f = e_old > 0 ? pow2_biased(127 + e_old - e) : 0.f;   // (a scale of 0)
         uint8_t *codes = reinterpret_cast<uint8_t *>(is_k ? p.kc : p.vc);
 #pragma unroll 1
         for (int r = lane / TPR; r < old; r += RPI) {
@@ -336,7 +338,7 @@ __global__ void __launch_bounds__(kThreads, 3)
       __syncwarp();   // every lane has read the bound and the older exponent
       if (lane == 0) {
         *ep = (uint8_t)e;
-        scale[job] = pow2_biased(254 - e);
+        scale[job] = inverse_pow2(e);
       }
     }
   }
