@@ -47,6 +47,8 @@ constexpr int kGroups = 8;         // of the join
 // What a unit costs besides its tiles (its queries, the first loads' latency, its
 // rows at the end: 5 to 6 us where a tile takes 1), in tiles.
 constexpr int kUnitTiles = 5;
+constexpr uint32_t kNoScale = 255;   // a scale exponent: elements that are no numbers (0: a scale of 0)
+constexpr uint32_t kNanCodes = 0x7F7F7F7Fu;
 constexpr uint32_t kBadPage = 0xFFFFFFFFu;   // in place of the scales' place: nothing to see
 constexpr float kNone = -1e30f;    // reference of a row that has seen no key
 constexpr float kSumLimit = 64.f;  // log2 of a term of the sum below
@@ -90,7 +92,7 @@ CC_DEV uint32_t widen2(uint32_t two) {   // e4m3 pair (low 16 bits) -> fp16 pair
   return r;
 }
 CC_DEV uint32_t nan_bytes(uint32_t w) {   // 0xFF in every byte of w that is a NaN code
-  return __vcmpeq4(w & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+  return __vcmpeq4(w & kNanCodes, kNanCodes);
 }
 // Key of index n of the products' 16: odd ones half an 8-row group away.
 CC_DEV int row_of(int n) { return n ^ ((n & 1) << 2); }
@@ -469,7 +471,7 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
         }
       }
       // ---- scores in the log2 domain, against the references
-      const float kf = __uint_as_float(ek << 23);
+      const float scale_k = __uint_as_float(ek << 23), kf = fmaf(scale_k, 0.f, scale_k);   // (e = 255: NaN)
       const float lv = (float)((int)ev - 127);
       const bool mask = slot + 16 > seen_lo;   // uniform over the warp
       float qk[NT][2];   // what makes them scores: 1 where they are masked, and scores already
@@ -547,7 +549,13 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
         else
           *reinterpret_cast<uint2 *>(w[r]) = *reinterpret_cast<const uint2 *>(src);
       }
-      if (mask) {
+      if (mask || ev - 1u >= kNoScale - 1u) {
+        if (ev - 1u >= kNoScale - 1u) {   // a scale of 0, or none: codes that say so
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < VW; ++j) w[r][j] = ev ? kNanCodes : nan_bytes(w[r][j]) & kNanCodes;
+        }
         // keys that some rows do not see: a NaN among their values may reach only
         // the rows that do (0 times NaN is NaN), so it leaves the product
         uint32_t any = 0;
@@ -974,10 +982,12 @@ __global__ void __launch_bounds__(256, 8)
   auto convert = [&](const uint8_t *in, int exp, bool clean, uint16_t *out) {
     const uint4 x = *reinterpret_cast<const uint4 *>(in);
     uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    const float f = __uint_as_float((uint32_t)exp << 23);
+    const bool none = exp == (int)kNoScale;
+    const float f = none ? 1.f : __uint_as_float((uint32_t)exp << 23);
     uint32_t o[8];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
+      if (none) w[j] = kNanCodes;
       if (clean) w[j] &= ~nan_bytes(w[j]);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -991,7 +1001,7 @@ __global__ void __launch_bounds__(256, 8)
     d[1] = make_uint4(o[4], o[5], o[6], o[7]);
   };
   // (the slots of a bad page: keys of NaN, so that the rows that see them are 0)
-  convert(p.k + at * dh + e, vec < 0 ? 255 : p.ke[ei], false, ko + dst);
+  convert(p.k + at * dh + e, vec < 0 ? (int)kNoScale : p.ke[ei], false, ko + dst);
   convert(p.v + at * dh + e, vec < 0 ? 0 : p.ve[ei], i >= s.seq || vec < 0, vo + dst);
 }
 
@@ -1024,11 +1034,13 @@ __global__ void __launch_bounds__(256) kv_restore_nan_kernel(const __grid_consta
   const int g = c * 16 / dh, e = c * 16 - g * dh;
   const long long vec = kv_vec(p.pg, p.rows.cap, b, g, s.seq + r - s.r0);
   if (vec < 0) return;
+  const long long ei = p.pg.head_major ? vec / p.block : vec / p.hkv / p.block * p.hkv + g;
+  const bool none = p.ve[ei] == kNoScale;
   const uint4 u = *reinterpret_cast<const uint4 *>(p.v + vec * dh + e);
-  if (!(nan_bytes(u.x) | nan_bytes(u.y) | nan_bytes(u.z) | nan_bytes(u.w))) return;
+  if (!none && !(nan_bytes(u.x) | nan_bytes(u.y) | nan_bytes(u.z) | nan_bytes(u.w))) return;
   const T nan = std::is_same_v<T, __half> ? T(__ushort_as_half(0x7FFF)) : T(__ushort_as_bfloat16(0x7FFF));
   for (int d = 0; d < 16; ++d) {
-    if ((p.v[vec * dh + e + d] & 0x7F) != 0x7F) continue;
+    if (!none && (p.v[vec * dh + e + d] & 0x7F) != 0x7F) continue;
     for (int i = r; i < s.r0 + s.count; ++i)
       for (int h = 0; h < G; ++h)
         if (fabsf(p.lse[(long long)i * p.hq + g * G + h]) < INFINITY)

@@ -1,12 +1,42 @@
 """Scale exponents at the ends of their byte: 0 stands for a scale of 0, 254 for 2^127, 255 for no
-number."""
+number, in single rows and in chunks alike.  Tolerances as tests/test_gpu_kv_attention.py
+derives them."""
 import numpy as np
 import pytest
 import torch
 
 from tests._step import DeviceCache, device_rows, shape
+from tests.test_gpu_kv_nonfinite import Case
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("memory", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("size", [("slot", 256, [200], [0, 1], 1), ("head", 256, [150], [0, 5], 5),
+                                  ("paged", 512, [300], [0, 100], 100)])
+@pytest.mark.parametrize("name,e", [("v", 0), ("v", 255), ("k", 0), ("k", 255)])
+def test_ends_of_the_exponents(name, e, size, dtype, memory):
+    """One head's block of the memory."""
+    c = Case(8, 2, 64, *size, dtype, seed=e)
+    c.exps[name][0, 3, 1] = e
+    if e == 0 and name == "v":   # (no value to hide behind: what is left is that block's alone)
+        c.exps["v"][0, :, 1] = 0
+    got, ls, want = c.run(memory)
+    if name == "v":
+        assert (got[:, 4:] == 0).all() if e == 0 else got[:, 4:].isnan().all()
+    c.check(got, ls, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("count", [6, 100])
+def test_a_new_block_of_no_numbers(count, dtype):
+    """An exponent of 255 over the values of new tokens reaches the rows that see them and no others."""
+    c = Case(8, 2, 64, "slot", 512, [318], [0, count], count, dtype)
+    c.exps["v"][0, 10, 0] = 255   # slots 320 .. 351
+    got, ls, want = c.run()
+    assert got[:2].isfinite().all() and got[2:, :4].isnan().all()
+    c.check(got, ls, want)
 
 
 @pytest.mark.parametrize("e_old", [0, 254, 255])
