@@ -7,7 +7,8 @@
 // sum below, so that 2^(x - m) neither overflows nor vanishes, and mv for the sum
 // above, so that the largest 2^(x + lv - mv) fills fp16, in which the
 // probabilities meet the codes (exact in fp16) on the tensor cores.  Both are
-// whole numbers: every rescaling is by a power of two.  Queries are scaled by a
+// whole numbers: every rescaling is by a power of two.  mv is held as dv = mv - m, which
+// stays exact where scores are past 2^24.  Queries are scaled by a
 // power of two per row so that bf16 ones fit fp16 exactly; sums are fp32.
 //
 // Bound by the cache's bytes: a tcgen05 tile of 128 query rows would be
@@ -50,7 +51,8 @@ constexpr int kUnitTiles = 5;
 constexpr uint32_t kNoScale = 255;   // a scale exponent: elements that are no numbers (0: a scale of 0)
 constexpr uint32_t kNanCodes = 0x7F7F7F7Fu;
 constexpr uint32_t kBadPage = 0xFFFFFFFFu;   // in place of the scales' place: nothing to see
-constexpr float kNone = -1e30f;    // reference of a row that has seen no key
+constexpr float kNone = -3.402823466e38f;   // reference of a row that has seen no key: the lowest fp32
+constexpr float kFar = 0x1p22f;    // of a reference from which scores are rounded before it is taken off
 constexpr float kSumLimit = 64.f;  // log2 of a term of the sum below
 constexpr float kTop = 15.f, kHead = 8.f;   // log2 of a term above: limit, and what a new reference leaves
 
@@ -204,14 +206,14 @@ CC_DEV RowAt row_at(const KvAttnParams &p, const SeqRows &s, int g, int R) {
   return {s.r0 + pos, g * G + R - pos * G, pos < s.count};
 }
 
-// What the sum above of a row is multiplied by: 2^(mv - m) / l as two factors,
+// What the sum above of a row is multiplied by: 2^dv / l as two factors,
 // neither of which leaves fp32's range (0 for a row without a finite sum below).
 struct OutScale {
   float a, b;
 };
-CC_DEV OutScale out_scale(float m, float mv, float l) {
+CC_DEV OutScale out_scale(float dv, float l) {
   if (!(l > 0.f && l < INFINITY)) return {0.f, 0.f};
-  const int shift = min(max((int)(mv - m), -250), 250), half = shift / 2;
+  const int shift = min(max((int)dv, -250), 250), half = shift / 2;
   return {__uint_as_float((uint32_t)(127 + half) << 23) / l, __uint_as_float((uint32_t)(127 + shift - half) << 23)};
 }
 CC_DEV float row_lse(float m, float l) {
@@ -232,7 +234,7 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
   // (out against 64 bits 2.9e-4 with one, 2.1e-4 with two, the output's own rounding)
   constexpr bool PAIRS = std::is_same_v<T, __half>;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float s_m[kWarps][L::ROWS], s_mv[kWarps][L::ROWS], s_l[kWarps][L::ROWS];
+  __shared__ float s_m[kWarps][L::ROWS], s_dv[kWarps][L::ROWS], s_l[kWarps][L::ROWS];
   __shared__ float4 s_f[L::ROWS];
   __shared__ float s_b[L::ROWS];
   __shared__ long long s_to[L::ROWS];
@@ -417,11 +419,12 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
       }
     }
     if constexpr (L::Q_SHARED) __syncthreads();
-    float o[NT][DT][4], m[NT][2], mv[NT][2], l[NT][2];
+    float o[NT][DT][4], m[NT][2], dv[NT][2], l[NT][2];
+    bool far = false;   // a reference of this lane's rows is past kFar
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      m[t][0] = m[t][1] = mv[t][0] = mv[t][1] = kNone;
-      l[t][0] = l[t][1] = 0.f;
+      m[t][0] = m[t][1] = kNone;
+      dv[t][0] = dv[t][1] = l[t][0] = l[t][1] = 0.f;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -474,12 +477,12 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
       const float scale_k = __uint_as_float(ek << 23), kf = fmaf(scale_k, 0.f, scale_k);   // (e = 255: NaN)
       const float lv = (float)((int)ev - 127);
       const bool mask = slot + 16 > seen_lo;   // uniform over the warp
-      float qk[NT][2];   // what makes them scores: 1 where they are masked, and scores already
+      float qk[NT][2];   // what makes them scores: 1 where they are scores already
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int c = 0; c < 2; ++c) qk[t][c] = qf[t][c] * kf;
-      if (mask) {
+      if (mask || far) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -494,8 +497,9 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int c = 0; c < 2; ++c)
-          over |= fmaxf(sc[t][c], sc[t][2 + c]) * qk[t][c] > fminf(m[t][c] + kSumLimit, mv[t][c] + room);
+          over |= fmaf(fmaxf(sc[t][c], sc[t][2 + c]), qk[t][c], -m[t][c]) > fminf(kSumLimit, dv[t][c] + room);
       if (__any_sync(0xFFFFFFFFu, over)) {
+        far = false;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -504,17 +508,27 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
             x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 4));
             x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 8));
             x = ceilf(fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 16)));
-            const float m1 = fmaxf(m[t][c], x), mv1 = fmaxf(mv[t][c], x + lv - kHead);
-            l[t][c] = m1 < INFINITY ? l[t][c] * ex2(m[t][c] - m1) : NAN;   // (a score past fp32)
-            const float f = ex2(mv[t][c] - mv1);
+            const float m1 = fmaxf(m[t][c], x), fall = m[t][c] - m1;
+            const float dv1 = fmaxf(dv[t][c] + fall, x - m1 + (lv - kHead));
+            l[t][c] = m1 < INFINITY ? l[t][c] * ex2(fall) : NAN;   // (a score past fp32)
+            const float f = ex2(dv[t][c] + fall - dv1);
             m[t][c] = m1;
-            mv[t][c] = mv1;
+            dv[t][c] = dv1;
+            far |= fabsf(m1) >= kFar && m1 > kNone;
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
               o[t][d][c] *= f;
               o[t][d][2 + c] *= f;
             }
           }
+        if (far) {   // the product's rounding, which counts here, is to be the reference's
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sc[t][k] *= qk[t][k & 1];
+            qk[t][0] = qk[t][1] = 1.f;
+          }
+        }
       }
       uint32_t pb[NT][2], pl[PAIRS ? NT : 1][2];
 #pragma unroll
@@ -523,7 +537,7 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           // (finite: a key of probability 0 may have any scale)
-          const float f = ex2(fminf(lv + m[t][c] - mv[t][c], 126.f));
+          const float f = ex2(fminf(lv - dv[t][c], 126.f));
           const float p0 = ex2(fmaf(sc[t][c], qk[t][c], -m[t][c])), p1 = ex2(fmaf(sc[t][2 + c], qk[t][c], -m[t][c]));
           l[t][c] += p0 + p1;
           y[c] = p0 * f;
@@ -625,7 +639,7 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
         const int row = 8 * t + 2 * quad + c;
         if (n8 == 0) {
           s_m[warp][row] = m[t][c];
-          s_mv[warp][row] = mv[t][c];
+          s_dv[warp][row] = dv[t][c];
           s_l[warp][row] = x;
         }
         float4 *dst = reinterpret_cast<float4 *>(so + (warp * L::ROWS + row) * DH + n8 * L::VB);
@@ -643,25 +657,26 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
     const long long part = (2ll * cta + (first && tile0 > 0 ? 0 : 1)) * L::ROWS;
     if (tid < L::ROWS) {   // per row: the warps' weights, and where it goes
       const RowAt r = row_at(p, s, g, R0 + tid);
-      float mt = kNone, mvt = kNone, lt = 0.f, f[kWarps];
+      float mt = kNone, dvt = -INFINITY, lt = 0.f, f[kWarps];
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        mt = fmaxf(mt, s_m[w][tid]);
-        mvt = fmaxf(mvt, s_mv[w][tid]);
-      }
+      for (int w = 0; w < kWarps; ++w) mt = fmaxf(mt, s_m[w][tid]);
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {   // a warp without keys holds zeros
-        lt += s_l[w][tid] * ex2(s_m[w][tid] - mt);
-        f[w] = ex2(s_mv[w][tid] - mvt);
+        const float fall = s_m[w][tid] - mt;
+        lt += s_l[w][tid] * ex2(fall);
+        f[w] = s_dv[w][tid] + fall;
+        dvt = fmaxf(dvt, f[w]);
       }
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) f[w] = ex2(f[w] - dvt);
       OutScale k{1.f, 1.f};
       long long to = r.live ? (part + tid) * DH : -1;
       if (whole) {
-        k = out_scale(mt, mvt, lt);
+        k = out_scale(dvt, lt);
         if (r.live) to = r.row * p.out_ld + (long long)r.head * DH;
         if (r.live && p.lse) p.lse[(long long)r.row * p.hq + r.head] = row_lse(mt, lt);
       } else {
-        p.part_ml[part + tid] = make_float4(mt, mvt, lt, 0.f);
+        p.part_ml[part + tid] = make_float4(mt, dvt, lt, 0.f);
       }
       s_f[tid] = make_float4(f[0] * k.a, f[1] * k.a, f[2] * k.a, f[3] * k.a);
       s_b[tid] = k.b;
@@ -708,7 +723,7 @@ template <typename T, int DH, int NT, bool SPREAD>
 __global__ void __launch_bounds__(kGroups * DH / 2, SPREAD ? 1 : 1024 / (kGroups * DH / 2))
     kv_combine_kernel(const __grid_constant__ KvAttnParams p) {
   constexpr int ROWS = 8 * NT, kJoin = SPREAD ? 8 : 4;
-  __shared__ float4 part[SPREAD ? kGroups : 1][DH / 2];   // m, mv and the two sums
+  __shared__ float4 part[SPREAD ? kGroups : 1][DH / 2];   // m, dv and the two sums
   __shared__ float part_l[kGroups];
   const int group = threadIdx.x / (DH / 2), d = (threadIdx.x - group * (DH / 2)) * 2;
   const int R = SPREAD ? blockIdx.y : blockIdx.y * kGroups + group;
@@ -728,15 +743,16 @@ __global__ void __launch_bounds__(kGroups * DH / 2, SPREAD ? 1 : 1024 / (kGroups
   // share c0 holds the unit's start, those after it start inside the unit
   auto slot = [&](int c) { return (2ll * ((long long)c * p.hkv + g) + (c == c0 ? 1 : 0)) * ROWS + R; };
   constexpr int STEP = SPREAD ? kGroups : 1;
-  float m = kNone, mv = kNone, l = 0.f, o0 = 0.f, o1 = 0.f;
-  auto join = [&](float xm, float xmv, float xl, float x0, float x1) {
-    const float m1 = fmaxf(m, xm), mv1 = fmaxf(mv, xmv);
-    l = l * ex2(m - m1) + xl * ex2(xm - m1);
-    const float f = ex2(mv - mv1), g = ex2(xmv - mv1);
+  float m = kNone, dv = 0.f, l = 0.f, o0 = 0.f, o1 = 0.f;
+  auto join = [&](float xm, float xdv, float xl, float x0, float x1) {
+    const float m1 = fmaxf(m, xm), fall = m - m1, x_fall = xm - m1;
+    const float a = dv + fall, b = xdv + x_fall, dv1 = fmaxf(a, b);
+    l = l * ex2(fall) + xl * ex2(x_fall);
+    const float f = ex2(a - dv1), g = ex2(b - dv1);
     o0 = o0 * f + x0 * g;
     o1 = o1 * f + x1 * g;
     m = m1;
-    mv = mv1;
+    dv = dv1;
   };
 #pragma unroll 1
   for (int c = c0 + (SPREAD ? group : 0); c <= c1; c += kJoin * STEP) {
@@ -753,7 +769,7 @@ __global__ void __launch_bounds__(kGroups * DH / 2, SPREAD ? 1 : 1024 / (kGroups
       if (c + k * STEP <= c1) join(x[k].x, x[k].y, x[k].z, v[k].x, v[k].y);
   }
   if constexpr (SPREAD) {
-    part[group][d / 2] = make_float4(m, mv, o0, o1);
+    part[group][d / 2] = make_float4(m, dv, o0, o1);
     if (d == 0) part_l[group] = l;
     __syncthreads();
     if (group > 0) return;
@@ -764,7 +780,7 @@ __global__ void __launch_bounds__(kGroups * DH / 2, SPREAD ? 1 : 1024 / (kGroups
     }
   }
   if (!r.live) return;
-  const OutScale k = out_scale(m, mv, l);
+  const OutScale k = out_scale(dv, l);
   *reinterpret_cast<uint32_t *>(reinterpret_cast<T *>(p.out) + r.row * p.out_ld + (long long)r.head * DH + d) =
       k.b == 0.f ? 0u : pack2<T>(o0 * k.a * k.b, o1 * k.a * k.b);
   if (p.lse && d == 0) p.lse[(long long)r.row * p.hq + r.head] = row_lse(m, l);
