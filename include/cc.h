@@ -233,7 +233,8 @@ typedef struct {
    * [n_layers] of device uint8 scale exponents, ordered as the codes: a slot-major cache's
    * [batch][cap / kv_block][Hkv], a paged one's [n_pages][page_size / kv_block][Hkv], a
    * head-major one's [batch][Hkv][cap / kv_block].  e = 1 .. 254 stands for 2^(e - 127),
-   * 0 for a scale of 0 (e = 255 is not a number).  cc_kv_append writes 10 .. 247. */
+   * 0 for a scale of 0; the elements of a block with e = 255 are not numbers.
+   * cc_kv_append writes 10 .. 247, or what older slots of the block have. */
   int32_t kv_block;
   void *const *k_exp;
   void *const *v_exp;
@@ -494,10 +495,17 @@ cc_status cc_kv_append(const cc_model_cfg *cfg, const cc_kv_cache *cache, int32_
  *   lse:    device fp32 [n_rows][Hq], or NULL: ln sum_j exp(score_j), by which
  *           results over disjoint slots join.
  * A row that sees no slot gets 0 and -inf.  A row with a score that is NaN or
- * infinite gets 0 (its lse is no finite number).  Slots that a row does not see
- * may hold any bits.  Chunks of more than a few dozen query rows a KV head run on
- * tcgen05 over a bf16 copy of the layer in the workspace (exact; fp16 rows as
- * bf16 pairs), which the workspace size includes. */
+ * infinite gets 0 (its lse is no finite number), whatever the values; else a value
+ * that is NaN makes its column NaN in the rows that see it.  Slots that a row does
+ * not see may hold any bits.
+ * One of two kernels takes the whole call.  Where sequences have, on average over
+ * all of the batch, more than 64 query rows a KV head (n_rows * Hq / Hkv > 64 * batch;
+ * fp16 96) and one may have 4 rows or more, it is tcgen05 tiles over a bf16 copy of
+ * the layer in the workspace (exact; fp16 rows as bf16 pairs).  The copy goes by room,
+ * not by what is held: 4 * Hkv * head_dim bytes for each of batch * cap slots.  There
+ * a bf16 row's probabilities are rounded to bf16 before they weigh the values (scores
+ * past 2^30 are out of its range); the other kernel rounds them to fp16.  An fp16
+ * row's are two such parts in either. */
 size_t cc_kv_attention_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *cache,
                                       const cc_rows *rows);
 cc_status cc_kv_attention(const cc_model_cfg *cfg, const cc_kv_cache *cache, int32_t layer,

@@ -1841,6 +1841,7 @@ KvAttnParams kv_attn_params(const cc_model_cfg *c, const cc_kv_cache *kv, const 
 // tiles multiply pairs: three).  Direct and tiles, 8 sequences of 8192 slots and 32/8
 // heads: 64 rows 114 and 142 us, 96 rows 161 and 143; fp16 96 rows 175 and 208, 128
 // rows 228 and 209; one Qwen2.5-7B sequence: 56 rows 23 and 30, 112 rows 32 and 30.
+// (One kernel for the whole call: a chunk among many single rows is slow on either.)
 constexpr int kTileRows = 64, kTileRowsF16 = 96, kTileMinRows = 4;
 bool step_on_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows, bool f16) {
   const long long group = c->n_q_heads / c->n_kv_heads;
@@ -1891,7 +1892,9 @@ StepTileWs step_tile_layout(const cc_model_cfg *c, const cc_kv_cache *kv, const 
 }
 
 // The rows' attention as tiles of 256 query rows (attn.cu) over a bf16 copy of
-// the layer; fp16 rows as bf16 pairs, P as pairs too (twice the products).
+// the layer; fp16 rows as bf16 pairs, P as pairs too (twice the products).  bf16 rows
+// take P as bf16, at half of that: out against 64 bits 0.0022, of which the output's own
+// rounding is 0.0017.
 cc_status run_step_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows,
                          KvAttnParams kp, void *ws, int sms, cudaStream_t st) {
   StepTileWs L = step_tile_layout(c, kv, rows, std::min(sms, kStepMaxSms));

@@ -17,8 +17,8 @@
 // copies what it will read a few heads (rows, for the bound) ahead into slots of its
 // own (cp.async, no barrier): loops unrolled over loads instead held as much in
 // flight but half of the time nothing, and their code was a single token's latency.
-// Four chunks of 4096 tokens, 32/8 heads of 128, bf16: 369 MB in 69 us (5.3 TB/s); 2957
-// tokens of five ragged sequences, 28/4 heads, fp32: 100 MB in 16.6 us (6.0 TB/s); a
+// Four chunks of 4096 tokens, 32/8 heads of 128, bf16: 369 MB in 71 us (5.2 TB/s); 2957
+// tokens of five ragged sequences, 28/4 heads, fp32: 100 MB in 16.7 us (6.0 TB/s); a
 // token each of 64 sequences: 6.6 us, latency (launch, bound, rows one after another).
 #include "kvappend.cuh"
 

@@ -9,7 +9,8 @@
 // probabilities meet the codes (exact in fp16) on the tensor cores.  Both are
 // whole numbers: every rescaling is by a power of two.  mv is held as dv = mv - m, which
 // stays exact where scores are past 2^24.  Queries are scaled by a
-// power of two per row so that bf16 ones fit fp16 exactly; sums are fp32.
+// power of two per row so that bf16 ones fit fp16 exactly; sums are fp32.  A bf16 row's
+// probabilities are one fp16 each (out against 64 bits 0.00165, with fp32 ones 0.00163).
 //
 // Bound by the cache's bytes: a tcgen05 tile of 128 query rows would be
 // nearly all padding, so the products are m16n8k16 with the keys (then the head
@@ -29,9 +30,10 @@
 // order (row_of) in which, with the rows' pieces swizzled, neither product's reads
 // meet in a bank.
 //
-// 64 ragged sequences of 1500 to 32767 slots, a row each, 32/8 heads: 2.25 GB in 337 us
-// (6.7 TB/s); one of 8192 slots, 28/4 heads: 11.3 us, of which the stream is 1.3.  Units
-// of 24 rows are bound by issue: 16 sequences' 5 rows of fp16, 153 MB in 60 us.
+// 64 ragged sequences of 1500 to 32767 slots, a row each, 32/8 heads: 2.25 GB in 345 us
+// (6.5 TB/s); one of 8192 slots, 28/4 heads: 12.3 us, of which the stream is 1.3.  Units
+// of 24 rows wait for their own latencies (40 % of the issue slots): 16 sequences' 5 rows of
+// fp16, 153 MB in 59 us.
 #include "kvattn.cuh"
 
 #include <algorithm>

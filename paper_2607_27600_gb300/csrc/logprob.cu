@@ -21,8 +21,11 @@
 // cluster of up to 8 CTAs does, a contiguous segment each, and rank 0 joins their
 // sums and sorted lists through distributed shared memory.
 //
-// 4096 rows of 128256 bf16 logits, 8 alternatives: 1.05 GB in 181 us (5.8 TB/s); 64 rows
-// of 152064: 10 us; one fp32 row: 7.3 us, launch, cluster and sort one after another.
+// 4096 rows of 128256 bf16 logits, 8 alternatives: 1.05 GB in 187 us (5.6 TB/s); 64 rows
+// of 152064: 12.3 us a call, 10 of them in the kernel; one fp32 row: 10.2 us, 7.3 in the
+// kernel, cluster and sort one after another.
+// One of the 64 rows done again (nothing allowed, or the lowest value everywhere): 156 us,
+// of one warp that reads it twice.
 #include "logprob.cuh"
 
 #include <type_traits>
