@@ -12,9 +12,10 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("dh,lens,counts", [(64, [200, 0, 77], [1, 1, 1]), (128, [1, 500], [9, 2]),
-                                            (64, [3000], [1]), (64, [100], [200])])
-@pytest.mark.parametrize("power", [14, 24, 27, 31])
+@pytest.mark.parametrize("power,dh,lens,counts", [
+    (power, *case) for power in (14, 24, 27, 31, 36, 70)
+    for case in ((64, [200, 0, 77], [1, 1, 1]), (128, [1, 500], [9, 2]), (64, [3000], [1]), (64, [100], [200]),
+                 (64, [3000], [60])) if power < 36 or max(case[2]) < 60])   # (chunks reach to 2^30)
 def test_large_scores(power, dh, lens, counts, dtype):
     import paper_2607_27600_gb300 as pkg
     from paper_2607_27600_gb300 import cc
