@@ -110,8 +110,9 @@ typedef enum {
  * block of kv_block slots and KV head, K and V apart, held as one byte e: an
  * element is code * 2^(e - 127).  A power of two costs a floating-point code no
  * precision, makes an element exact in bf16 and lets a block that meets a
- * larger value be rescaled exactly.  It is written by cc_kv_append and read by
- * cc_kv_attention; the calls that run the model's layers themselves refuse it
+ * larger value be rescaled exactly.  It is written by cc_kv_append, read by
+ * cc_kv_attention and cc_kv_accumulate and compacted by cc_kv_compact; the calls
+ * that run the model's layers themselves, and cc_compact_kv, refuse it
  * (CC_ERR_UNSUPPORTED). */
 typedef enum {
   CC_KV_BF16 = 0,
@@ -512,6 +513,62 @@ cc_status cc_kv_attention(const cc_model_cfg *cfg, const cc_kv_cache *cache, int
                           const cc_rows *rows, cc_dtype dtype, int32_t memory_only,
                           const void *q, int64_t q_ld, void *out, int64_t out_ld, float *lse,
                           void *ws, size_t ws_bytes, void *stream);
+
+/* cc_kv_join -- attention over disjoint slots joined: parts o_i with their lse
+ * s_i (of cc_kv_attention, or of the caller's own) become
+ *   out = sum_i e^(s_i - s) o_i,   lse = s = ln sum_i e^s_i,
+ * row by row and head by head.  For a batch that shares a long prefix, attend it
+ * once for all: the rows as one sequence of a cache of batch 1 that holds the
+ * prefix (memory_only), the same rows over each sequence's own cache, then joined;
+ * the joint lse is what cc_kv_accumulate takes.
+ *   part, part_ld, part_lse: HOST arrays [n_parts], 1 <= n_parts <= 16 (more:
+ *     CC_ERR_UNSUPPORTED), of device [n_rows][Hq * head_dim] of `dtype`, rows
+ *     part_ld[i] elements apart, and device fp32 [n_rows][Hq];
+ *   out, lse: as a part; lse may be NULL.  Either may lie exactly where one of the
+ *     parts (its lse) does, with the same pitch, and must not overlap them otherwise.
+ * A part whose lse is -inf saw no slot and is not looked at; a row and head with only
+ * such gets 0 and -inf.  One whose lse is NaN or +inf in any part gets 0 and NaN. */
+cc_status cc_kv_join(const cc_model_cfg *cfg, cc_dtype dtype, int32_t n_rows, int32_t n_parts,
+                     const void *const *part, const int64_t *part_ld, const float *const *part_lse,
+                     void *out, int64_t out_ld, float *lse, void *stream);
+
+/* cc_kv_accumulate -- the attention that the slots receive from a step's rows, by
+ * which an eviction ranks them: adds to cache->h2o_acc
+ *   acc[b][j] += sum_{r, t} e^(q[r][t] . K[j] / sqrt(head_dim) - lse[r][t])
+ * over the rows r of sequence b that see slot j (as in cc_kv_attention, with
+ * memory_only too) and all their heads t.  Call it for a layer (or several: the totals
+ * add up) with that layer's q and lse, after cc_kv_attention and before
+ * cc_kv_advance; cc_score_h2o then ranks by the totals and cc_kv_compact moves them.
+ *   first: the slots of the rows themselves start from 0, whatever they hold: for
+ *          the step's first layer.  Not with memory_only (CC_ERR_INVALID_ARG).
+ *   q:     device [n_rows][Hq * head_dim], bf16 or fp16, as in cc_kv_attention;
+ *   lse:   device fp32 [n_rows][Hq].  A row and head whose lse is not finite adds
+ *          nothing, whatever the slots hold.
+ * Block format only (others: CC_ERR_UNSUPPORTED).  Slots that no row sees keep their
+ * totals.  Sums run in a fixed order: the same call gives the same bits. */
+size_t cc_kv_accumulate_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *cache,
+                                       const cc_rows *rows);
+cc_status cc_kv_accumulate(const cc_model_cfg *cfg, const cc_kv_cache *cache, int32_t layer,
+                           const cc_rows *rows, cc_dtype dtype, int32_t first, int32_t memory_only,
+                           const void *q, int64_t q_ld, const float *lse, void *ws, size_t ws_bytes,
+                           void *stream);
+
+/* cc_kv_compact -- cc_compact_kv for the block format (others:
+ * CC_ERR_UNSUPPORTED): in place, slot k < keep_count[b] of every non-NULL k[l], v[l] with
+ * its exponents, of tokens, pos and (if non-NULL) h_last and h2o_acc receives old slot
+ * keep_idx[b*cap + k]; then seq_len[b] = keep_count[b].  keep_idx must be strictly
+ * ascending per sequence and below seq_len[b] (as cc_select_keep writes it).
+ * A block's exponent becomes the largest of its slots' old ones; codes of smaller
+ * scales are rounded to nearest (ties to even) in it.  Slots of a block with e = 255 do
+ * not count there and become NaN codes; a block of only such stays one.  Codes past
+ * keep_count[b] keep their bits.
+ * A count outside [0, cap] is reported as CC_ERR_DEVICE_ARG and taken as 0.  An entry
+ * of keep_idx out of order or range is reported; what its sequence's slots then hold is
+ * unspecified.  A block-table entry outside the pool is reported and the slots that come
+ * from its page or go to it stay as they are. */
+size_t cc_kv_compact_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *cache);
+cc_status cc_kv_compact(const cc_model_cfg *cfg, const cc_kv_cache *cache, const int32_t *keep_idx,
+                        const int32_t *keep_count, void *ws, size_t ws_bytes, void *stream);
 
 /* cc_kv_advance -- ends a step: the rows' positions and, with tokens (device
  * int32 [n_rows]), token ids into the cache's pos and tokens, then seq_len[b]

@@ -28,7 +28,7 @@ typedef enum {
   CC_KERNEL_GEMM_LMHEAD = 8, /* LM-head GEMM + log-sum-exp partials (log-prob)    */
   CC_KERNEL_LSE_COMBINE = 9, /* log-sum-exp combine (log-prob)                    */
   CC_KERNEL_SELECT = 10,     /* keep-set radix select                             */
-  CC_KERNEL_COMPACT = 11,    /* in-place compaction                               */
+  CC_KERNEL_COMPACT = 11,    /* in-place compaction, of either kind of cache       */
   CC_KERNEL_OTHER = 12,      /* kernel-level entry points (cc_kernels.h)          */
   CC_KERNEL_GEMM_KV = 13,    /* key (+ RoPE) and value projections (append)       */
   CC_KERNEL_ATTN_CAUSAL = 14,/* memory-augmented causal attention (append)        */
@@ -41,7 +41,9 @@ typedef enum {
   CC_KERNEL_KV_APPEND = 19,  /* cc_kv_append, cc_kv_advance                       */
   CC_KERNEL_KV_ATTENTION = 20,/* cc_kv_attention but for a chunk's copy            */
   CC_KERNEL_TOKEN_LOGPROB = 21,/* cc_token_logprobs                               */
-  CC_KERNEL_COUNT = 22
+  CC_KERNEL_KV_ACCUMULATE = 22,/* cc_kv_accumulate                                */
+  CC_KERNEL_KV_JOIN = 23,    /* cc_kv_join                                        */
+  CC_KERNEL_COUNT = 24
 } cc_kernel_kind;
 
 /* on != 0: start recording (also clears earlier records); 0: stop. */

@@ -46,6 +46,11 @@ Parity status per function (what pins it, in tests/test_oracle_*.py):
                            every written value within half a step; a scalar case
   attend_rows              torch SDPA with an explicit mask (library routine)
   token_logprobs           torch log_softmax, topk (library routines); scipy entropy
+  received                 with the rows' own lse the weights of a row and head sum to 1;
+                           equal keys -> uniform; torch softmax (library routine)
+  compact_blocks           equal scales = a gather of codes and exponents; values within
+                           half a step of the new scale; a scalar case
+  join_parts               attend_rows over all slots = over two halves, joined
 The paper prints no worked example with score values, so no pin is a
 printed number; every step of the score is pinned by the checks above.
 """
@@ -57,5 +62,5 @@ from .refresh import (rms_norm, rope, rope_angles, rope_inv_freq, project, softm
                       key_attention_colsums, importance_scores, h2o_update, h2o_scores,
                       decode_step)
 from .fp8 import e4m3_decode, e4m3_encode, kv_quantize  # noqa: F401
-from .step import (append_blocks, attend_rows, block_exponent, k_bound, rotate_rows,  # noqa: F401
-                   token_logprobs, v_bound)
+from .step import (append_blocks, attend_rows, block_exponent, compact_blocks,  # noqa: F401
+                   join_parts, k_bound, received, rotate_rows, token_logprobs, v_bound)

@@ -110,3 +110,71 @@ def token_logprobs(z, targets, top):
         order = np.lexsort((np.arange(len(row)), -row))[:top]
         ids[r], tlp[r] = order, log_p[order]
     return lp, ent, ids, tlp
+
+
+def received(q, k, lse, seq_len, start, memory_only=False):
+    """The attention that each slot of values k [B][cap][Hkv][dh] receives from the rows:
+    sum over rows and heads of exp(score - lse) where a row sees the slot; lse [n][Hq],
+    rows and heads where it is not finite add nothing.  Returns (sums, slack), both
+    [B][cap]: slack = sum of the same terms, each times sum_i |q_i K_i| / sqrt(dh) (what
+    rounding of a product's sum is relative to) + |score| + |lse|."""
+    q, lse = np.asarray(q, np.float64), np.asarray(lse, np.float64)
+    n, hq, dh = q.shape
+    g = hq // k.shape[2]
+    out, slack = np.zeros(k.shape[:2]), np.zeros(k.shape[:2])
+    for b in range(len(seq_len)):
+        for r in range(start[b], start[b + 1]):
+            end = seq_len[b] if memory_only else seq_len[b] + r - start[b] + 1
+            for h in range(hq):
+                if end == 0 or not np.isfinite(lse[r, h]):
+                    continue
+                x = k[b, :end, h // g]
+                s = x @ q[r, h] / np.sqrt(dh)
+                w = np.exp(s - lse[r, h])
+                out[b, :end] += w
+                slack[b, :end] += w * (np.abs(x) @ np.abs(q[r, h]) / np.sqrt(dh) + np.abs(s) + abs(lse[r, h]))
+    return out, slack
+
+
+def compact_blocks(codes, exps, block, keep):
+    """The kept slots keep[b] (ascending) of codes [B][cap][Hkv][dh] moved down, in copies
+    of codes and exps: a block's exponent is the largest of its slots' old ones but 255,
+    and codes are rounded to it; slots of exponent 255 become NaN codes, unless the block
+    holds nothing else."""
+    old_codes, old_exps = codes, exps
+    codes, exps = codes.copy(), exps.copy()
+    for b, idx in enumerate(keep):
+        for j in range(0, len(idx), block):
+            src = np.asarray(idx[j:j + block], int)
+            for g in range(codes.shape[2]):
+                e = old_exps[b, src // block, g].astype(int)
+                numbers = e[e != 255]
+                top = numbers.max() if len(numbers) else 255
+                exps[b, j // block, g] = top
+                for i, (s, es) in enumerate(zip(src, e)):
+                    c = old_codes[b, s, g]
+                    if es == 255 and top != 255:
+                        c = np.full_like(c, 0x7F)
+                    elif es != top:   # (a scale of 0: zeros, but for codes that are no numbers)
+                        c = e4m3_encode(e4m3_decode(c) * (2.0 ** (es - top) if es else 0.0))
+                    codes[b, j + i, g] = c
+    return codes, exps
+
+
+def join_parts(parts, lses):
+    """Attention over disjoint slots joined: parts [P][n][Hq][dh], lses [P][n][Hq]."""
+    parts, lses = np.asarray(parts, np.float64), np.asarray(lses, np.float64)
+    out, lse = np.zeros(parts.shape[1:]), np.full(lses.shape[1:], -np.inf)
+    for r in range(lses.shape[1]):
+        for h in range(lses.shape[2]):
+            s = lses[:, r, h]
+            if (np.isnan(s) | (s == np.inf)).any():
+                lse[r, h] = np.nan
+                continue
+            live = [i for i in range(len(s)) if s[i] > -np.inf]
+            if live:
+                m = s[live].max()
+                w = np.exp(s[live] - m)
+                out[r, h] = sum(wi * parts[i, r, h] for wi, i in zip(w, live)) / w.sum()
+                lse[r, h] = m + np.log(w.sum())
+    return out, lse

@@ -169,13 +169,29 @@ _SIGS = {
                                        ctypes.c_int32, ctypes.POINTER(cc_rows), ctypes.c_int,
                                        ctypes.c_int32] + [ctypes.c_void_p, ctypes.c_int64] * 2
                         + [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "cc_kv_join": (ctypes.c_int, [ctypes.POINTER(cc_model_cfg), ctypes.c_int, ctypes.c_int32,
+                                  ctypes.c_int32] + [ctypes.c_void_p] * 4
+                   + [ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p]),
+    "cc_kv_accumulate_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(cc_model_cfg),
+                                                          ctypes.POINTER(cc_kv_cache),
+                                                          ctypes.POINTER(cc_rows)]),
+    "cc_kv_accumulate": (ctypes.c_int, [ctypes.POINTER(cc_model_cfg), ctypes.POINTER(cc_kv_cache),
+                                        ctypes.c_int32, ctypes.POINTER(cc_rows), ctypes.c_int,
+                                        ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
+                                        ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p,
+                                        ctypes.c_size_t, ctypes.c_void_p]),
+    "cc_kv_compact_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(cc_model_cfg),
+                                                       ctypes.POINTER(cc_kv_cache)]),
+    "cc_kv_compact": (ctypes.c_int, [ctypes.POINTER(cc_model_cfg), ctypes.POINTER(cc_kv_cache),
+                                     ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                     ctypes.c_size_t, ctypes.c_void_p]),
     "cc_kv_advance": (ctypes.c_int, [ctypes.POINTER(cc_kv_cache), ctypes.POINTER(cc_rows),
                                      ctypes.c_void_p, ctypes.c_void_p]),
     "cc_token_logprobs": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int32,
                                          ctypes.c_int32, ctypes.c_int64] + [ctypes.c_void_p] * 3
                           + [ctypes.c_int32] + [ctypes.c_void_p] * 3),
 }
-KERNEL_COUNT = 22
+KERNEL_COUNT = 24
 
 
 def library_path() -> str:
@@ -705,6 +721,61 @@ def cc_kv_attention(cfg, cache: Cache, layer: int, rows: Rows, q, out, ws, lse=N
         *_row_ptr(q, "q", n, hq, q.dtype), *_row_ptr(out, "out", n, hq, q.dtype),
         _vec_ptr(lse, "lse", n * c.n_q_heads, torch.float32), _dev_ptr(ws, "ws"),
         ws.numel() * ws.element_size(), _stream(stream)), "cc_kv_attention")
+
+
+def cc_kv_join(cfg, parts, part_lses, out, lse=None, stream=None):
+    """Attention over disjoint slots joined: parts (a list of [n_rows, Hq, dh] of one
+    type) with their log-sum-exp (fp32 [n_rows, Hq] each) into out and lse (or None).
+    out may be one of the parts, and lse one of theirs."""
+    c = _cfg(cfg)
+    k = len(parts)
+    if k < 1 or len(part_lses) != k:
+        raise ValueError(f"{k} parts with {len(part_lses)} lse")
+    if None in (*parts, *part_lses, out):
+        raise TypeError("parts, their lse and out must be CUDA tensors")
+    n, hq = out.shape[0], c.n_q_heads * c.head_dim
+    at = [_row_ptr(x, f"parts[{i}]", n, hq, out.dtype) for i, x in enumerate(parts)]
+    ptrs = (ctypes.c_void_p * k)(*[a[0] for a in at])
+    lds = (ctypes.c_int64 * k)(*[a[1] for a in at])
+    lses = (ctypes.c_void_p * k)(*[_vec_ptr(x, f"part_lses[{i}]", n * c.n_q_heads, torch.float32)
+                                   for i, x in enumerate(part_lses)])
+    _check(load_library().cc_kv_join(
+        c, _dtype(out, "out"), n, k, ptrs, lds, lses, *_row_ptr(out, "out", n, hq, out.dtype),
+        _vec_ptr(lse, "lse", n * c.n_q_heads, torch.float32), _stream(stream)), "cc_kv_join")
+
+
+def cc_kv_accumulate_workspace_size(cfg, cache: Cache, rows: Rows) -> int:
+    return int(load_library().cc_kv_accumulate_workspace_size(_cfg(cfg), cache.c,
+                                                              _step_rows(cache, rows)))
+
+
+def cc_kv_accumulate(cfg, cache: Cache, layer: int, rows: Rows, q, lse, ws, first: bool = False,
+                     memory_only: bool = False, stream=None):
+    """Adds to the cache's h2o_acc the attention that each slot receives from the rows
+    (q [n_rows, Hq, dh], bf16 or fp16, with lse fp32 [n_rows, Hq] as cc_kv_attention
+    leaves it) in layer `layer` of a block-format cache.  first: the rows' own slots
+    start from 0."""
+    c, r = _cfg(cfg), _step_rows(cache, rows)
+    n, hq = r.n_rows, c.n_q_heads * c.head_dim
+    _check(load_library().cc_kv_accumulate(
+        c, cache.c, layer, r, _dtype(q, "q"), 1 if first else 0, 1 if memory_only else 0,
+        *_row_ptr(q, "q", n, hq, q.dtype), _vec_ptr(lse, "lse", n * c.n_q_heads, torch.float32),
+        _dev_ptr(ws, "ws"), ws.numel() * ws.element_size(), _stream(stream)), "cc_kv_accumulate")
+
+
+def cc_kv_compact_workspace_size(cfg, cache: Cache) -> int:
+    return int(load_library().cc_kv_compact_workspace_size(_cfg(cfg), cache.c))
+
+
+def cc_kv_compact(cfg, cache: Cache, keep_idx, keep_count, ws, stream=None):
+    """In place, slot k of every array of a block-format cache receives old slot
+    keep_idx[b, k], k < keep_count[b] (int32 [B, cap] and [B]); the codes of a new block
+    come to its largest scale."""
+    b, cap = cache.c.batch, cache.c.cap
+    _check(load_library().cc_kv_compact(
+        _cfg(cfg), cache.c, _vec_ptr(keep_idx, "keep_idx", b * cap, torch.int32),
+        _vec_ptr(keep_count, "keep_count", b, torch.int32), _dev_ptr(ws, "ws"),
+        ws.numel() * ws.element_size(), _stream(stream)), "cc_kv_compact")
 
 
 def cc_kv_advance(cache: Cache, rows: Rows, tokens=None, stream=None):

@@ -27,6 +27,9 @@
 #include "keyattn.cuh"
 #include "kvappend.cuh"
 #include "kvattn.cuh"
+#include "kvcompact.cuh"
+#include "kvjoin.cuh"
+#include "kvreceived.cuh"
 #include "logprob.cuh"
 #include "rowops.cuh"
 #include "select.cuh"
@@ -2078,6 +2081,158 @@ cc_status cc_kv_attention(const cc_model_cfg *cfg, const cc_kv_cache *kv, int32_
   return CC_OK;
 }
 
+cc_status cc_kv_join(const cc_model_cfg *cfg, cc_dtype dtype, int32_t n_rows, int32_t n_parts,
+                     const void *const *part, const int64_t *part_ld, const float *const *part_lse,
+                     void *out, int64_t out_ld, float *lse, void *stream) {
+  const cc_status s = check_cfg(cfg);
+  if (s != CC_OK) return s;
+  if (dtype != CC_BF16 && dtype != CC_F16 && dtype != CC_F32) return CC_ERR_INVALID_ARG;
+  if (n_rows < 0 || n_parts < 1) return CC_ERR_INVALID_ARG;
+  if (n_parts > kMaxJoinParts) return CC_ERR_UNSUPPORTED;
+  if (n_rows == 0) return CC_OK;
+  const int bytes = dtype == CC_F32 ? 4 : 2, hq = cfg->n_q_heads;
+  if (!part || !part_ld || !part_lse || !rows_ok(cfg, out, out_ld, hq, bytes)) return CC_ERR_INVALID_ARG;
+  KvJoinParams p{};
+  for (int i = 0; i < n_parts; ++i) {
+    if (!rows_ok(cfg, part[i], part_ld[i], hq, bytes) || !part_lse[i]) return CC_ERR_INVALID_ARG;
+    p.part[i] = part[i];
+    p.part_ld[i] = part_ld[i];
+    p.part_lse[i] = part_lse[i];
+  }
+  if ((uint64_t)n_rows * hq * cfg->head_dim >= (1ull << 40)) return CC_ERR_UNSUPPORTED;   // (the grid's size)
+  p.n_rows = n_rows;
+  p.hq = hq;
+  p.head_dim = cfg->head_dim;
+  p.n_parts = n_parts;
+  p.dtype = dtype;
+  p.out = out;
+  p.out_ld = out_ld;
+  p.lse = lse;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  TimedScope t(CC_KERNEL_KV_JOIN, st);
+  CC_TRY(launch_kv_join(p, st));
+  return CC_OK;
+}
+
+namespace {
+
+KvReceivedParams kv_received_params(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows, int sms) {
+  KvReceivedParams p{};
+  p.rows = step_rows(kv, rows);
+  p.block = kv->kv_block;
+  p.pg = kv_layout(c, kv);
+  p.hq = c->n_q_heads;
+  p.hkv = c->n_kv_heads;
+  p.head_dim = c->head_dim;
+  p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)c->head_dim));
+  kv_received_plan(p, std::min(sms, kStepMaxSms));
+  return p;
+}
+
+// The compaction's arrays and units; which of the arguments are wrong.
+cc_status kv_compact_params(const cc_model_cfg *c, const cc_kv_cache *kv, KvCompactParams &p) {
+  const cc_status s = check_cfg(c);
+  if (s != CC_OK) return s;
+  if (!kv || kv->batch < 1 || kv->cap < 1 || !kv->k || !kv->v || !kv->tokens || !kv->pos || !kv->seq_len ||
+      !kv_layout_ok(kv))
+    return CC_ERR_INVALID_ARG;
+  if (kv->kv_format != CC_KV_E4M3_BLOCK) return CC_ERR_UNSUPPORTED;
+  if (!block_size_ok(kv) || !kv->k_exp || !kv->v_exp) return CC_ERR_INVALID_ARG;
+  if ((uint64_t)kv->batch * kv->cap >= (1ull << 31) || kv->batch > 65534 || 2 * c->n_layers > kMaxBlockArrays)
+    return CC_ERR_UNSUPPORTED;
+  for (int l = 0; l < c->n_layers; ++l)
+    for (int i = 0; i < 2; ++i) {
+      void *codes = (i ? kv->v : kv->k)[l], *exps = (i ? kv->v_exp : kv->k_exp)[l];
+      if (!codes) continue;
+      if (!aligned16(codes) || !exps) return CC_ERR_INVALID_ARG;
+      p.codes[p.n_arrays] = reinterpret_cast<uint8_t *>(codes);
+      p.exps[p.n_arrays++] = reinterpret_cast<uint8_t *>(exps);
+    }
+  if (kv->h_last && !aligned16(kv->h_last)) return CC_ERR_INVALID_ARG;
+  p.batch = kv->batch;
+  p.cap = kv->cap;
+  p.hkv = c->n_kv_heads;
+  p.head_dim = c->head_dim;
+  p.block = kv->kv_block;
+  p.pg = kv_layout(c, kv);
+  p.tokens = kv->tokens;
+  p.pos = kv->pos;
+  p.acc = kv->h2o_acc;
+  p.h = reinterpret_cast<uint8_t *>(kv->h_last);
+  p.h_bytes = c->d_model * 2;
+  p.seq_len = kv->seq_len;
+  kv_compact_plan(p);
+  return CC_OK;
+}
+
+}  // namespace
+
+size_t cc_kv_accumulate_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *kv,
+                                       const cc_rows *rows) {
+  if (check_cfg(cfg) != CC_OK || check_step(kv, rows) != CC_OK || rows->n_rows == 0) return 0;
+  return 256;
+}
+
+cc_status cc_kv_accumulate(const cc_model_cfg *cfg, const cc_kv_cache *kv, int32_t layer,
+                           const cc_rows *rows, cc_dtype dtype, int32_t first, int32_t memory_only,
+                           const void *q, int64_t q_ld, const float *lse, void *ws, size_t ws_bytes,
+                           void *stream) {
+  cc_status s = check_cfg(cfg);
+  if (s == CC_OK) s = check_step(kv, rows);
+  if (s == CC_OK) s = check_layer(cfg, kv, layer);
+  if (s != CC_OK) return s;
+  if (kv->kv_format != CC_KV_E4M3_BLOCK || dtype == CC_F32) return CC_ERR_UNSUPPORTED;
+  if (dtype != CC_BF16 && dtype != CC_F16) return CC_ERR_INVALID_ARG;
+  if (!kv->h2o_acc || (first && memory_only)) return CC_ERR_INVALID_ARG;
+  if (rows->n_rows == 0) return CC_OK;
+  if (!rows_ok(cfg, q, q_ld, cfg->n_q_heads, 2) || !lse) return CC_ERR_INVALID_ARG;
+  if (!ws || !aligned16(ws) || ws_bytes < cc_kv_accumulate_workspace_size(cfg, kv, rows))
+    return CC_ERR_WORKSPACE;
+  DevState *dev;
+  if (!dev_state(&dev)) return device_fail();
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  KvReceivedParams p = kv_received_params(cfg, kv, rows, dev->sms);
+  p.memory_only = memory_only ? 1 : 0;
+  p.first = first ? 1 : 0;
+  p.f16 = dtype == CC_F16 ? 1 : 0;
+  p.q = q;
+  p.q_ld = q_ld;
+  p.lse = lse;
+  p.k = reinterpret_cast<const uint8_t *>(kv->k[layer]);
+  p.ke = reinterpret_cast<const uint8_t *>(kv->k_exp[layer]);
+  p.acc = kv->h2o_acc;
+  p.status = dev->status;
+  CC_TRY(wait_kv_ready(kv, layer, layer + 1, st));
+  TimedScope t(CC_KERNEL_KV_ACCUMULATE, st);
+  CC_TRY(launch_kv_received(p, st));
+  return CC_OK;
+}
+
+size_t cc_kv_compact_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *kv) {
+  KvCompactParams p{};
+  return kv_compact_params(cfg, kv, p) == CC_OK ? kv_compact_bytes(p) : 0;
+}
+
+cc_status cc_kv_compact(const cc_model_cfg *cfg, const cc_kv_cache *kv, const int32_t *keep_idx,
+                        const int32_t *keep_count, void *ws, size_t ws_bytes, void *stream) {
+  KvCompactParams p{};
+  const cc_status s = kv_compact_params(cfg, kv, p);
+  if (s != CC_OK) return s;
+  if (!keep_idx || !keep_count) return CC_ERR_INVALID_ARG;
+  if (!ws || !aligned16(ws) || ws_bytes < kv_compact_bytes(p)) return CC_ERR_WORKSPACE;
+  DevState *dev;
+  if (!dev_state(&dev)) return device_fail();
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  kv_compact_bind(p, ws);
+  p.keep_idx = keep_idx;
+  p.keep_count = keep_count;
+  p.status = dev->status;
+  CC_TRY(wait_kv_ready(kv, 0, cfg->n_layers, st));
+  TimedScope t(CC_KERNEL_COMPACT, st);
+  CC_TRY(launch_kv_compact(p, dev->sms, st));
+  return CC_OK;
+}
+
 cc_status cc_kv_advance(const cc_kv_cache *kv, const cc_rows *rows, const int32_t *tokens,
                         void *stream) {
   const cc_status s = check_step(kv, rows);
@@ -2276,7 +2431,7 @@ const char *cc_kernel_name(int32_t kind) {
       "rmsnorm", "embed", "gemm_qrope", "attention", "gemm_oproj", "gemm_gateup", "gemm_down",
       "head_logit", "gemm_lmhead", "lse_combine", "select", "compact", "other",
       "gemm_kv", "attention_causal", "append", "gemm_qkv", "keyattn", "kv_dequant",
-      "kv_append", "kv_attention", "token_logprob"};
+      "kv_append", "kv_attention", "token_logprob", "kv_accumulate", "kv_join"};
   return (kind >= 0 && kind < CC_KERNEL_COUNT) ? names[kind] : "unknown";
 }
 
