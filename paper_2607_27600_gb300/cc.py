@@ -731,7 +731,7 @@ def cc_kv_join(cfg, parts, part_lses, out, lse=None, stream=None):
     k = len(parts)
     if k < 1 or len(part_lses) != k:
         raise ValueError(f"{k} parts with {len(part_lses)} lse")
-    if None in (*parts, *part_lses, out):
+    if any(x is None for x in (*parts, *part_lses, out)):
         raise TypeError("parts, their lse and out must be CUDA tensors")
     n, hq = out.shape[0], c.n_q_heads * c.head_dim
     at = [_row_ptr(x, f"parts[{i}]", n, hq, out.dtype) for i, x in enumerate(parts)]

@@ -2125,8 +2125,16 @@ KvReceivedParams kv_received_params(const cc_model_cfg *c, const cc_kv_cache *kv
   p.hkv = c->n_kv_heads;
   p.head_dim = c->head_dim;
   p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)c->head_dim));
+  const double kappa = (double)p.scale_log2 * sqrt((double)c->head_dim);
+  p.kappa = (float)kappa;
+  p.kappa_lo = (float)(kappa - p.kappa);
   kv_received_plan(p, std::min(sms, kStepMaxSms));
   return p;
+}
+
+// Whether a step's rows take the tiles, as the attention's do.
+bool received_on_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows) {
+  return c->n_q_heads / c->n_kv_heads <= kReceivedMaxGroup && step_on_tiles(c, kv, rows, false);
 }
 
 // The compaction's arrays and units; which of the arguments are wrong.
@@ -2170,7 +2178,8 @@ cc_status kv_compact_params(const cc_model_cfg *c, const cc_kv_cache *kv, KvComp
 size_t cc_kv_accumulate_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *kv,
                                        const cc_rows *rows) {
   if (check_cfg(cfg) != CC_OK || check_step(kv, rows) != CC_OK || rows->n_rows == 0) return 0;
-  return 256;
+  return received_on_tiles(cfg, kv, rows)
+             ? align256(kv_received_part_bytes(kv_received_params(cfg, kv, rows, kStepMaxSms), kStepMaxSms)) : 256;
 }
 
 cc_status cc_kv_accumulate(const cc_model_cfg *cfg, const cc_kv_cache *kv, int32_t layer,
@@ -2204,7 +2213,17 @@ cc_status cc_kv_accumulate(const cc_model_cfg *cfg, const cc_kv_cache *kv, int32
   p.status = dev->status;
   CC_TRY(wait_kv_ready(kv, layer, layer + 1, st));
   TimedScope t(CC_KERNEL_KV_ACCUMULATE, st);
-  CC_TRY(launch_kv_received(p, st));
+  if (received_on_tiles(cfg, kv, rows)) {
+    const int G = p.hq / p.hkv, dh = cfg->head_dim;
+    CUtensorMap tq;
+    const uint64_t dims[3] = {(uint64_t)dh, (uint64_t)p.hq, (uint64_t)rows->n_rows};
+    const uint64_t strides[2] = {(uint64_t)dh * 2, (uint64_t)q_ld * 2};
+    const uint32_t box[3] = {64, (uint32_t)G, (uint32_t)kv_received_positions(G)};
+    if (!make_tmap(&tq, q, 3, dims, strides, box)) return tmap_fail();
+    CC_TRY(launch_kv_received_tiles(p, tq, ws, std::min(dev->sms, kStepMaxSms), st));
+  } else {
+    CC_TRY(launch_kv_received(p, st));
+  }
   return CC_OK;
 }
 

@@ -28,13 +28,7 @@ constexpr int kStep = 16;            // slots of a warp's step
 constexpr int kResident = 2;         // CTAs per SM
 constexpr int kAhead = 3;            // heads of a step in flight per warp
 constexpr int kQueryBytes = 96 * 1024;   // of the queries in shared memory, at most
-constexpr float kLog2e = 1.44269504088896341f;
 
-CC_DEV float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 CC_DEV uint32_t widen2(uint32_t two) {   // e4m3 pair (low 16 bits) -> fp16 pair, exact
   uint32_t r;
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)two));
@@ -97,8 +91,8 @@ CC_DEV int find_step(const KvReceivedParams &p, long long at, long long &before)
 
 // Per query row: what makes its products scores, its log2-sum-exp (+inf where it adds
 // nothing), and the slots that it sees.
-struct RowTerm {
-  float f, y;
+struct __align__(16) RowTerm {
+  float f, y, rest;   // rest: in the log2 domain
   int seen;
 };
 
@@ -183,9 +177,9 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
                 make_uint2(pack_f16x2(x[4 * k] * up, x[4 * k + 1] * up),
                            pack_f16x2(x[4 * k + 2] * up, x[4 * k + 3] * up));
           if (quad == 0) {
-            float y = live ? p.lse[row * p.hq + head] : INFINITY;
-            y = fabsf(y) < INFINITY ? y * kLog2e : INFINITY;
-            r_sh[h * NT * 8 + 8 * t + n8] = {down, y, p.memory_only ? s.seq : s.seq + pos + 1};
+            const RowLse y = row_lse(p, live ? p.lse[row * p.hq + head] : INFINITY);
+            r_sh[h * NT * 8 + 8 * t + n8] = {down, y.y, y.rest * 1.44269504f,
+                                             p.memory_only ? s.seq : s.seq + pos + 1};
           }
         }
         __syncthreads();
@@ -281,7 +275,7 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
                   const bool adds = r.y < INFINITY && e < 256u;
 #pragma unroll
                   for (int k = 0; k < 2; ++k)
-                    if (adds && slot + 8 * k < r.seen) sum[k] += ex2(fmaf(d[2 * k + c], f, -r.y));
+                    if (adds && slot + 8 * k < r.seen) sum[k] += ex2(fmaf(d[2 * k + c], f, -r.y) - r.rest);
                 }
               }
               if (++h == heads) {   // the slots' sums of this pass

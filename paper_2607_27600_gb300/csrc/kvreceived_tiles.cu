@@ -1,0 +1,521 @@
+// kvreceived_tiles.cu -- the attention that the slots of a block-scaled cache receive
+// from chunks of rows (kvreceived.cu has the definition, and few rows).
+//
+// Bound by the tensor cores and, about as much, by the exponentials: with 128 slots
+// as the M rows of a tcgen05 product and 128 query rows as its N, each thread has a slot
+// and adds that slot's own weights, no sum crosses threads, and the slot's scale is
+// a factor of the thread.  The key codes become bf16 (fp16 for fp16 rows; exact, without
+// their scale) once per unit and stay in tensor memory as the A operand; the query
+// tiles stream through shared memory by TMA, each for both of a CTA's slot tiles.
+//
+// A unit is 256 slots of one KV head against all query tiles that see them.  The units
+// of all sequences form one line, each with a little for its start, cut into equal
+// shares, a CTA per share; the sums of a unit that spans shares are added up in share
+// order, then the heads' in theirs (finish_kernel): fixed orders, no atomics.
+//
+//   warps 0-3, 4-7  a slot tile each: codes to tensor memory, then per query tile the
+//                   scores from tensor memory, weights, sums
+//   warp 8          query tiles (TMA) and their rows' log2-sum-exp
+//   warp 9          tensor memory and the products, each slot tile's in turn, in three
+//                   buffers of scores
+//
+// A row's y is its rounded part, which the scores' multiply-add takes off, and a factor
+// e^-rest of its weights.
+#include "kvreceived.cuh"
+
+namespace cc {
+
+namespace {
+
+constexpr int KT = 128;             // slots of a tile, query rows of a tile
+constexpr int kUnitSlots = 2 * KT;
+constexpr int kStages = 4;
+constexpr int kThreads = 320;
+constexpr int kUnitCost = 3;        // of a unit's start, in query tiles
+
+template <int DH>
+struct RtSmem {
+  static constexpr int NH = DH / 64;                   // 64-column (128-byte) halves
+  static constexpr int TILE = NH * KT * 128;
+  static constexpr int OFF_Q = 0;
+  static constexpr int OFF_Y = OFF_Q + kStages * TILE;             // [stage][KT]: -y of each query row
+  static constexpr int OFF_C = OFF_Y + kStages * KT * 4;           // [stage][KT]: 2^-rest
+  static constexpr int OFF_LIVE = OFF_C + kStages * KT * 4;        // [stage]: bit i: columns 32 i ... all add
+  static constexpr int OFF_BAR = OFF_LIVE + kStages * 4;
+  static constexpr int BYTES = OFF_BAR + 256 + 1024;               // barriers + alignment slack
+};
+
+// ---------------------------------------------------------------------------
+// the line of units
+// ---------------------------------------------------------------------------
+struct SeqLine {
+  SeqRows s;
+  int keys;       // slots that some row sees
+  int nk;         // units of a KV head
+  int tiles;      // query tiles of a KV head
+  int nfull;      // units (from the first) that all query tiles see
+};
+CC_DEV SeqLine seq_line(const KvReceivedParams &p, int b) {
+  SeqLine q;
+  q.s = seq_rows(p.rows, b, !p.memory_only);
+  q.keys = q.s.count == 0 ? 0 : q.s.seq + (p.memory_only ? 0 : q.s.count);
+  q.nk = (q.keys + kUnitSlots - 1) / kUnitSlots;
+  q.tiles = (q.s.count + p.P - 1) / p.P;
+  q.nfull = p.memory_only ? q.nk : min(q.nk, (q.s.seq + p.P - 1) / kUnitSlots + 1);
+  return q;
+}
+// The first query tile that sees a slot of unit kt.
+CC_DEV int first_tile(const KvReceivedParams &p, const SeqLine &q, int kt) {
+  return p.memory_only ? 0 : max(0, kt * kUnitSlots - q.s.seq) / p.P;
+}
+CC_DEV long long seq_length(const KvReceivedParams &p, const SeqLine &q) {
+  long long n = (long long)q.nfull * (q.tiles + kUnitCost);
+  for (int kt = q.nfull; kt < q.nk; ++kt) n += q.tiles - first_tile(p, q, kt) + kUnitCost;
+  return n * p.hkv;
+}
+CC_DEV long long line_length(const KvReceivedParams &p) {   // a whole warp calls
+  long long all = 0;
+  for (int b = threadIdx.x & 31; b < p.rows.batch; b += 32) all += seq_length(p, seq_line(p, b));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
+  return all;
+}
+CC_DEV long long length_before(const KvReceivedParams &p, int seq) {   // a whole warp calls
+  long long all = 0;
+  for (int b = threadIdx.x & 31; b < seq; b += 32) all += seq_length(p, seq_line(p, b));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
+  return all;
+}
+__host__ __device__ __forceinline__ int line_shares(int most, long long total) { return total < most ? (int)total : most; }
+CC_DEV int share_at(long long t, long long total, int n) {   // the last c with total * c / n <= t
+  return (int)(((t + 1) * n - 1) / total);
+}
+
+// The pieces of units in a share, in order; every warp walks them for itself.
+struct Pieces {
+  long long at, end, before;   // position, the share's end, the line before sequence b
+  int b;
+  SeqLine q;
+  // the piece: unit kt of KV head g, query tiles [t0, t1); where its sums go
+  int kt, g, t0, t1;
+  bool whole, begins;
+  CC_DEV void start(const KvReceivedParams &p, long long total, int n, int share) {
+    at = total * share / n;
+    end = total * (share + 1) / n;
+    before = 0;
+    // the sequence that holds `at`, 32 at a time
+    const int lane = threadIdx.x & 31;
+    b = 0;
+    for (int b0 = 0; b0 < p.rows.batch; b0 += 32) {
+      const long long w = b0 + lane < p.rows.batch ? seq_length(p, seq_line(p, b0 + lane)) : 0;
+      long long sum = w;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long x = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+        if (lane >= o) sum += x;
+      }
+      const unsigned past = __ballot_sync(0xFFFFFFFFu, before + sum > at);
+      if (past) {
+        const int k = __ffs(past) - 1;
+        before += __shfl_sync(0xFFFFFFFFu, sum - w, k);
+        b = b0 + k;
+        break;
+      }
+      before += __shfl_sync(0xFFFFFFFFu, sum, 31);
+    }
+    q = seq_line(p, b);
+  }
+  CC_DEV bool next(const KvReceivedParams &p) {
+    while (at < end) {
+      long long x = at - before;
+      const int span0 = q.tiles + kUnitCost;
+      const long long full = (long long)q.nfull * p.hkv * span0;
+      int span = span0, unit = 0;
+      t0 = 0;
+      if (x < full) {
+        unit = (int)(x / span0);
+        x -= (long long)unit * span0;
+        kt = unit / p.hkv;
+        g = unit - kt * p.hkv;
+      } else {
+        x -= full;
+        for (kt = q.nfull; kt < q.nk; ++kt) {
+          t0 = first_tile(p, q, kt);
+          span = q.tiles - t0 + kUnitCost;
+          if (x < (long long)span * p.hkv) break;
+          x -= (long long)span * p.hkv;
+        }
+        if (kt >= q.nk) {   // the next sequence
+          before += seq_length(p, q);
+          q = seq_line(p, ++b);
+          continue;
+        }
+        g = (int)(x / span);
+        x -= (long long)g * span;
+      }
+      const int from = (int)x, to = (int)min((long long)span, x + (end - at));
+      at += to - from;
+      begins = from == 0;
+      whole = begins && to == span;
+      t1 = t0 + to - kUnitCost;
+      t0 += max(0, from - kUnitCost);
+      if (t1 > t0) return true;   // (else the share ends before the unit's first tile)
+    }
+    return false;
+  }
+};
+
+// Two e4m3 codes (lo and hi byte of `two`) -> the operand type's pair, exact.  bf16: the code's bits shifted
+// into place make the value times 2^-120 (NaN codes: see where they are found).
+template <bool F16>
+CC_DEV uint32_t widen2(uint32_t two) {
+  uint32_t r;
+  if constexpr (F16) {
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)two));
+  } else {
+    const uint32_t x = __byte_perm(two, 0, 0x1404);   // a byte at the top of each half
+    const uint32_t y = (x & 0x80008000u) | ((x >> 4) & 0x07F007F0u);
+    const uint32_t scale = 0x7B807B80u;               // 2^120, twice
+    const __nv_bfloat162 z = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&y),
+                                     *reinterpret_cast<const __nv_bfloat162 *>(&scale));
+    r = *reinterpret_cast<const uint32_t *>(&z);
+  }
+  return r;
+}
+
+template <int DH, bool F16>
+__global__ void __launch_bounds__(kThreads, 1)
+    received_tiles_kernel(const __grid_constant__ KvReceivedParams p, const __grid_constant__ CUtensorMap tq) {
+  using L = RtSmem<DH>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  float *ny_sh = reinterpret_cast<float *>(smem + L::OFF_Y);
+  float *c_sh = reinterpret_cast<float *>(smem + L::OFF_C);
+  volatile uint32_t *live_sh = reinterpret_cast<volatile uint32_t *>(smem + L::OFF_LIVE);
+  uint64_t *q_full = reinterpret_cast<uint64_t *>(smem + L::OFF_BAR);   // [kStages]
+  uint64_t *q_empty = q_full + kStages;                                 // [kStages]
+  uint64_t *s_full = q_empty + kStages;                                 // [3]
+  uint64_t *s_empty = s_full + 3;                                       // [3]
+  uint64_t *a_full = s_empty + 3;                                       // [2]
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(a_full + 2);
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+
+  pdl_trigger();   // the finish may launch: it waits for this grid
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long total = line_length(p);
+  const int n = line_shares(p.shares, total), share = blockIdx.x;
+  if (share == 0)   // reported once: sequences whose rows or lengths are bad
+    for (int b = threadIdx.x; b < p.rows.batch; b += kThreads)
+      if (!seq_rows(p.rows, b, !p.memory_only).ok) set_status(p.status, CC_ERR_DEVICE_ARG);
+  if (share >= n) return;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&q_full[s], 1);
+      mbar_init(&q_empty[s], 1 + 8);   // the products, and the warps that read the terms
+    }
+    for (int i = 0; i < 3; ++i) {
+      mbar_init(&s_full[i], 1);
+      mbar_init(&s_empty[i], 4);
+    }
+    for (int i = 0; i < 2; ++i) mbar_init(&a_full[i], 4);
+    *abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == 9) tmem_alloc(tmem_slot, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const int G = p.hq / p.hkv;
+  Pieces u;
+  u.start(p, total, n, share);
+
+  if (warp == 8) {
+    // ------------------------------------------------ query tiles and their rows' terms
+    if (lane == 0) tma_prefetch_desc(&tq);
+    int it = 0;
+    bool ok = true;
+    while (ok && u.next(p)) {
+      for (int t = u.t0; t < u.t1; ++t, ++it) {
+        const int s = it % kStages, row0 = u.q.s.r0 + t * p.P;
+        float lse[KT / 32];
+#pragma unroll
+        for (int i = 0; i < KT / 32; ++i) {
+          const int col = lane + 32 * i, pos = col / G;
+          const bool there = pos < p.P && t * p.P + pos < u.q.s.count;
+          lse[i] = there ? p.lse[(long long)(row0 + pos) * p.hq + u.g * G + col - pos * G] : INFINITY;
+        }
+        if (!(ok = mbar_wait(&q_empty[s], ((it / kStages) & 1) ^ 1, abort_flag, p.status))) break;
+        uint32_t live = 0;
+#pragma unroll
+        for (int i = 0; i < KT / 32; ++i) {
+          const RowLse y = row_lse(p, lse[i]);
+          ny_sh[s * KT + lane + 32 * i] = -y.y;
+          c_sh[s * KT + lane + 32 * i] = 1.f - y.rest + 0.5f * y.rest * y.rest;   // e^-rest, a small one
+          live |= (__all_sync(0xFFFFFFFFu, y.y < INFINITY) ? 1u : 0u) << i;
+        }
+        if (lane == 0) live_sh[s] = live;
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive_expect_tx(&q_full[s], (uint32_t)(L::NH * p.P * G * 128));
+          for (int h = 0; h < L::NH; ++h)
+            tma_load_3d(smem + L::OFF_Q + s * L::TILE + h * KT * 128, &tq, &q_full[s], h * 64, u.g * G, row0);
+        }
+      }
+    }
+  } else if (warp == 9) {
+    // ------------------------------------------------------------- products
+    constexpr uint32_t idesc = F16 ? make_idesc_f16(128, KT, 0, 0) : make_idesc_bf16(128, KT, 0, 0);
+    int it = 0;
+    unsigned job = 0, filled[2] = {0, 0};   // times that a slot tile's operand was
+    bool ok = true;
+    while (ok && u.next(p)) {
+      const int tiles2 = u.q.keys - u.kt * kUnitSlots > KT ? 2 : 1;   // slot tiles of the unit
+      if (lane == 0)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (ok && i < tiles2) ok = mbar_wait(&a_full[i], filled[i]++ & 1, abort_flag, p.status);
+      for (int t = u.t0; t < u.t1; ++t, ++it) {
+        if (lane == 0 && ok) {
+          const int s = it % kStages;
+          ok = mbar_wait(&q_full[s], (it / kStages) & 1, abort_flag, p.status);
+          const uint64_t qd = make_sdesc_sw128(smem_u32(smem + L::OFF_Q + s * L::TILE), 16, 1024);
+          for (int i = 0; ok && i < tiles2; ++i) {
+            const unsigned j = job + i;
+            if (!(ok = mbar_wait(&s_empty[j % 3], ((j / 3) & 1) ^ 1, abort_flag, p.status))) break;
+            tc_fence_after();
+#pragma unroll
+            for (int kk = 0; kk < DH / 16; ++kk)
+              umma_ts(tmem + 128 + (j % 3) * KT, tmem + i * 64 + kk * 8,
+                      qd + (uint64_t)((((kk >> 2) * KT * 128) >> 4) + (kk & 3) * 2), idesc, kk > 0);
+            umma_commit(&s_full[j % 3]);
+          }
+          if (ok) umma_commit(&q_empty[s]);
+        }
+        job += tiles2;
+      }
+      ok = __shfl_sync(0xFFFFFFFFu, ok ? 1 : 0, 0) != 0;
+    }
+  } else {
+    // ------------------------------------------------------ slots, one per thread
+    const int w = warp >> 2;   // which slot tile of the unit
+    const int r = (warp & 3) * 32 + lane;
+    const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
+    const int hs = p.pg.head_major ? 1 : p.hkv, log_block = 31 - __clz(p.block);
+    int it = 0;
+    unsigned job = 0;
+    bool ok = true;
+    while (ok && u.next(p)) {
+      const int tiles2 = u.q.keys - u.kt * kUnitSlots > KT ? 2 : 1;
+      const int slot0 = u.kt * kUnitSlots + w * KT, slot = slot0 + r;
+      float f = 0.f, sum = 0.f;
+      bool page = true;
+      if (w < tiles2) {
+        // ---- the slot's codes, its scale a factor of its scores
+        uint32_t code[DH / 4];
+#pragma unroll
+        for (int i = 0; i < DH / 4; ++i) code[i] = 0;
+        if (slot < u.q.keys) {
+          const long long row = p.pg.head_major ? ((long long)u.b * p.hkv + u.g) * p.rows.cap + slot
+                                                : kv_row(p.pg, p.rows.cap, u.b, slot);
+          page = row >= 0;
+          if (page) {
+            const int gs = p.pg.head_major ? 0 : u.g;
+            const uint4 *src = reinterpret_cast<const uint4 *>(p.k + (row * hs + gs) * DH);
+#pragma unroll
+            for (int i = 0; i < DH / 16; ++i) *reinterpret_cast<uint4 *>(&code[4 * i]) = __ldg(src + i);
+            const uint32_t e = p.ke[(row >> log_block) * hs + gs];
+            const float scale = __uint_as_float(e << 23);
+            f = p.scale_log2 * fmaf(scale, 0.f, scale);   // (e = 255: NaN)
+          } else {
+            set_status(p.status, CC_ERR_DEVICE_ARG);
+          }
+        }
+        if constexpr (!F16) {   // a NaN code: every score of the slot is none
+          uint32_t any = 0;
+#pragma unroll
+          for (int i = 0; i < DH / 4; ++i) any |= __vcmpeq4(code[i] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+          if (any) f = NAN;
+        }
+        const uint32_t a_t = tmem + lanes + w * 64;
+#pragma unroll
+        for (int h = 0; h < DH / 64; ++h) {
+          uint32_t a[32];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            a[2 * i] = widen2<F16>(code[h * 16 + i] & 0xFFFFu);
+            a[2 * i + 1] = widen2<F16>(code[h * 16 + i] >> 16);
+          }
+          tmem_st32(a_t + h * 32, a);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&a_full[w]);
+      }
+      float2 acc[4] = {};
+      for (int t = u.t0; t < u.t1; ++t, ++it) {
+        const int s = it % kStages;
+        // the tile's terms; also where the unit has no second tile of slots: an arrival counts for its phase
+        if (!(ok = mbar_wait(&q_full[s], (it / kStages) & 1, abort_flag, p.status))) break;
+        if (w < tiles2) {
+          const unsigned j = job + w;
+          if (!(ok = mbar_wait(&s_full[j % 3], (j / 3) & 1, abort_flag, p.status))) break;
+          tc_fence_after();
+          uint32_t sr[KT];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            tmem_ld32(tmem + lanes + 128 + (j % 3) * KT + 32 * i, *reinterpret_cast<uint32_t(*)[32]>(&sr[32 * i]));
+          tmem_ld_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&s_empty[j % 3]);   // copied out: the buffer may be refilled
+          const float4 *ny = reinterpret_cast<const float4 *>(ny_sh + s * KT);
+          const float4 *cs = reinterpret_cast<const float4 *>(c_sh + s * KT);
+          // rows that see the slot: columns from `from` on
+          const int ahead = p.memory_only ? 0 : slot - u.q.s.seq - t * p.P;
+          const int from = ahead * G;
+          const bool all = p.memory_only || slot0 + KT - 1 <= u.q.s.seq + t * p.P;   // uniform: every slot of the tile
+          const uint32_t live = all ? live_sh[s] : 0u;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if ((live >> i) & 1u) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const float4 y = ny[8 * i + k], c = cs[8 * i + k];
+                const int col = 32 * i + 4 * k;
+                float2 x = __ffma2_rn(make_float2(__uint_as_float(sr[col]), __uint_as_float(sr[col + 1])),
+                                      make_float2(f, f), make_float2(y.x, y.y));
+                acc[k & 3] = __ffma2_rn(make_float2(ex2(x.x), ex2(x.y)), make_float2(c.x, c.y), acc[k & 3]);
+                x = __ffma2_rn(make_float2(__uint_as_float(sr[col + 2]), __uint_as_float(sr[col + 3])),
+                               make_float2(f, f), make_float2(y.z, y.w));
+                acc[k & 3] = __ffma2_rn(make_float2(ex2(x.x), ex2(x.y)), make_float2(c.z, c.w), acc[k & 3]);
+              }
+            } else {
+#pragma unroll
+              for (int k = 0; k < 32; ++k) {
+                const int col = 32 * i + k;
+                const float y = ny_sh[s * KT + col];
+                const float e = ex2(fmaf(__uint_as_float(sr[col]), f, y)) * c_sh[s * KT + col];
+                acc[k & 3].x += y > -INFINITY && col >= from ? e : 0.f;
+              }
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&q_empty[s]);   // the terms are read
+        job += tiles2;
+      }
+      if (ok && w < tiles2 && slot < u.q.keys) {
+        sum = ((acc[0].x + acc[0].y) + (acc[1].x + acc[1].y)) + ((acc[2].x + acc[2].y) + (acc[3].x + acc[3].y));
+        if (!page) sum = 0.f;
+        if (u.whole)
+          p.part[((long long)u.g * p.rows.batch + u.b) * p.rows.cap + slot] = sum;
+        else
+          p.cut[(2 * share + (u.begins ? 1 : 0)) * kUnitSlots + w * KT + r] = sum;
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) __nanosleep(1000000);   // let copies still in flight land
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// acc[b][j] += the heads' sums in order; a unit that spans shares is the sum of its pieces.
+__global__ void __launch_bounds__(kUnitSlots) finish_kernel(const __grid_constant__ KvReceivedParams p) {
+  // of each KV head's unit: the first share with query tiles of it (-1: it lies in one), the last
+  __shared__ int first_sh[kUnitSlots], last_sh[kUnitSlots];
+  pdl_wait();
+  const int per_seq = (p.rows.cap + kUnitSlots - 1) / kUnitSlots, tid = threadIdx.x;
+  const int b = blockIdx.x / per_seq, kt = blockIdx.x - b * per_seq;
+  const SeqLine q = seq_line(p, b);
+  if (kt >= q.nk) return;
+  const long long total = line_length(p), before = length_before(p, b);
+  const int n = line_shares(p.shares, total);
+  const int slot = kt * kUnitSlots + tid;
+  float sum = 0.f;
+  for (int g0 = 0; g0 < p.hkv; g0 += kUnitSlots) {
+    __syncthreads();
+    if (g0 + tid < p.hkv) {
+      const int g = g0 + tid;
+      const int span0 = q.tiles + kUnitCost;
+      int span = span0;
+      long long at = before;
+      if (kt < q.nfull) {
+        at += ((long long)kt * p.hkv + g) * span0;
+      } else {
+        at += (long long)q.nfull * p.hkv * span0;
+        for (int k = q.nfull; k < kt; ++k) at += (long long)(q.tiles - first_tile(p, q, k) + kUnitCost) * p.hkv;
+        span = q.tiles - first_tile(p, q, kt) + kUnitCost;
+        at += (long long)g * span;
+      }
+      const int c0 = share_at(at, total, n);
+      int lo = c0;
+      const int c1 = share_at(at + span - 1, total, n);
+      // (shares that end before the first query tile have no sums)
+      while (lo < c1 && total * (lo + 1) / n - at <= kUnitCost) ++lo;
+      first_sh[tid] = c0 == c1 ? -1 : lo * 2 + (lo == c0 ? 1 : 0);
+      last_sh[tid] = c1;
+    }
+    __syncthreads();
+    if (slot < q.keys)
+      for (int i = 0; i < min(kUnitSlots, p.hkv - g0); ++i) {
+        const int first = first_sh[i];   // share, and whether the unit begins there
+        if (first < 0) {
+          sum += p.part[((long long)(g0 + i) * p.rows.batch + b) * p.rows.cap + slot];
+          continue;
+        }
+        float x = p.cut[first * kUnitSlots + tid];
+        for (int c = first / 2 + 1; c <= last_sh[i]; ++c) x += p.cut[2 * c * kUnitSlots + tid];
+        sum += x;
+      }
+  }
+  if (slot < q.keys) {
+    float *dst = p.acc + (long long)b * p.rows.cap + slot;
+    *dst = (p.first && slot >= q.s.seq ? 0.f : *dst) + sum;
+  }
+}
+
+template <int DH, bool F16>
+cudaError_t launch(const KvReceivedParams &p, const CUtensorMap &tq, cudaStream_t st) {
+  static bool attr_set[64] = {};
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (dev < 64 && !attr_set[dev]) {
+    const cudaError_t e = cudaFuncSetAttribute(received_tiles_kernel<DH, F16>,
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize, RtSmem<DH>::BYTES);
+    if (e != cudaSuccess) return e;
+    attr_set[dev] = true;
+  }
+  received_tiles_kernel<DH, F16><<<p.shares, kThreads, RtSmem<DH>::BYTES, st>>>(p, tq);
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  const unsigned blocks = (unsigned)((p.rows.cap + kUnitSlots - 1) / kUnitSlots) * (unsigned)p.rows.batch;
+  return launch_pdl(finish_kernel, dim3(blocks), dim3(kUnitSlots), 0, st, p);
+}
+
+}  // namespace
+
+int kv_received_positions(int group) { return KT / group; }
+
+size_t kv_received_part_bytes(const KvReceivedParams &p, int sms) {
+  return (size_t)p.hkv * p.rows.batch * p.rows.cap * 4 + (size_t)sms * 2 * kUnitSlots * 4;
+}
+
+cudaError_t launch_kv_received_tiles(KvReceivedParams p, const CUtensorMap &tq, void *ws, int sms, cudaStream_t st) {
+  p.P = kv_received_positions(p.hq / p.hkv);
+  p.shares = sms;
+  p.cut = reinterpret_cast<float *>(ws);
+  p.part = p.cut + (size_t)sms * 2 * kUnitSlots;
+  if (p.head_dim == 128) return p.f16 ? launch<128, true>(p, tq, st) : launch<128, false>(p, tq, st);
+  return p.f16 ? launch<64, true>(p, tq, st) : launch<64, false>(p, tq, st);
+}
+
+}  // namespace cc

@@ -159,6 +159,36 @@ def test_rows_without_a_finite_lse_add_nothing(pkg, counts, dtype):
     assert (got[:, :30] < whole[:, :30]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("counts", [[1], [130]])
+def test_every_code(pkg, counts, dtype):
+    """All codes that are numbers, the least ones under a scale that makes them count."""
+    c = Case(pkg, 9, 4, 1, 128, 16, "slot", dtype, 512, [320], counts)
+    numbers = np.array([x for x in range(256) if x & 0x7F != 0x7F], np.uint8)
+    c.codes["k"][0, :, 0] = c.rng.choice(numbers, c.codes["k"][0, :, 0].shape)
+    c.codes["k"][0, :160, 0] &= 0x87          # subnormal ones
+    c.exps["k"][:] = 118
+    c.exps["k"][0, :10] = 132
+    c.k = values(c.codes["k"], c.exps["k"])
+    _, lse, _ = oracle.attend_rows(c.q, c.k, c.k * 0, c.lens, c.start)
+    c.lse = lse.astype(np.float32)
+    c.c = DeviceCache(c.pkg, c.codes, c.exps, c.lens, "slot")
+    c.check(c.run())
+
+
+def test_not_a_number_under_a_finite_lse(pkg):
+    """A slot that is no number with an lse that knows nothing of it: its total is NaN, no other."""
+    for counts in ([1], [130]):
+        for dtype in TYPES:
+            c = Case(pkg, 10, 4, 2, 64, 16, "slot", dtype, 256, [100], counts)
+            c.codes["k"][0, 20, 1, 5] = 0xFF
+            c.c = DeviceCache(c.pkg, c.codes, c.exps, c.lens, "slot")
+            got = c.run()
+            assert np.isnan(got[0, 20])
+            got[0, 20] = c.want()[0][0, 20]
+            c.check(got)
+
+
 def test_scales_that_are_none(pkg):
     """An exponent of 0 makes scores of 0; rows that see one of 255 come without an lse."""
     c = Case(pkg, 5, 4, 2, 128, 16, "paged", "bf16", 256, [100, 60], [1, 3])
