@@ -15,9 +15,10 @@
 //
 //   warps 0-3, 4-7  a slot tile each: codes to tensor memory, then per query tile the
 //                   scores from tensor memory, weights, sums
-//   warp 8          query tiles (TMA) and their rows' log2-sum-exp
+//   warp 8          query tiles (TMA)
 //   warp 9          tensor memory and the products, each slot tile's in turn, in three
 //                   buffers of scores
+//   warps 10, 11    the rows' terms, a query tile each in turn
 //
 // A row's y is its rounded part, which the scores' multiply-add takes off, and a factor
 // e^-rest of its weights.
@@ -30,7 +31,10 @@ namespace {
 constexpr int KT = 128;             // slots of a tile, query rows of a tile
 constexpr int kUnitSlots = 2 * KT;
 constexpr int kStages = 4;
-constexpr int kThreads = 320;
+constexpr int kThreads = 384;
+// Registers of a launch's 384 threads at 168 shared out anew between its three warpgroups.
+constexpr int kRegsSlots = 216, kRegsOthers = 72;
+static_assert(2 * kRegsSlots + kRegsOthers <= 3 * 168, "more registers than the block is launched with");
 constexpr int kUnitCost = 3;        // of a unit's start, in query tiles
 
 template <int DH>
@@ -38,9 +42,9 @@ struct RtSmem {
   static constexpr int NH = DH / 64;                   // 64-column (128-byte) halves
   static constexpr int TILE = NH * KT * 128;
   static constexpr int OFF_Q = 0;
-  static constexpr int OFF_Y = OFF_Q + kStages * TILE;             // [stage][KT]: -y of each query row
-  static constexpr int OFF_C = OFF_Y + kStages * KT * 4;           // [stage][KT]: 2^-rest
-  static constexpr int OFF_LIVE = OFF_C + kStages * KT * 4;        // [stage]: bit i: columns 32 i ... all add
+  // [stage][KT / 2] float4: of two query rows -y, -y, e^-rest, e^-rest
+  static constexpr int OFF_TERM = OFF_Q + kStages * TILE;
+  static constexpr int OFF_LIVE = OFF_TERM + kStages * KT * 8;     // [stage]: bit i: columns 32 i ... all add
   static constexpr int OFF_BAR = OFF_LIVE + kStages * 4;
   static constexpr int BYTES = OFF_BAR + 256 + 1024;               // barriers + alignment slack
 };
@@ -190,8 +194,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   using L = RtSmem<DH>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  float *ny_sh = reinterpret_cast<float *>(smem + L::OFF_Y);
-  float *c_sh = reinterpret_cast<float *>(smem + L::OFF_C);
+  float4 *term_sh = reinterpret_cast<float4 *>(smem + L::OFF_TERM);
   volatile uint32_t *live_sh = reinterpret_cast<volatile uint32_t *>(smem + L::OFF_LIVE);
   uint64_t *q_full = reinterpret_cast<uint64_t *>(smem + L::OFF_BAR);   // [kStages]
   uint64_t *q_empty = q_full + kStages;                                 // [kStages]
@@ -199,6 +202,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t *s_empty = s_full + 3;                                       // [3]
   uint64_t *a_full = s_empty + 3;                                       // [2]
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(a_full + 2);
+  __shared__ Pieces walk_sh[8];
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
 
   pdl_trigger();   // the finish may launch: it waits for this grid
@@ -212,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&q_full[s], 1);
+      mbar_init(&q_full[s], 2);   // the copies, the terms
       mbar_init(&q_empty[s], 1 + 8);   // the products, and the warps that read the terms
     }
     for (int i = 0; i < 3; ++i) {
@@ -232,38 +236,71 @@ __global__ void __launch_bounds__(kThreads, 1)
   Pieces u;
   u.start(p, total, n, share);
 
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOthers));
   if (warp == 8) {
-    // ------------------------------------------------ query tiles and their rows' terms
+    // ----------------------------------------------------------- query tiles
     if (lane == 0) tma_prefetch_desc(&tq);
     int it = 0;
     bool ok = true;
     while (ok && u.next(p)) {
-      for (int t = u.t0; t < u.t1; ++t, ++it) {
-        const int s = it % kStages, row0 = u.q.s.r0 + t * p.P;
+      if (lane == 0)
+        for (int t = u.t0; ok && t < u.t1; ++t, ++it) {
+          const int s = it % kStages;
+          if (!(ok = mbar_wait(&q_empty[s], ((it / kStages) & 1) ^ 1, abort_flag, p.status))) break;
+          mbar_arrive_expect_tx(&q_full[s], (uint32_t)(L::NH * p.P * G * 128));
+          for (int h = 0; h < L::NH; ++h)
+            tma_load_3d(smem + L::OFF_Q + s * L::TILE + h * KT * 128, &tq, &q_full[s], h * 64, u.g * G,
+                        u.q.s.r0 + t * p.P);
+        }
+      ok = __shfl_sync(0xFFFFFFFFu, ok ? 1 : 0, 0) != 0;
+    }
+  } else if (warp >= 10) {
+    // ------------------- the rows' terms, every other tile; their loads a tile of this warp's ahead
+    int pos[KT / 32], at[KT / 32];
+#pragma unroll
+    for (int i = 0; i < KT / 32; ++i) {
+      const int col = lane + 32 * i;
+      pos[i] = col / G;
+      at[i] = pos[i] * p.hq + col - pos[i] * G;
+      if (pos[i] >= p.P) pos[i] = 0x40000000;   // no row
+    }
+    int it = 0;
+    bool ok = true;
+    while (ok && u.next(p)) {
+      const float *src = p.lse + (long long)u.q.s.r0 * p.hq + u.g * G;
+      float next[KT / 32];
+      auto load = [&](int t) {
+        const int left = u.q.s.count - t * p.P;   // rows of the tile and on
+#pragma unroll
+        for (int i = 0; i < KT / 32; ++i)
+          next[i] = t < u.t1 && pos[i] < left ? __ldg(src + (long long)t * p.P * p.hq + at[i]) : INFINITY;
+      };
+      int t = u.t0 + ((warp - 10 - it) & 1);
+      it += t - u.t0;
+      load(t);
+      for (; t < u.t1; t += 2, it += 2) {
+        const int s = it % kStages;
         float lse[KT / 32];
 #pragma unroll
-        for (int i = 0; i < KT / 32; ++i) {
-          const int col = lane + 32 * i, pos = col / G;
-          const bool there = pos < p.P && t * p.P + pos < u.q.s.count;
-          lse[i] = there ? p.lse[(long long)(row0 + pos) * p.hq + u.g * G + col - pos * G] : INFINITY;
-        }
+        for (int i = 0; i < KT / 32; ++i) lse[i] = next[i];
+        load(t + 2);
         if (!(ok = mbar_wait(&q_empty[s], ((it / kStages) & 1) ^ 1, abort_flag, p.status))) break;
         uint32_t live = 0;
 #pragma unroll
         for (int i = 0; i < KT / 32; ++i) {
           const RowLse y = row_lse(p, lse[i]);
-          ny_sh[s * KT + lane + 32 * i] = -y.y;
-          c_sh[s * KT + lane + 32 * i] = 1.f - y.rest + 0.5f * y.rest * y.rest;   // e^-rest, a small one
+          const int col = lane + 32 * i;
+          float *term = reinterpret_cast<float *>(term_sh + s * (KT / 2) + col / 2) + (col & 1);
+          term[0] = -y.y;
+          term[2] = 1.f - y.rest + 0.5f * y.rest * y.rest;   // e^-rest, a small one
           live |= (__all_sync(0xFFFFFFFFu, y.y < INFINITY) ? 1u : 0u) << i;
         }
         if (lane == 0) live_sh[s] = live;
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive_expect_tx(&q_full[s], (uint32_t)(L::NH * p.P * G * 128));
-          for (int h = 0; h < L::NH; ++h)
-            tma_load_3d(smem + L::OFF_Q + s * L::TILE + h * KT * 128, &tq, &q_full[s], h * 64, u.g * G, row0);
-        }
+        if (lane == 0) mbar_arrive(&q_full[s]);
       }
+      it -= t - u.t1;   // (t is t1, or t1 + 1)
     }
   } else if (warp == 9) {
     // ------------------------------------------------------------- products
@@ -298,38 +335,55 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       ok = __shfl_sync(0xFFFFFFFFu, ok ? 1 : 0, 0) != 0;
     }
+  }
   } else {
-    // ------------------------------------------------------ slots, one per thread
-    const int w = warp >> 2;   // which slot tile of the unit
-    const int r = (warp & 3) * 32 + lane;
+    // ------------------------------------------------------ slots and their weights
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSlots));
+    const int w = warp >> 2;                // slot tile of the unit
+    const int r = (warp & 3) * 32 + lane;   // slot whose codes this thread widens
     const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
     const int hs = p.pg.head_major ? 1 : p.hkv, log_block = 31 - __clz(p.block);
+    const int mine = lane >> 2, quad = lane & 3;
     int it = 0;
     unsigned job = 0;
     bool ok = true;
-    while (ok && u.next(p)) {
+    // (between pieces the walk waits in shared memory: its registers are needed)
+    if (lane == 0) walk_sh[warp] = u;
+    while (ok) {
+      __syncwarp();
+      Pieces u = walk_sh[warp];
+      if (!u.next(p)) break;
+      __syncwarp();
+      if (lane == 0) walk_sh[warp] = u;
       const int tiles2 = u.q.keys - u.kt * kUnitSlots > KT ? 2 : 1;
+      if (w >= tiles2) {   // no second tile of slots: an arrival for each phase all the same
+        for (int t = u.t0; ok && t < u.t1; ++t, ++it) {
+          ok = mbar_wait(&q_full[it % kStages], (it / kStages) & 1, abort_flag, p.status);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&q_empty[it % kStages]);
+        }
+        job += u.t1 - u.t0;
+        continue;
+      }
       const int slot0 = u.kt * kUnitSlots + w * KT, slot = slot0 + r;
-      float f = 0.f, sum = 0.f;
-      bool page = true;
-      if (w < tiles2) {
-        // ---- the slot's codes, its scale a factor of its scores
+      // ---- the slot's codes, its scale a factor of its scores (-1: there is no such page)
+      float f = 0.f;
+      {
         uint32_t code[DH / 4];
 #pragma unroll
         for (int i = 0; i < DH / 4; ++i) code[i] = 0;
         if (slot < u.q.keys) {
           const long long row = p.pg.head_major ? ((long long)u.b * p.hkv + u.g) * p.rows.cap + slot
                                                 : kv_row(p.pg, p.rows.cap, u.b, slot);
-          page = row >= 0;
-          if (page) {
+          if (row >= 0) {
             const int gs = p.pg.head_major ? 0 : u.g;
             const uint4 *src = reinterpret_cast<const uint4 *>(p.k + (row * hs + gs) * DH);
 #pragma unroll
             for (int i = 0; i < DH / 16; ++i) *reinterpret_cast<uint4 *>(&code[4 * i]) = __ldg(src + i);
-            const uint32_t e = p.ke[(row >> log_block) * hs + gs];
-            const float scale = __uint_as_float(e << 23);
+            const float scale = __uint_as_float((uint32_t)p.ke[(row >> log_block) * hs + gs] << 23);
             f = p.scale_log2 * fmaf(scale, 0.f, scale);   // (e = 255: NaN)
           } else {
+            f = -1.f;
             set_status(p.status, CC_ERR_DEVICE_ARG);
           }
         }
@@ -339,7 +393,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int i = 0; i < DH / 4; ++i) any |= __vcmpeq4(code[i] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
           if (any) f = NAN;
         }
-        const uint32_t a_t = tmem + lanes + w * 64;
 #pragma unroll
         for (int h = 0; h < DH / 64; ++h) {
           uint32_t a[32];
@@ -348,73 +401,97 @@ __global__ void __launch_bounds__(kThreads, 1)
             a[2 * i] = widen2<F16>(code[h * 16 + i] & 0xFFFFu);
             a[2 * i + 1] = widen2<F16>(code[h * 16 + i] >> 16);
           }
-          tmem_st32(a_t + h * 32, a);
+          tmem_st32(tmem + lanes + w * 64 + h * 32, a);
         }
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&a_full[w]);
       }
-      float2 acc[4] = {};
-      for (int t = u.t0; t < u.t1; ++t, ++it) {
+      // ---- a lane has the weights of four slots (8 apart) and every fourth pair of rows, so that a
+      // row's terms are read once for four
+      float2 fs[4], acc[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        fs[i].x = fs[i].y = __shfl_sync(0xFFFFFFFFu, f, mine + 8 * i);
+        acc[i] = make_float2(0.f, 0.f);
+      }
+      unsigned j = job + w;
+      for (int t = u.t0; t < u.t1; ++t, ++it, j += tiles2) {
         const int s = it % kStages;
-        // the tile's terms; also where the unit has no second tile of slots: an arrival counts for its phase
-        if (!(ok = mbar_wait(&q_full[s], (it / kStages) & 1, abort_flag, p.status))) break;
-        if (w < tiles2) {
-          const unsigned j = job + w;
-          if (!(ok = mbar_wait(&s_full[j % 3], (j / 3) & 1, abort_flag, p.status))) break;
-          tc_fence_after();
-          uint32_t sr[KT];
+        if (!(ok = mbar_wait(&q_full[s], (it / kStages) & 1, abort_flag, p.status) &&
+                   mbar_wait(&s_full[j % 3], (j / 3) & 1, abort_flag, p.status)))
+          break;
+        tc_fence_after();
+        uint32_t sr[4][2][16];   // of 32 columns each: slots 0 - 15 and 16 - 31 of the warp's
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t at = tmem + lanes + 128 + (j % 3) * KT + 32 * c;
+          tmem_ld_rows16(at, sr[c][0]);
+          tmem_ld_rows16(at + (16u << 16), sr[c][1]);
+        }
+        const float4 *terms = term_sh + s * (KT / 2) + quad;
+        const uint32_t live = live_sh[s];   // bit c: every row of columns 32 c ... adds
+        const int seen_first = p.memory_only ? 0x7FFFFFFF : u.q.s.seq + t * p.P;   // last slot that the tile's first row sees
+        tmem_ld_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s_empty[j % 3]);   // copied out: the buffer may be refilled
+        if (live == 15u && slot0 + KT - 1 <= seen_first) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float4 y = terms[16 * c + 4 * k];   // of two columns -y and e^-rest
+              float2 x[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t *x2 = &sr[c][i >> 1][4 * k + 2 * (i & 1)];
+                x[i] = __ffma2_rn(make_float2(__uint_as_float(x2[0]), __uint_as_float(x2[1])), fs[i], make_float2(y.x, y.y));
+              }
+#pragma unroll
+              for (int i = 0; i < 4; ++i) x[i] = make_float2(ex2(x[i].x), ex2(x[i].y));
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[i] = __ffma2_rn(x[i], make_float2(y.z, y.w), acc[i]);
+            }
+        } else if (p.memory_only || slot0 <= seen_first + p.P - 1) {   // (some row sees some slot)
+          int from[4];   // of the lane's columns (8 k, and 8 k + 1, of each 32), the first that sees the slot
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            tmem_ld32(tmem + lanes + 128 + (j % 3) * KT + 32 * i, *reinterpret_cast<uint32_t(*)[32]>(&sr[32 * i]));
-          tmem_ld_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&s_empty[j % 3]);   // copied out: the buffer may be refilled
-          const float4 *ny = reinterpret_cast<const float4 *>(ny_sh + s * KT);
-          const float4 *cs = reinterpret_cast<const float4 *>(c_sh + s * KT);
-          // rows that see the slot: columns from `from` on
-          const int ahead = p.memory_only ? 0 : slot - u.q.s.seq - t * p.P;
-          const int from = ahead * G;
-          const bool all = p.memory_only || slot0 + KT - 1 <= u.q.s.seq + t * p.P;   // uniform: every slot of the tile
-          const uint32_t live = all ? live_sh[s] : 0u;
+            from[i] = p.memory_only ? -1 : (slot0 + (warp & 3) * 32 + mine + 8 * i - seen_first) * G - 2 * quad;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if ((live >> i) & 1u) {
+          for (int c = 0; c < 4; ++c)
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const float4 y = ny[8 * i + k], c = cs[8 * i + k];
-                const int col = 32 * i + 4 * k;
-                float2 x = __ffma2_rn(make_float2(__uint_as_float(sr[col]), __uint_as_float(sr[col + 1])),
-                                      make_float2(f, f), make_float2(y.x, y.y));
-                acc[k & 3] = __ffma2_rn(make_float2(ex2(x.x), ex2(x.y)), make_float2(c.x, c.y), acc[k & 3]);
-                x = __ffma2_rn(make_float2(__uint_as_float(sr[col + 2]), __uint_as_float(sr[col + 3])),
-                               make_float2(f, f), make_float2(y.z, y.w));
-                acc[k & 3] = __ffma2_rn(make_float2(ex2(x.x), ex2(x.y)), make_float2(c.z, c.w), acc[k & 3]);
-              }
-            } else {
+            for (int k = 0; k < 4; ++k) {
+              const float4 y = terms[16 * c + 4 * k];
+              const int col = 32 * c + 8 * k;
 #pragma unroll
-              for (int k = 0; k < 32; ++k) {
-                const int col = 32 * i + k;
-                const float y = ny_sh[s * KT + col];
-                const float e = ex2(fmaf(__uint_as_float(sr[col]), f, y)) * c_sh[s * KT + col];
-                acc[k & 3].x += y > -INFINITY && col >= from ? e : 0.f;
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t *x2 = &sr[c][i >> 1][4 * k + 2 * (i & 1)];
+                // (chosen, not multiplied by 0: what a row does not see, or one that adds nothing, may be no number)
+                const float x0 = col >= from[i] && y.x > -INFINITY ? fmaf(__uint_as_float(x2[0]), fs[i].x, y.x) : -INFINITY;
+                const float x1 = col + 1 >= from[i] && y.y > -INFINITY ? fmaf(__uint_as_float(x2[1]), fs[i].x, y.y) : -INFINITY;
+                acc[i] = __ffma2_rn(make_float2(ex2(x0), ex2(x1)), make_float2(y.z, y.w), acc[i]);
               }
             }
-          }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&q_empty[s]);   // the terms are read
-        job += tiles2;
       }
-      if (ok && w < tiles2 && slot < u.q.keys) {
-        sum = ((acc[0].x + acc[0].y) + (acc[1].x + acc[1].y)) + ((acc[2].x + acc[2].y) + (acc[3].x + acc[3].y));
-        if (!page) sum = 0.f;
+      job += tiles2 * (u.t1 - u.t0);
+      if (!ok) break;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x = acc[i].x + acc[i].y;
+        x += __shfl_xor_sync(0xFFFFFFFFu, x, 1);
+        x += __shfl_xor_sync(0xFFFFFFFFu, x, 2);
+        const int row = (warp & 3) * 32 + mine + 8 * i;
+        if (quad != i || slot0 + row >= u.q.keys) continue;
+        if (fs[i].x == -1.f) x = 0.f;
         if (u.whole)
-          p.part[((long long)u.g * p.rows.batch + u.b) * p.rows.cap + slot] = sum;
+          p.part[((long long)u.g * p.rows.batch + u.b) * p.rows.cap + slot0 + row] = x;
         else
-          p.cut[(2 * share + (u.begins ? 1 : 0)) * kUnitSlots + w * KT + r] = sum;
+          p.cut[(2 * share + (u.begins ? 1 : 0)) * kUnitSlots + w * KT + row] = x;
       }
     }
   }
