@@ -104,6 +104,25 @@ CC_DEV bool mbar_wait(uint64_t *bar, uint32_t parity, volatile int *abort, unsig
   }
 }
 
+// The same limits, but the clock is first read after 64 tries: for waits that are many
+// and short.
+CC_DEV bool mbar_wait_short(uint64_t *bar, uint32_t parity, volatile int *abort, unsigned *status) {
+  uint64_t t0 = 0;
+  for (uint32_t it = 1;; ++it) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((it & 63u) == 0) {
+      if (*abort) return false;
+      const uint64_t now = globaltimer();
+      if (t0 == 0) t0 = now;
+      if (now - t0 > kWaitLimitNs) {
+        *abort = 1;
+        set_status(status, CC_ERR_TIMEOUT);
+        return false;
+      }
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------
 // TMA (cp.async.bulk.tensor) and bulk copies
 // ---------------------------------------------------------------------------
@@ -382,6 +401,12 @@ CC_DEV void tmem_ld_rows16(uint32_t taddr, uint32_t (&r)[16]) {
         "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
         "=r"(r[14]), "=r"(r[15])
       : "r"(taddr));
+}
+CC_DEV void tmem_ld_rows16(uint32_t taddr, uint32_t (&r)[8]) {   // 16 columns
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+                 "=r"(r[7])
+               : "r"(taddr));
 }
 CC_DEV void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 

@@ -25,8 +25,8 @@ struct KvReceivedParams {
   int shares;                   // CTAs
   // chunks (set by launch_kv_received_tiles)
   int P;                        // positions of a query tile
-  float *part;                  // [hkv][batch][cap]: the sums of whole units
-  float *cut;                   // [2 * shares][256]: of a share's pieces of units
+  float *part;                  // [hkv][batch][cap][2]: the sums of whole units, over half of the rows each
+  float *cut;                   // [2 * shares][256][2]: of a share's pieces of units
 };
 
 CC_DEV float ex2(float x) {
@@ -51,9 +51,9 @@ CC_DEV RowLse row_lse(const KvReceivedParams &p, float lse) {
 void kv_received_plan(KvReceivedParams &p, int sms);
 cudaError_t launch_kv_received(const KvReceivedParams &p, cudaStream_t st);
 
-// Chunks: tiles of 128 query rows, kv_received_positions consecutive ones of a KV head's
+// Chunks: tiles of up to 96 query rows, kv_received_positions consecutive ones of a KV head's
 // heads.  tq: q as [n_rows][hq][head_dim], box {64, heads of a KV head, positions}.
-constexpr int kReceivedMaxGroup = 128;   // heads of a KV head
+constexpr int kReceivedMaxGroup = 96;   // heads of a KV head
 int kv_received_positions(int group);
 size_t kv_received_part_bytes(const KvReceivedParams &p, int sms);
 cudaError_t launch_kv_received_tiles(KvReceivedParams p, const CUtensorMap &tq, void *ws, int sms, cudaStream_t st);

@@ -2,7 +2,7 @@
 // from chunks of rows (kvreceived.cu has the definition, and few rows).
 //
 // Bound by the tensor cores and, about as much, by the exponentials: with 128 slots
-// as the M rows of a tcgen05 product and 128 query rows as its N, each thread has a slot
+// as the M rows of a tcgen05 product and 96 query rows as its N, each thread has a slot
 // and adds that slot's own weights, no sum crosses threads, and the slot's scale is
 // a factor of the thread.  The key codes become bf16 (fp16 for fp16 rows; exact, without
 // their scale) once per unit and stay in tensor memory as the A operand; the query
@@ -13,38 +13,42 @@
 // shares, a CTA per share; the sums of a unit that spans shares are added up in share
 // order, then the heads' in theirs (finish_kernel): fixed orders, no atomics.
 //
-//   warps 0-3, 4-7  a slot tile each: codes to tensor memory, then per query tile the
-//                   scores from tensor memory, weights, sums
-//   warp 8          query tiles (TMA)
-//   warp 9          tensor memory and the products, each slot tile's in turn, in three
-//                   buffers of scores
-//   warps 10, 11    the rows' terms, a query tile each in turn
+//   warps 0-7, 8-15  a slot tile each: codes to tensor memory, then per query tile the
+//                    scores from tensor memory (four warps half of the columns), weights, sums
+//   warps 16, 17     the products of a slot tile each, in two buffers of scores of its own
+//                    (warp 17 has the tensor memory)
+//   warp 18          query tiles (TMA)
+//   warp 19          the rows' terms
 //
 // A row's y is its rounded part, which the scores' multiply-add takes off, and a factor
 // e^-rest of its weights.
 #include "kvreceived.cuh"
 
+#include <type_traits>
+
 namespace cc {
 
 namespace {
 
-constexpr int KT = 128;             // slots of a tile, query rows of a tile
+constexpr int KT = 128;             // slots of a tile
+constexpr int QT = 96;              // query rows of a tile: two buffers of scores for each of two slot tiles
+constexpr int CH = QT / 2;          // of them (columns of the scores) a warp's
 constexpr int kUnitSlots = 2 * KT;
-constexpr int kStages = 4;
-constexpr int kThreads = 384;
-// Registers of a launch's 384 threads at 168 shared out anew between its three warpgroups.
-constexpr int kRegsSlots = 216, kRegsOthers = 72;
-static_assert(2 * kRegsSlots + kRegsOthers <= 3 * 168, "more registers than the block is launched with");
+constexpr int kStages = 6;
+constexpr int kThreads = 640;
+// Registers of a launch's 640 threads at 96 shared out anew between its five warpgroups.
+constexpr int kRegsSlots = 104, kRegsOthers = 64;
+static_assert(4 * kRegsSlots + kRegsOthers <= 5 * 96, "more registers than the block is launched with");
 constexpr int kUnitCost = 3;        // of a unit's start, in query tiles
 
 template <int DH>
 struct RtSmem {
   static constexpr int NH = DH / 64;                   // 64-column (128-byte) halves
-  static constexpr int TILE = NH * KT * 128;
+  static constexpr int TILE = NH * QT * 128;
   static constexpr int OFF_Q = 0;
-  // [stage][KT / 2] float4: of two query rows -y, -y, e^-rest, e^-rest
+  // [stage][QT / 2] float4: of two query rows -y, -y, e^-rest, e^-rest
   static constexpr int OFF_TERM = OFF_Q + kStages * TILE;
-  static constexpr int OFF_LIVE = OFF_TERM + kStages * KT * 8;     // [stage]: bit i: columns 32 i ... all add
+  static constexpr int OFF_LIVE = OFF_TERM + kStages * QT * 8;     // [stage]: bit h: columns 48 h ... all add
   static constexpr int OFF_BAR = OFF_LIVE + kStages * 4;
   static constexpr int BYTES = OFF_BAR + 256 + 1024;               // barriers + alignment slack
 };
@@ -198,11 +202,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile uint32_t *live_sh = reinterpret_cast<volatile uint32_t *>(smem + L::OFF_LIVE);
   uint64_t *q_full = reinterpret_cast<uint64_t *>(smem + L::OFF_BAR);   // [kStages]
   uint64_t *q_empty = q_full + kStages;                                 // [kStages]
-  uint64_t *s_full = q_empty + kStages;                                 // [3]
-  uint64_t *s_empty = s_full + 3;                                       // [3]
-  uint64_t *a_full = s_empty + 3;                                       // [2]
+  uint64_t *s_full = q_empty + kStages;                                 // [2 slot tiles][2]
+  uint64_t *s_empty = s_full + 4;                                       // [2][2]
+  uint64_t *a_full = s_empty + 4;                                       // [2]
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(a_full + 2);
-  __shared__ Pieces walk_sh[8];
+  __shared__ Pieces walk_sh[16];
+  __shared__ float f_sh[2][2][2][KT];   // [piece's parity][slot tile][half of the codes][slot]
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
 
   pdl_trigger();   // the finish may launch: it waits for this grid
@@ -217,28 +222,34 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&q_full[s], 2);   // the copies, the terms
-      mbar_init(&q_empty[s], 1 + 8);   // the products, and the warps that read the terms
+      mbar_init(&q_empty[s], 16);   // the slots' warps: they have seen the products' end and read the terms
     }
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < 4; ++i) {
       mbar_init(&s_full[i], 1);
-      mbar_init(&s_empty[i], 4);
+      mbar_init(&s_empty[i], 8);
     }
-    for (int i = 0; i < 2; ++i) mbar_init(&a_full[i], 4);
+    for (int i = 0; i < 2; ++i) mbar_init(&a_full[i], 8);
     *abort_flag = 0;
     fence_barrier_init();
   }
-  if (warp == 9) tmem_alloc(tmem_slot, 512);
+  const int G = p.hq / p.hkv;
+  {   // rows of a tile that hold no query: zeros, so that their scores are numbers
+    const int pad = (QT - p.P * G) * 8;   // 16-byte pieces
+    for (int i = threadIdx.x; i < pad * L::NH * kStages; i += kThreads)
+      *reinterpret_cast<uint4 *>(smem + L::OFF_Q + (i / pad) * (QT * 128) + p.P * G * 128 + i % pad * 16) = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+  }
+  if (warp == 17) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const int G = p.hq / p.hkv;
   Pieces u;
   u.start(p, total, n, share);
 
-  if (warp >= 8) {
+  if (warp >= 16) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOthers));
-  if (warp == 8) {
+  if (warp == 18) {
     // ----------------------------------------------------------- query tiles
     if (lane == 0) tma_prefetch_desc(&tq);
     int it = 0;
@@ -247,19 +258,19 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0)
         for (int t = u.t0; ok && t < u.t1; ++t, ++it) {
           const int s = it % kStages;
-          if (!(ok = mbar_wait(&q_empty[s], ((it / kStages) & 1) ^ 1, abort_flag, p.status))) break;
+          if (!(ok = mbar_wait_short(&q_empty[s], ((it / kStages) & 1) ^ 1, abort_flag, p.status))) break;
           mbar_arrive_expect_tx(&q_full[s], (uint32_t)(L::NH * p.P * G * 128));
           for (int h = 0; h < L::NH; ++h)
-            tma_load_3d(smem + L::OFF_Q + s * L::TILE + h * KT * 128, &tq, &q_full[s], h * 64, u.g * G,
+            tma_load_3d(smem + L::OFF_Q + s * L::TILE + h * QT * 128, &tq, &q_full[s], h * 64, u.g * G,
                         u.q.s.r0 + t * p.P);
         }
       ok = __shfl_sync(0xFFFFFFFFu, ok ? 1 : 0, 0) != 0;
     }
-  } else if (warp >= 10) {
-    // ------------------- the rows' terms, every other tile; their loads a tile of this warp's ahead
-    int pos[KT / 32], at[KT / 32];
+  } else if (warp == 19) {
+    // ------------------------------------ the rows' terms, their loads a tile ahead
+    int pos[QT / 32], at[QT / 32];
 #pragma unroll
-    for (int i = 0; i < KT / 32; ++i) {
+    for (int i = 0; i < QT / 32; ++i) {
       const int col = lane + 32 * i;
       pos[i] = col / G;
       at[i] = pos[i] * p.hq + col - pos[i] * G;
@@ -269,84 +280,88 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     while (ok && u.next(p)) {
       const float *src = p.lse + (long long)u.q.s.r0 * p.hq + u.g * G;
-      float next[KT / 32];
+      float next[QT / 32];
       auto load = [&](int t) {
         const int left = u.q.s.count - t * p.P;   // rows of the tile and on
 #pragma unroll
-        for (int i = 0; i < KT / 32; ++i)
+        for (int i = 0; i < QT / 32; ++i)
           next[i] = t < u.t1 && pos[i] < left ? __ldg(src + (long long)t * p.P * p.hq + at[i]) : INFINITY;
       };
-      int t = u.t0 + ((warp - 10 - it) & 1);
-      it += t - u.t0;
-      load(t);
-      for (; t < u.t1; t += 2, it += 2) {
+      load(u.t0);
+      for (int t = u.t0; t < u.t1; ++t, ++it) {
         const int s = it % kStages;
-        float lse[KT / 32];
+        RowLse y[QT / 32];
+        uint32_t dead = 0;   // bit h: a row of columns 48 h ... adds nothing
 #pragma unroll
-        for (int i = 0; i < KT / 32; ++i) lse[i] = next[i];
-        load(t + 2);
-        if (!(ok = mbar_wait(&q_empty[s], ((it / kStages) & 1) ^ 1, abort_flag, p.status))) break;
-        uint32_t live = 0;
-#pragma unroll
-        for (int i = 0; i < KT / 32; ++i) {
-          const RowLse y = row_lse(p, lse[i]);
-          const int col = lane + 32 * i;
-          float *term = reinterpret_cast<float *>(term_sh + s * (KT / 2) + col / 2) + (col & 1);
-          term[0] = -y.y;
-          term[2] = 1.f - y.rest + 0.5f * y.rest * y.rest;   // e^-rest, a small one
-          live |= (__all_sync(0xFFFFFFFFu, y.y < INFINITY) ? 1u : 0u) << i;
+        for (int i = 0; i < QT / 32; ++i) {
+          y[i] = row_lse(p, next[i]);
+          // (or holds no query)
+          const uint32_t adds = __ballot_sync(0xFFFFFFFFu, y[i].y < INFINITY || pos[i] >= p.P);
+          const int c = 32 * i / CH;
+          if (i % 3 == 1)
+            dead |= ((adds & 0xFFFFu) != 0xFFFFu ? 1u << c : 0u) | (adds >> 16 != 0xFFFFu ? 2u << c : 0u);
+          else
+            dead |= adds != ~0u ? 1u << c : 0u;
         }
-        if (lane == 0) live_sh[s] = live;
+        load(t + 1);
+        if (!(ok = mbar_wait_short(&q_empty[s], ((it / kStages) & 1) ^ 1, abort_flag, p.status))) break;
+#pragma unroll
+        for (int i = 0; i < QT / 32; ++i) {
+          const int col = lane + 32 * i;
+          float *term = reinterpret_cast<float *>(term_sh + s * (QT / 2) + col / 2) + (col & 1);
+          term[0] = -y[i].y;
+          term[2] = 1.f - y[i].rest + 0.5f * y[i].rest * y[i].rest;   // e^-rest, a small one
+        }
+        if (lane == 0) live_sh[s] = ~dead;
         __syncwarp();
         if (lane == 0) mbar_arrive(&q_full[s]);
       }
-      it -= t - u.t1;   // (t is t1, or t1 + 1)
     }
-  } else if (warp == 9) {
-    // ------------------------------------------------------------- products
-    constexpr uint32_t idesc = F16 ? make_idesc_f16(128, KT, 0, 0) : make_idesc_bf16(128, KT, 0, 0);
+  } else {
+    // ------- products: a warp per slot tile, so that one's run while the other waits and starts
+    constexpr uint32_t idesc = F16 ? make_idesc_f16(128, QT, 0, 0) : make_idesc_bf16(128, QT, 0, 0);
+    const int w = warp - 16;
     int it = 0;
-    unsigned job = 0, filled[2] = {0, 0};   // times that a slot tile's operand was
+    unsigned job = 0, filled = 0;   // of this slot tile: products, times that its operand was
     bool ok = true;
     while (ok && u.next(p)) {
-      const int tiles2 = u.q.keys - u.kt * kUnitSlots > KT ? 2 : 1;   // slot tiles of the unit
-      if (lane == 0)
+      const int n = u.t1 - u.t0;
+      if (w == 1 && u.q.keys - u.kt * kUnitSlots <= KT) {   // no second tile of slots
+        it += n;
+        continue;
+      }
+      if (lane == 0) {
+        ok = mbar_wait_short(&a_full[w], filled++ & 1, abort_flag, p.status);
+        for (int i = 0; ok && i < n; ++i, ++it, ++job) {
+          if (!(ok = mbar_wait_short(&q_full[it % kStages], (it / kStages) & 1, abort_flag, p.status) &&
+                     mbar_wait_short(&s_empty[2 * w + (job & 1)], ((job >> 1) & 1) ^ 1, abort_flag, p.status)))
+            break;
+          tc_fence_after();
+          const uint64_t qd = make_sdesc_sw128(smem_u32(smem + L::OFF_Q + it % kStages * L::TILE), 16, 1024);
+          const uint32_t d = tmem + 128 + (2 * w + (job & 1)) * QT, a = tmem + w * 64;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          if (ok && i < tiles2) ok = mbar_wait(&a_full[i], filled[i]++ & 1, abort_flag, p.status);
-      for (int t = u.t0; t < u.t1; ++t, ++it) {
-        if (lane == 0 && ok) {
-          const int s = it % kStages;
-          ok = mbar_wait(&q_full[s], (it / kStages) & 1, abort_flag, p.status);
-          const uint64_t qd = make_sdesc_sw128(smem_u32(smem + L::OFF_Q + s * L::TILE), 16, 1024);
-          for (int i = 0; ok && i < tiles2; ++i) {
-            const unsigned j = job + i;
-            if (!(ok = mbar_wait(&s_empty[j % 3], ((j / 3) & 1) ^ 1, abort_flag, p.status))) break;
-            tc_fence_after();
-#pragma unroll
-            for (int kk = 0; kk < DH / 16; ++kk)
-              umma_ts(tmem + 128 + (j % 3) * KT, tmem + i * 64 + kk * 8,
-                      qd + (uint64_t)((((kk >> 2) * KT * 128) >> 4) + (kk & 3) * 2), idesc, kk > 0);
-            umma_commit(&s_full[j % 3]);
-          }
-          if (ok) umma_commit(&q_empty[s]);
+          for (int kk = 0; kk < DH / 16; ++kk)
+            umma_ts(d, a + kk * 8, qd + (uint64_t)((((kk >> 2) * QT * 128) >> 4) + (kk & 3) * 2), idesc, kk > 0);
+          umma_commit(&s_full[2 * w + (job & 1)]);
         }
-        job += tiles2;
       }
       ok = __shfl_sync(0xFFFFFFFFu, ok ? 1 : 0, 0) != 0;
+      it = __shfl_sync(0xFFFFFFFFu, it, 0);
     }
   }
   } else {
     // ------------------------------------------------------ slots and their weights
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSlots));
-    const int w = warp >> 2;                // slot tile of the unit
-    const int r = (warp & 3) * 32 + lane;   // slot whose codes this thread widens
+    const int w = warp >> 3, half = (warp >> 2) & 1;   // slot tile of the unit; which columns of its scores
+    const int r = (warp & 3) * 32 + lane;              // slot whose codes this thread widens, half of them
     const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
     const int hs = p.pg.head_major ? 1 : p.hkv, log_block = 31 - __clz(p.block);
     const int mine = lane >> 2, quad = lane & 3;
     int it = 0;
-    unsigned job = 0;
+    unsigned job = 0, filled = 0;
     bool ok = true;
+    // positions in the tile of the first and last of the warp's columns
+    const int col0 = half * CH, first_pos = col0 / G, last_pos = min(p.P - 1, (col0 + CH - 1) / G);
     // (between pieces the walk waits in shared memory: its registers are needed)
     if (lane == 0) walk_sh[warp] = u;
     while (ok) {
@@ -355,31 +370,31 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!u.next(p)) break;
       __syncwarp();
       if (lane == 0) walk_sh[warp] = u;
-      const int tiles2 = u.q.keys - u.kt * kUnitSlots > KT ? 2 : 1;
-      if (w >= tiles2) {   // no second tile of slots: an arrival for each phase all the same
+      if (w == 1 && u.q.keys - u.kt * kUnitSlots <= KT) {
+        // no second tile of slots: an arrival for each query tile all the same
         for (int t = u.t0; ok && t < u.t1; ++t, ++it) {
-          ok = mbar_wait(&q_full[it % kStages], (it / kStages) & 1, abort_flag, p.status);
+          ok = mbar_wait_short(&q_full[it % kStages], (it / kStages) & 1, abort_flag, p.status);
           __syncwarp();
           if (lane == 0) mbar_arrive(&q_empty[it % kStages]);
         }
-        job += u.t1 - u.t0;
         continue;
       }
-      const int slot0 = u.kt * kUnitSlots + w * KT, slot = slot0 + r;
-      // ---- the slot's codes, its scale a factor of its scores (-1: there is no such page)
-      float f = 0.f;
+      const int slot0 = u.kt * kUnitSlots + w * KT;
+      // ---- the slots' codes, a slot's scale a factor of its scores (-1: there is no such page)
       {
-        uint32_t code[DH / 4];
+        const int slot = slot0 + r;
+        float f = 0.f;
+        uint32_t code[DH / 8];
 #pragma unroll
-        for (int i = 0; i < DH / 4; ++i) code[i] = 0;
+        for (int i = 0; i < DH / 8; ++i) code[i] = 0;
         if (slot < u.q.keys) {
           const long long row = p.pg.head_major ? ((long long)u.b * p.hkv + u.g) * p.rows.cap + slot
                                                 : kv_row(p.pg, p.rows.cap, u.b, slot);
           if (row >= 0) {
             const int gs = p.pg.head_major ? 0 : u.g;
-            const uint4 *src = reinterpret_cast<const uint4 *>(p.k + (row * hs + gs) * DH);
+            const uint4 *src = reinterpret_cast<const uint4 *>(p.k + (row * hs + gs) * DH + half * (DH / 2));
 #pragma unroll
-            for (int i = 0; i < DH / 16; ++i) *reinterpret_cast<uint4 *>(&code[4 * i]) = __ldg(src + i);
+            for (int i = 0; i < DH / 32; ++i) *reinterpret_cast<uint4 *>(&code[4 * i]) = __ldg(src + i);
             const float scale = __uint_as_float((uint32_t)p.ke[(row >> log_block) * hs + gs] << 23);
             f = p.scale_log2 * fmaf(scale, 0.f, scale);   // (e = 255: NaN)
           } else {
@@ -390,19 +405,19 @@ __global__ void __launch_bounds__(kThreads, 1)
         if constexpr (!F16) {   // a NaN code: every score of the slot is none
           uint32_t any = 0;
 #pragma unroll
-          for (int i = 0; i < DH / 4; ++i) any |= __vcmpeq4(code[i] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+          for (int i = 0; i < DH / 8; ++i) any |= __vcmpeq4(code[i] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
           if (any) f = NAN;
         }
+        f_sh[filled & 1][w][half][r] = f;
+        uint32_t a[DH / 4];
 #pragma unroll
-        for (int h = 0; h < DH / 64; ++h) {
-          uint32_t a[32];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            a[2 * i] = widen2<F16>(code[h * 16 + i] & 0xFFFFu);
-            a[2 * i + 1] = widen2<F16>(code[h * 16 + i] >> 16);
-          }
-          tmem_st32(tmem + lanes + w * 64 + h * 32, a);
+        for (int i = 0; i < DH / 8; ++i) {
+          a[2 * i] = widen2<F16>(code[i] & 0xFFFFu);
+          a[2 * i + 1] = widen2<F16>(code[i] >> 16);
         }
+        const uint32_t a_t = tmem + lanes + w * 64 + half * (DH / 4);
+        if constexpr (DH == 128) tmem_st32(a_t, a);
+        else tmem_st16(a_t, a);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -410,43 +425,49 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       // ---- a lane has the weights of four slots (8 apart) and every fourth pair of rows, so that a
       // row's terms are read once for four
+      if (!(ok = mbar_wait_short(&a_full[w], filled & 1, abort_flag, p.status))) break;
       float2 fs[4], acc[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        fs[i].x = fs[i].y = __shfl_sync(0xFFFFFFFFu, f, mine + 8 * i);
+        const int row = (warp & 3) * 32 + mine + 8 * i;
+        const float f0 = f_sh[filled & 1][w][0][row], f1 = f_sh[filled & 1][w][1][row];
+        fs[i].x = fs[i].y = f0 == f0 ? f1 : f0;   // NaN where either half is
         acc[i] = make_float2(0.f, 0.f);
       }
-      unsigned j = job + w;
-      for (int t = u.t0; t < u.t1; ++t, ++it, j += tiles2) {
+      ++filled;
+      for (int t = u.t0; t < u.t1; ++t, ++it, ++job) {
         const int s = it % kStages;
-        if (!(ok = mbar_wait(&q_full[s], (it / kStages) & 1, abort_flag, p.status) &&
-                   mbar_wait(&s_full[j % 3], (j / 3) & 1, abort_flag, p.status)))
+        const unsigned buf = 2 * w + (job & 1);
+        if (!(ok = mbar_wait_short(&q_full[s], (it / kStages) & 1, abort_flag, p.status) &&
+                   mbar_wait_short(&s_full[buf], (job >> 1) & 1, abort_flag, p.status)))
           break;
         tc_fence_after();
-        uint32_t sr[4][2][16];   // of 32 columns each: slots 0 - 15 and 16 - 31 of the warp's
+        {
+          uint32_t sr[2][CH / 2];   // slots 0 - 15 and 16 - 31 of the warp's
+          const uint32_t at = tmem + lanes + 128 + buf * QT + col0;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const uint32_t at = tmem + lanes + 128 + (j % 3) * KT + 32 * c;
-          tmem_ld_rows16(at, sr[c][0]);
-          tmem_ld_rows16(at + (16u << 16), sr[c][1]);
-        }
-        const float4 *terms = term_sh + s * (KT / 2) + quad;
-        const uint32_t live = live_sh[s];   // bit c: every row of columns 32 c ... adds
-        const int seen_first = p.memory_only ? 0x7FFFFFFF : u.q.s.seq + t * p.P;   // last slot that the tile's first row sees
-        tmem_ld_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&s_empty[j % 3]);   // copied out: the buffer may be refilled
-        if (live == 15u && slot0 + KT - 1 <= seen_first) {
+          for (int i = 0; i < 2; ++i) {
+            tmem_ld_rows16(at + ((uint32_t)i << 20), *reinterpret_cast<uint32_t(*)[16]>(&sr[i][0]));
+            tmem_ld_rows16(at + ((uint32_t)i << 20) + 32, *reinterpret_cast<uint32_t(*)[8]>(&sr[i][16]));
+          }
+          const bool live = (live_sh[s] >> half) & 1u;   // every row of the columns adds
+          const float4 *terms = term_sh + s * (QT / 2) + col0 / 2 + quad;
+          // the last slots that the first and the last row of the columns see
+          const int pos = u.q.s.seq + t * p.P;
+          const int seen_first = p.memory_only ? 0x7FFFFFFF : pos + first_pos;
+          const int seen_last = p.memory_only ? 0x7FFFFFFF : pos + last_pos;
+          tmem_ld_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&s_empty[buf]);   // copied out: the buffer may be refilled
+          if (live && slot0 + KT - 1 <= seen_first) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float4 y = terms[16 * c + 4 * k];   // of two columns -y and e^-rest
+            for (int k = 0; k < CH / 8; ++k) {
+              const float4 y = terms[4 * k];   // of two columns -y and e^-rest
               float2 x[4];
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const uint32_t *x2 = &sr[c][i >> 1][4 * k + 2 * (i & 1)];
+                const uint32_t *x2 = &sr[i >> 1][4 * k + 2 * (i & 1)];
                 x[i] = __ffma2_rn(make_float2(__uint_as_float(x2[0]), __uint_as_float(x2[1])), fs[i], make_float2(y.x, y.y));
               }
 #pragma unroll
@@ -454,31 +475,36 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
               for (int i = 0; i < 4; ++i) acc[i] = __ffma2_rn(x[i], make_float2(y.z, y.w), acc[i]);
             }
-        } else if (p.memory_only || slot0 <= seen_first + p.P - 1) {   // (some row sees some slot)
-          int from[4];   // of the lane's columns (8 k, and 8 k + 1, of each 32), the first that sees the slot
+          } else if (slot0 <= seen_last) {   // (some row sees some slot)
+            // of the lane's columns (8 k, and 8 k + 1), the first that sees the slot
+            int from[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            from[i] = p.memory_only ? -1 : (slot0 + (warp & 3) * 32 + mine + 8 * i - seen_first) * G - 2 * quad;
+            for (int i = 0; i < 4; ++i)
+              from[i] = p.memory_only ? -1 : (slot0 + (warp & 3) * 32 + mine + 8 * i - pos) * G - col0 - 2 * quad;
+            // (chosen, not multiplied by 0: what a row does not see, or one that adds nothing, may be no number)
+            auto weigh = [&](auto some_dead) {
+              constexpr bool dead = decltype(some_dead)::value;
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
+              for (int k = 0; k < CH / 8; ++k) {
+                const float4 y = terms[4 * k];
+                const bool some0 = !dead || y.x > -INFINITY, some1 = !dead || y.y > -INFINITY;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float4 y = terms[16 * c + 4 * k];
-              const int col = 32 * c + 8 * k;
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const uint32_t *x2 = &sr[c][i >> 1][4 * k + 2 * (i & 1)];
-                // (chosen, not multiplied by 0: what a row does not see, or one that adds nothing, may be no number)
-                const float x0 = col >= from[i] && y.x > -INFINITY ? fmaf(__uint_as_float(x2[0]), fs[i].x, y.x) : -INFINITY;
-                const float x1 = col + 1 >= from[i] && y.y > -INFINITY ? fmaf(__uint_as_float(x2[1]), fs[i].x, y.y) : -INFINITY;
-                acc[i] = __ffma2_rn(make_float2(ex2(x0), ex2(x1)), make_float2(y.z, y.w), acc[i]);
+                for (int i = 0; i < 4; ++i) {
+                  const uint32_t *x2 = &sr[i >> 1][4 * k + 2 * (i & 1)];
+                  float2 x = __ffma2_rn(make_float2(__uint_as_float(x2[0]), __uint_as_float(x2[1])), fs[i], make_float2(y.x, y.y));
+                  x.x = some0 && 8 * k >= from[i] ? x.x : -INFINITY;
+                  x.y = some1 && 8 * k + 1 >= from[i] ? x.y : -INFINITY;
+                  acc[i] = __ffma2_rn(make_float2(ex2(x.x), ex2(x.y)), make_float2(y.z, y.w), acc[i]);
+                }
               }
-            }
+            };
+            if (live) weigh(std::false_type());
+            else weigh(std::true_type());
+          }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&q_empty[s]);   // the terms are read
       }
-      job += tiles2 * (u.t1 - u.t0);
       if (!ok) break;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -489,9 +515,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (quad != i || slot0 + row >= u.q.keys) continue;
         if (fs[i].x == -1.f) x = 0.f;
         if (u.whole)
-          p.part[((long long)u.g * p.rows.batch + u.b) * p.rows.cap + slot0 + row] = x;
+          p.part[(((long long)u.g * p.rows.batch + u.b) * p.rows.cap + slot0 + row) * 2 + half] = x;
         else
-          p.cut[(2 * share + (u.begins ? 1 : 0)) * kUnitSlots + w * KT + row] = x;
+          p.cut[((2 * share + (u.begins ? 1 : 0)) * kUnitSlots + w * KT + row) * 2 + half] = x;
       }
     }
   }
@@ -499,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   __syncthreads();
   if (*abort_flag) __nanosleep(1000000);   // let copies still in flight land
-  if (warp == 9) {
+  if (warp == 17) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
@@ -546,12 +572,17 @@ __global__ void __launch_bounds__(kUnitSlots) finish_kernel(const __grid_constan
       for (int i = 0; i < min(kUnitSlots, p.hkv - g0); ++i) {
         const int first = first_sh[i];   // share, and whether the unit begins there
         if (first < 0) {
-          sum += p.part[((long long)(g0 + i) * p.rows.batch + b) * p.rows.cap + slot];
+          const float2 x = reinterpret_cast<const float2 *>(p.part)[((long long)(g0 + i) * p.rows.batch + b) * p.rows.cap + slot];
+          sum += x.x + x.y;
           continue;
         }
-        float x = p.cut[first * kUnitSlots + tid];
-        for (int c = first / 2 + 1; c <= last_sh[i]; ++c) x += p.cut[2 * c * kUnitSlots + tid];
-        sum += x;
+        const float2 *cut = reinterpret_cast<const float2 *>(p.cut);
+        float2 x = cut[first * kUnitSlots + tid];
+        for (int c = first / 2 + 1; c <= last_sh[i]; ++c) {
+          const float2 y = cut[2 * c * kUnitSlots + tid];
+          x = make_float2(x.x + y.x, x.y + y.y);
+        }
+        sum += x.x + x.y;
       }
   }
   if (slot < q.keys) {
@@ -580,17 +611,17 @@ cudaError_t launch(const KvReceivedParams &p, const CUtensorMap &tq, cudaStream_
 
 }  // namespace
 
-int kv_received_positions(int group) { return KT / group; }
+int kv_received_positions(int group) { return QT / group; }
 
 size_t kv_received_part_bytes(const KvReceivedParams &p, int sms) {
-  return (size_t)p.hkv * p.rows.batch * p.rows.cap * 4 + (size_t)sms * 2 * kUnitSlots * 4;
+  return (size_t)p.hkv * p.rows.batch * p.rows.cap * 8 + (size_t)sms * 2 * kUnitSlots * 8;
 }
 
 cudaError_t launch_kv_received_tiles(KvReceivedParams p, const CUtensorMap &tq, void *ws, int sms, cudaStream_t st) {
   p.P = kv_received_positions(p.hq / p.hkv);
   p.shares = sms;
   p.cut = reinterpret_cast<float *>(ws);
-  p.part = p.cut + (size_t)sms * 2 * kUnitSlots;
+  p.part = p.cut + (size_t)sms * 4 * kUnitSlots;
   if (p.head_dim == 128) return p.f16 ? launch<128, true>(p, tq, st) : launch<128, false>(p, tq, st);
   return p.f16 ? launch<64, true>(p, tq, st) : launch<64, false>(p, tq, st);
 }
