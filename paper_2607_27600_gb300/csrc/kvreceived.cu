@@ -25,9 +25,10 @@ namespace {
 
 constexpr int kWarps = 8;
 constexpr int kStep = 16;            // slots of a warp's step
-constexpr int kResident = 2;         // CTAs per SM
-constexpr int kAhead = 3;            // heads of a step in flight per warp
-constexpr int kQueryBytes = 96 * 1024;   // of the queries in shared memory, at most
+// CTAs per SM.
+constexpr int resident(int tiles) { return tiles == 1 ? 3 : 2; }
+constexpr int kSegment = 32;         // steps between joins of the warps' sums
+constexpr int kQueryBytes = 92 * 1024;   // of the queries in shared memory, at most
 
 CC_DEV uint32_t widen2(uint32_t two) {   // e4m3 pair (low 16 bits) -> fp16 pair, exact
   uint32_t r;
@@ -89,19 +90,22 @@ CC_DEV int find_step(const KvReceivedParams &p, long long at, long long &before)
   return p.rows.batch;
 }
 
-// Per query row: what makes its products scores, its log2-sum-exp (+inf where it adds
-// nothing), and the slots that it sees.
+// Per query row: what makes its products scores, its log2-sum-exp, and the slots that it sees
+// (none where it adds nothing).
 struct __align__(16) RowTerm {
   float f, y, rest;   // rest: in the log2 domain
   int seen;
 };
 
-template <typename T, int DH>
-__global__ void __launch_bounds__(kWarps * 32, kResident)
+// TILES: eights of query rows of a KV head in a pass where there are few, all of which take the
+// slots' widened codes as they are made; 0: any number, which are widened first.
+template <typename T, int DH, int TILES>
+__global__ void __launch_bounds__(kWarps * 32, resident(TILES))
     kv_received_kernel(const __grid_constant__ KvReceivedParams p) {
   constexpr int KS = DH / 16;        // k steps of K Q^T
   constexpr int W = DH / 16;         // words of a slot that a lane holds
   extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ float sum_sh[kWarps][kSegment * kStep];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n8 = lane >> 2, quad = lane & 3;
   const long long total = total_steps(p);
   const int n_shares = (int)min((long long)p.shares, total);
@@ -116,9 +120,11 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
   int b = find_step(p, at, before);
   const int G = p.hq / p.hkv;
   const int hs = p.pg.head_major ? 1 : p.hkv;
-  const int log_block = 31 - __clz(p.block);
+  const int log_block = 31 - __clz(p.block), slot_bytes = hs * DH;
+  const long long head_bytes = (p.pg.head_major ? (long long)p.rows.cap : 1) * DH;
+  const long long head_exps = p.pg.head_major ? p.rows.cap >> log_block : 1;
   const int NT = p.tiles_at_once, HC = p.heads_at_once;
-  uint2 *q_sh = reinterpret_cast<uint2 *>(smem);                         // [HC][NT][KS][32]
+  uint4 *q_sh = reinterpret_cast<uint4 *>(smem);                         // [HC][NT][KS / 2][32]
   RowTerm *r_sh = reinterpret_cast<RowTerm *>(smem + (size_t)HC * NT * KS * 256);   // [HC][NT * 8]
   // whether a lane's 32 bytes may be one load
   const bool wide = (reinterpret_cast<uintptr_t>(p.k) & 31) == 0;
@@ -138,7 +144,83 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
     bool fresh = p.first != 0;        // the new rows' slots start from 0
     for (int g0 = 0; g0 < p.hkv; g0 += HC)
       for (int R0 = 0; R0 < q_rows; R0 += 8 * NT) {
-        const int heads = min(HC, p.hkv - g0), tiles = min(NT, (q_rows - R0 + 7) / 8);
+        const int heads = min(HC, p.hkv - g0), tiles = TILES > 0 ? TILES : min(NT, (q_rows - R0 + 7) / 8);
+        // ---- where this warp's items lie: every kWarps-th pair of heads, through the steps
+        const int pairs = (heads + 1) / 2;
+        const int step_skip = kWarps / pairs, pair_skip = kWarps - step_skip * pairs;
+        uint32_t kw[2][2][W], ke[2];
+        int next_step = 0, next_pair = 0, left = 0;
+        int run = 0;   // steps from next_step on that lie one after the other
+        int row = 0;   // of a slot-major buffer or pool, next_step's first slot's; -1: no page
+        const uint8_t *at[2], *at_e;   // of the next item: the lane's slots, their scale
+        // Where the next item lies.
+        auto find = [&]() {
+          const int slot = next_step * kStep;
+          if (run <= 0) {
+            if (!p.pg.table || p.pg.head_major) {
+              row = b * p.rows.cap + slot;
+              run = 0x7FFFFFFF;
+            } else {   // a page that is none: its slots receive nothing
+              row = (int)kv_row(p.pg, p.rows.cap, b, slot);
+              run = (p.pg.page - slot % p.pg.page) / kStep;
+              if (row < 0 && lane == 0) set_status(p.status, CC_ERR_DEVICE_ARG);
+            }
+          }
+          const int g = g0 + 2 * next_pair;
+          const long long vec = p.pg.head_major ? (long long)(b * p.hkv + g) * p.rows.cap + slot
+                                                : (long long)max(0, row) * p.hkv + g;
+          const uint8_t *src = p.k + vec * DH + quad * (DH / 4);
+          const int last = min(kStep - 1, v.keys - 1 - slot);   // (past the last seen slot: that one)
+          at[0] = src + min(n8, last) * slot_bytes;
+          at[1] = src + min(n8 + 8, last) * slot_bytes;
+          at_e = p.ke + (p.pg.head_major ? vec >> log_block : (long long)(max(0, row) >> log_block) * p.hkv + g);
+        };
+        auto load = [&](int i) {   // the i-th head of the pair
+          if (2 * next_pair + i >= heads) return;
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const uint8_t *src = at[r] + i * head_bytes;
+            if constexpr (DH == 128) {
+              if (wide) {
+                asm volatile("ld.global.nc.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                             : "=r"(kw[i][r][0]), "=r"(kw[i][r][1]), "=r"(kw[i][r][2]), "=r"(kw[i][r][3]),
+                               "=r"(kw[i][r][4]), "=r"(kw[i][r][5]), "=r"(kw[i][r][6]), "=r"(kw[i][r][7])
+                             : "l"(src));
+              } else {
+                *reinterpret_cast<uint4 *>(&kw[i][r][0]) = load_once(src);
+                *reinterpret_cast<uint4 *>(&kw[i][r][4]) = load_once(src + 16);
+              }
+            } else {
+              *reinterpret_cast<uint4 *>(&kw[i][r][0]) = load_once(src);
+            }
+          }
+          ke[i] = row < 0 ? 256u : at_e[i * head_exps];
+        };
+        auto advance = [&]() {
+          int on = step_skip;
+          next_pair += pair_skip;
+          if (next_pair >= pairs) {
+            next_pair -= pairs;
+            ++on;
+          }
+          next_step += on;
+          run -= on;
+          if (row >= 0) row += on * kStep;
+        };
+        // The first of this warp's items of the segment at `seg` on their way.
+        auto begin = [&](int seg) {
+          const int n = min(kSegment, to - seg);   // (may be <= 0)
+          left = max(0, (n * pairs - warp + kWarps - 1) / kWarps);
+          next_step = seg + warp / pairs;
+          next_pair = warp % pairs;
+          run = 0;
+          if (left > 0) {
+            find();
+            load(0);
+            load(1);
+          }
+        };
+        begin(from);
         // ---- the queries: row 8 t + n8 of a head as the second operand, fp16, scaled
         // to a largest magnitude of [2^7, 2^8)
         __syncthreads();   // the last pass is done with them
@@ -172,129 +254,120 @@ __global__ void __launch_bounds__(kWarps * 32, kResident)
           const float up = __uint_as_float((uint32_t)min(261 - e, 253) << 23);
           const float down = p.scale_log2 * __uint_as_float((uint32_t)max(e - 7, 1) << 23);
 #pragma unroll
-          for (int k = 0; k < KS; ++k)
-            q_sh[((h * NT + t) * KS + k) * 32 + lane] =
-                make_uint2(pack_f16x2(x[4 * k] * up, x[4 * k + 1] * up),
-                           pack_f16x2(x[4 * k + 2] * up, x[4 * k + 3] * up));
+          for (int k = 0; k < KS / 2; ++k)
+            q_sh[((h * NT + t) * (KS / 2) + k) * 32 + lane] =
+                make_uint4(pack_f16x2(x[8 * k] * up, x[8 * k + 1] * up), pack_f16x2(x[8 * k + 2] * up, x[8 * k + 3] * up),
+                           pack_f16x2(x[8 * k + 4] * up, x[8 * k + 5] * up), pack_f16x2(x[8 * k + 6] * up, x[8 * k + 7] * up));
           if (quad == 0) {
             const RowLse y = row_lse(p, live ? p.lse[row * p.hq + head] : INFINITY);
-            r_sh[h * NT * 8 + 8 * t + n8] = {down, y.y, y.rest * 1.44269504f,
-                                             p.memory_only ? s.seq : s.seq + pos + 1};
+            const int seen = p.memory_only ? s.seq : s.seq + pos + 1;
+            r_sh[h * NT * 8 + 8 * t + n8] = {down, y.y, y.rest * 1.44269504f, y.y < INFINITY ? seen : 0};
           }
         }
         __syncthreads();
-        // ---- this warp's steps: 16 slots of every head of the pass, kAhead heads ahead
-        const int mine = (to - from - warp + kWarps - 1) / kWarps;   // (may be <= 0)
-        const int items = max(mine, 0) * heads;
-        uint32_t kw[kAhead][2][W], ke[kAhead];
-        int next_step = from + warp, next_head = 0, left = items;
-        long long vec0 = 0;   // of slot 0 of the step: vector index of head 0
-        long long exp0 = 0;
-        bool ok = true;
-        auto enter = [&]() {   // where the step's slots lie
-          const int slot = next_step * kStep;
-          if (p.pg.head_major) {
-            vec0 = ((long long)b * p.hkv + g0) * p.rows.cap + slot;
-            exp0 = vec0 >> log_block;
-            return;
-          }
-          const long long row = kv_row(p.pg, p.rows.cap, b, slot);
-          ok = row >= 0;
-          if (!ok && lane == 0) set_status(p.status, CC_ERR_DEVICE_ARG);
-          vec0 = (ok ? row : 0) * hs + g0;
-          exp0 = ((ok ? row : 0) >> log_block) * hs + g0;
-        };
-        const long long head_step = p.pg.head_major ? p.rows.cap : 1;
-        const long long head_exps = p.pg.head_major ? p.rows.cap >> log_block : 1;
-        auto load = [&](uint32_t (&w)[2][W], uint32_t &e) {
-          if (left <= 0) return;
-          --left;
-          if (next_head == 0) enter();
-          const int slot = next_step * kStep + n8;
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const bool there = ok && slot + 8 * r < v.keys;
-            const uint8_t *src = p.k + (vec0 + next_head * head_step + (long long)(n8 + 8 * r) * hs) * DH + quad * (DH / 4);
-#pragma unroll
-            for (int i = 0; i < W; ++i) w[r][i] = 0;
-            if (there) {
-              if constexpr (DH == 128) {
-                if (wide) {
-                  asm("ld.global.nc.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                      : "=r"(w[r][0]), "=r"(w[r][1]), "=r"(w[r][2]), "=r"(w[r][3]), "=r"(w[r][4]),
-                        "=r"(w[r][5]), "=r"(w[r][6]), "=r"(w[r][7])
-                      : "l"(src));
-                } else {
-                  *reinterpret_cast<uint4 *>(&w[r][0]) = load_once(src);
-                  *reinterpret_cast<uint4 *>(&w[r][4]) = load_once(src + 16);
-                }
-              } else {
-                *reinterpret_cast<uint4 *>(&w[r][0]) = load_once(src);
-              }
-            }
-          }
-          // (a page that is none: its slots receive nothing)
-          e = ok ? p.ke[exp0 + next_head * head_exps] : 256u;
-          if (++next_head == heads) {
-            next_head = 0;
-            next_step += kWarps;
-          }
-        };
-#pragma unroll
-        for (int a = 0; a < kAhead; ++a) load(kw[a], ke[a]);
-        int step = from + warp, h = 0;
-        float sum[2] = {0.f, 0.f};
+        // ---- segments of kSegment steps: 16 slots of two heads at a time, a step's heads by
+        // neighbouring warps, so that a slot's bytes are read at about one time
+        for (int seg = from; seg < to; seg += kSegment) {
+          const int seg_end = min(to, seg + kSegment);
+          float *mine = sum_sh[warp];
+          for (int i = lane; i < (seg_end - seg) * kStep; i += 32) mine[i] = 0.f;
+          __syncwarp();
 #pragma unroll 1
-        for (int it = 0; it < items; it += kAhead) {
+          for (; left > 0; --left) {
+            const int step = next_step, pair = next_pair, slot = step * kStep + n8;
+            advance();
+            if (left > 1) find();
+            float sum[2] = {0.f, 0.f};
 #pragma unroll
-          for (int a = 0; a < kAhead; ++a) {
-            if (it + a < items) {
-              const int slot = step * kStep + n8;
-              uint32_t wa[W], wb[W];
-              const uint32_t e = ke[a];
-#pragma unroll
-              for (int i = 0; i < W; ++i) {
-                wa[i] = kw[a][0][i];
-                wb[i] = kw[a][1][i];
-              }
-              load(kw[a], ke[a]);
+            for (int i = 0; i < 2; ++i) {
+              const int h = 2 * pair + i;
+              if (h >= heads) break;
+              const uint32_t e = ke[i];
               const float scale = __uint_as_float((e & 255u) << 23), kf = fmaf(scale, 0.f, scale);   // (e = 255: NaN)
-              const RowTerm *rt = r_sh + h * NT * 8;
-              const uint2 *qh = q_sh + (size_t)h * NT * KS * 32 + lane;
-              for (int t = 0; t < tiles; ++t) {
-                float d[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                  const uint2 q2 = qh[(t * KS + k) * 32];
-                  mma_f16(d, widen2(wa[k]), widen2(wb[k]), widen2(wa[k] >> 16), widen2(wb[k] >> 16), q2.x, q2.y);
-                }
+              const RowTerm *rt = r_sh + h * NT * 8 + 2 * quad;
+              const uint4 *qh = q_sh + (size_t)h * NT * (KS / 2) * 32 + lane;
+              auto weigh = [&](const float (&d)[4], const RowTerm *of) {
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                  const RowTerm r = rt[8 * t + 2 * quad + c];
+                  const RowTerm r = of[c];
                   const float f = r.f * kf;
-                  const bool adds = r.y < INFINITY && e < 256u;
+                  // (a row that adds nothing sees no slot)
 #pragma unroll
-                  for (int k = 0; k < 2; ++k)
-                    if (adds && slot + 8 * k < r.seen) sum[k] += ex2(fmaf(d[2 * k + c], f, -r.y) - r.rest);
-                }
-              }
-              if (++h == heads) {   // the slots' sums of this pass
-                h = 0;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                  float x = sum[k];
-                  x += __shfl_xor_sync(0xFFFFFFFFu, x, 1);
-                  x += __shfl_xor_sync(0xFFFFFFFFu, x, 2);
-                  if (quad == 0 && slot + 8 * k < v.keys) {
-                    float *dst = p.acc + (long long)b * p.rows.cap + slot + 8 * k;
-                    *dst = (fresh && slot + 8 * k >= s.seq ? 0.f : *dst) + x;
+                  for (int k = 0; k < 2; ++k) {
+                    const float x = ex2(fmaf(d[2 * k + c], f, -r.y) - r.rest);
+                    sum[k] += slot + 8 * k < r.seen && e < 256u ? x : 0.f;
                   }
-                  sum[k] = 0.f;
                 }
-                step += kWarps;
+              };
+              if constexpr (TILES > 0) {
+                float d[TILES][4];
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.f;
+#pragma unroll
+                for (int k = 0; k < KS; k += 2) {
+                  uint32_t op[2][4];
+#pragma unroll
+                  for (int j = 0; j < 2; ++j) {
+                    op[j][0] = widen2(kw[i][0][k + j]);
+                    op[j][1] = widen2(kw[i][1][k + j]);
+                    op[j][2] = widen2(kw[i][0][k + j] >> 16);
+                    op[j][3] = widen2(kw[i][1][k + j] >> 16);
+                  }
+#pragma unroll
+                  for (int t = 0; t < TILES; ++t) {
+                    const uint4 q4 = qh[(t * (KS / 2) + k / 2) * 32];
+                    mma_f16(d[t], op[0][0], op[0][1], op[0][2], op[0][3], q4.x, q4.y);
+                    mma_f16(d[t], op[1][0], op[1][1], op[1][2], op[1][3], q4.z, q4.w);
+                  }
+                }
+                if (left > 1) load(i);
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) weigh(d[t], rt + 8 * t);
+              } else {
+                uint32_t op[KS][4];
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                  op[k][0] = widen2(kw[i][0][k]);
+                  op[k][1] = widen2(kw[i][1][k]);
+                  op[k][2] = widen2(kw[i][0][k] >> 16);
+                  op[k][3] = widen2(kw[i][1][k] >> 16);
+                }
+                if (left > 1) load(i);
+#pragma unroll 1
+                for (int t = 0; t < tiles; ++t, qh += KS / 2 * 32) {
+                  float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                  for (int k = 0; k < KS / 2; ++k) {
+                    const uint4 q4 = qh[k * 32];
+                    mma_f16(d, op[2 * k][0], op[2 * k][1], op[2 * k][2], op[2 * k][3], q4.x, q4.y);
+                    mma_f16(d, op[2 * k + 1][0], op[2 * k + 1][1], op[2 * k + 1][2], op[2 * k + 1][3], q4.z, q4.w);
+                  }
+                  weigh(d, rt + 8 * t);
+                }
               }
             }
+            // (an odd last head: the pair's second was not there, the next one's may be)
+            if (2 * pair + 1 >= heads && left > 1) load(1);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              sum[k] += __shfl_xor_sync(0xFFFFFFFFu, sum[k], 1);
+              sum[k] += __shfl_xor_sync(0xFFFFFFFFu, sum[k], 2);
+            }
+            if (quad < 2) mine[(step - seg) * kStep + n8 + 8 * quad] += quad ? sum[1] : sum[0];
           }
+          begin(seg + kSegment);
+          // the warps' sums in their order
+          __syncthreads();
+          for (int i = tid; i < (seg_end - seg) * kStep; i += kWarps * 32) {
+            const int slot = seg * kStep + i;
+            if (slot >= v.keys) break;
+            float x = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) x += sum_sh[w][i];
+            float *dst = p.acc + (long long)b * p.rows.cap + slot;
+            *dst = (fresh && slot >= s.seq ? 0.f : *dst) + x;
+          }
+          __syncthreads();
         }
         fresh = false;
       }
@@ -305,19 +378,28 @@ size_t smem_bytes(const KvReceivedParams &p) {
   return (size_t)p.heads_at_once * p.tiles_at_once * (p.head_dim / 16 * 256 + 8 * sizeof(RowTerm));
 }
 
-template <typename T, int DH>
-cudaError_t launch(const KvReceivedParams &p, cudaStream_t st) {
+template <typename T, int DH, int TILES>
+cudaError_t launch_tiles(const KvReceivedParams &p, cudaStream_t st) {
   static bool attr_set[64] = {};
   int dev = 0;
   cudaGetDevice(&dev);
   if (dev < 64 && !attr_set[dev]) {
-    const cudaError_t e = cudaFuncSetAttribute(kv_received_kernel<T, DH>,
+    const cudaError_t e = cudaFuncSetAttribute(kv_received_kernel<T, DH, TILES>,
                                                cudaFuncAttributeMaxDynamicSharedMemorySize, kQueryBytes);
     if (e != cudaSuccess) return e;
     attr_set[dev] = true;
   }
-  kv_received_kernel<T, DH><<<p.shares, kWarps * 32, smem_bytes(p), st>>>(p);
+  kv_received_kernel<T, DH, TILES><<<p.shares, kWarps * 32, smem_bytes(p), st>>>(p);
   return cudaGetLastError();
+}
+template <typename T, int DH>
+cudaError_t launch(const KvReceivedParams &p, cudaStream_t st) {
+  switch (p.tiles_at_once) {
+    case 1: return launch_tiles<T, DH, 1>(p, st);
+    case 2: return launch_tiles<T, DH, 2>(p, st);
+    case 3: return launch_tiles<T, DH, 3>(p, st);
+    default: return launch_tiles<T, DH, 0>(p, st);
+  }
 }
 
 }  // namespace
@@ -330,7 +412,7 @@ void kv_received_plan(KvReceivedParams &p, int sms) {
   const long long tiles = ((long long)p.rows.max_rows * G + 7) / 8;
   p.tiles_at_once = (int)std::min<long long>(tiles, room / p.heads_at_once);
   const long long most = (long long)p.rows.batch * ((p.rows.cap + kStep - 1) / kStep);
-  p.shares = (int)std::min<long long>((long long)sms * kResident, most);
+  p.shares = (int)std::min<long long>((long long)sms * resident(p.tiles_at_once), most);
 }
 
 cudaError_t launch_kv_received(const KvReceivedParams &p, cudaStream_t st) {
