@@ -13,8 +13,8 @@
 // blocks) of 128 bytes of one array's slots: a head or two, which have their own scales
 // and depend on nothing else.  It
 //   1. copies its sources to shared memory (cp.async) with their exponents,
-//   2. publishes that they are read (release),
-//   3. waits (acquire, bounded) for the lower units of its array and heads that read from its
+//   2. publishes that they are read,
+//   3. waits (bounded) for the lower units of its array and heads that read from its
 //      destinations, which a pre-pass finds from keep_idx, and
 //   4. rescales and writes.
 // Units are numbered sequence by sequence, slots ascending, the arrays and heads of
@@ -32,25 +32,32 @@ namespace cc {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
+constexpr int kResident = 10;        // CTAs per SM
+constexpr int kRows = kThreads / 8;  // slots of eight pieces of 16 bytes that the CTA moves at a time
+static_assert(kThreads == kCompactChunk && kCompactWidth == 128, "a thread per slot, eight pieces of a slot");
 constexpr int kPlanThreads = 256;
 constexpr int kNoNumbers = 255;      // a scale exponent
+constexpr int kStays = -1, kNoFall = 256;   // falls of a slot that is not written, and of one whose codes become NaN
 constexpr uint32_t kNanCodes = 0x7F7F7F7Fu;
-constexpr int kSharedBatch = 1024;   // sequences whose first chunks fit in shared memory
+constexpr int kSharedBatch = 512;    // sequences whose first chunks fit in shared memory
 
-CC_DEV void st_release(unsigned *p, unsigned v) {
-  asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+// Flags by relaxed accesses.  A unit's sources have arrived in shared memory before its flag is
+// stored, and a unit stores nothing before it has seen the flags, so that neither needs an
+// order among other accesses; a release would wait for the last unit's stores as well.
+CC_DEV void st_flag(unsigned *p) {
+  asm volatile("st.relaxed.gpu.global.u32 [%0], %1;" ::"l"(p), "r"(1u) : "memory");
 }
-CC_DEV unsigned ld_acquire(const unsigned *p) {
+CC_DEV unsigned ld_flag(const unsigned *p) {
   unsigned v;
-  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
   return v;
 }
 CC_DEV bool wait_flag(const unsigned *flag, unsigned *status) {
-  if (ld_acquire(flag)) return true;
+  if (ld_flag(flag)) return true;
   const uint64_t t0 = globaltimer();
   for (uint32_t it = 1;; ++it) {
-    if (ld_acquire(flag)) return true;
+    if (ld_flag(flag)) return true;
     __nanosleep(32);
     if ((it & 255u) == 0 && globaltimer() - t0 > kWaitLimitNs) {
       set_status(status, CC_ERR_TIMEOUT);
@@ -128,10 +135,23 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
   }
 }
 
-// 16 codes times 2^-fall (fall = 0 .. 255), rounded to nearest even.  Through fp16, which
-// holds code * 2^-fall exactly down to 2^-14 and else on a grid of 2^-24, fine enough that what
-// rounds to a code of 0 (up to 2^-10) stays on its side.
+// 16 codes times 2^-fall (fall = 1 .. 255), rounded to nearest even.  Where all of them are normal
+// numbers and stay so, their exponent fields fall.  Else through fp16, which holds code * 2^-fall
+// exactly down to 2^-14 and else on a grid of 2^-24, fine enough that what rounds to a code of
+// 0 (up to 2^-10) stays on its side.
 CC_DEV uint4 rescale(uint4 v, int fall) {
+  if (fall < 14) {
+    const uint32_t ones = 0x01010101u, tops = 0x80808080u, least = (uint32_t)(fall + 1) * 8 * ones, by = (uint32_t)fall * 8 * ones;
+    uint32_t fine = tops, none = 0;   // bytes of at least the least magnitude, and those that are no numbers
+    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t size = x[i] & ~tops;
+      fine &= (size | tops) - least;
+      none |= size + ones;
+    }
+    if ((fine & ~none & tops) == tops) return make_uint4(v.x - by, v.y - by, v.z - by, v.w - by);
+  }
   const int e = 15 - fall;   // of 2^-fall as fp16
   const uint32_t bits = e > 0 ? (uint32_t)e << 10 : e > -10 ? 1u << (9 + e) : 0u;
   const uint32_t f2 = bits | (bits << 16);
@@ -152,14 +172,21 @@ CC_DEV uint4 rescale(uint4 v, int fall) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-__global__ void __launch_bounds__(kThreads, 8) compact_kernel(const __grid_constant__ KvCompactParams p) {
+// A block's new exponent from its slots' old ones by one maximum: 255 (no number) ranks below
+// 0, and a slot that is not moved (-1) below that.
+CC_DEV int rank_of(int e) { return e == kNoNumbers ? 0 : e + 1; }
+CC_DEV int exponent_of(int rank) { return rank == 0 ? kNoNumbers : rank - 1; }
+
+__global__ void __launch_bounds__(kThreads, kResident) compact_kernel(const __grid_constant__ KvCompactParams p) {
   constexpr int C = kCompactChunk;
   __shared__ __align__(16) uint8_t st[C * kCompactWidth];
   __shared__ int base_sh[kSharedBatch + 1];
-  __shared__ long long from_sh[C], to_sh[C];   // vectors of 16 bytes in the array (-1: not moved)
-  __shared__ int e_sh[2][C], new_sh[2][C];     // exponents of the slots, and of their new blocks
+  __shared__ int src_sh[C];        // row of each slot's source in the array (-1: not moved)
+  __shared__ int top_sh[2][8];     // for each head of the plane: ranks of the maxima over 16 slots
+  // what becomes of each slot's codes: kStays, or they fall by so many steps of the exponent
+  __shared__ int fall_sh[2][C];
   __shared__ int go_sh;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31;
   const bool cached = p.batch <= kSharedBatch;
   if (cached)
     for (int i = tid; i <= p.batch; i += kThreads) base_sh[i] = p.first_chunk[i];
@@ -167,185 +194,163 @@ __global__ void __launch_bounds__(kThreads, 8) compact_kernel(const __grid_const
     for (int b = tid; b < p.batch; b += kThreads) p.seq_len[b] = kept_of(p, b);
   __syncthreads();
   const int *base = cached ? base_sh : p.first_chunk;
-  const long long total = (long long)base[p.batch] * p.planes;
-  const int log_block = 31 - __clz(p.block);
-  for (long long u = blockIdx.x; u < total; u += gridDim.x) {
-    const int chunk = (int)(u / p.planes), plane = (int)(u - (long long)chunk * p.planes);
-    int lo = 0, hi = p.batch - 1;
-    while (lo < hi) {   // the last sequence whose first chunk is at or before it
-      const int mid = (lo + hi + 1) >> 1;
-      if (base[mid] <= chunk) lo = mid; else hi = mid - 1;
+  const int chunks = base[p.batch];
+  const int log_block = 31 - __clz(p.block), each = kCompactWidth / p.head_dim;
+  // this CTA's units: chunk and plane step by step (units lie plane by plane within a chunk)
+  const int chunk_step = gridDim.x / p.planes, plane_step = gridDim.x - chunk_step * p.planes;
+  int chunk = blockIdx.x / p.planes, plane = blockIdx.x - chunk * p.planes;
+  int b = 0, J = 0, next_s = 0;   // next_s: of this thread's slot, the coming unit's entry of keep_idx
+  // The sequence of `chunk`, and its entries on their way.
+  auto enter = [&]() {
+    if (chunk >= chunks) return;
+    bool moved = J == 0;
+    while (base[b + 1] <= chunk) {
+      ++b;
+      moved = true;
     }
-    const int b = lo, c = chunk - base[b], k0 = c * C;
-    const int J = kept_of(p, b), rows = min(C, J - k0);
-    const int32_t *idx = p.keep_idx + (size_t)b * p.cap;
+    if (moved) J = kept_of(p, b);
+    const int k = (chunk - base[b]) * C + tid;
+    if (k < J) next_s = p.keep_idx[(size_t)b * p.cap + k];
+  };
+  enter();
+  while (chunk < chunks) {
+    const int c = chunk - base[b], k0 = c * C, rows = min(C, J - k0);
+    unsigned *flags = p.flags + ((size_t)base[b] * p.planes + plane);   // of the sequence's first chunk
+    // ---- what the plane is: heads of an array of codes, columns of h, or the small arrays
+    const bool codes = plane < p.n_arrays * p.array_planes, small = plane == p.planes - 1;
+    const int array = codes ? plane / p.array_planes : 0;
+    const int part = codes ? plane - array * p.array_planes : plane - p.n_arrays * p.array_planes;
+    uint8_t *buf = codes ? p.codes[array] : p.h;
+    const uint8_t *exps = codes ? p.exps[array] : nullptr;
+    // a slot's row starts at (first + row) * row_bytes + column of the array
+    long long first = 0;
+    int row_bytes = p.h_bytes, column = part * kCompactWidth, pieces = min(kCompactWidth, p.h_bytes - column) / 16;
+    int heads = 0, g = 0;
+    if (codes) {
+      g = p.pg.head_major ? part : part * each;
+      heads = p.pg.head_major ? 1 : min(each, p.hkv - g);
+      row_bytes = p.pg.head_major ? p.head_dim : p.hkv * p.head_dim;
+      column = p.pg.head_major ? 0 : g * p.head_dim;
+      pieces = heads * p.head_dim / 16;
+      if (p.pg.head_major) first = (long long)(b * p.hkv + g) * p.cap;
+    }
+    // row of the chunk's first slot (a chunk lies in one page; -1: none)
+    const bool paged = codes && p.pg.table && !p.pg.head_major;
+    const int seq_row = codes && p.pg.head_major ? 0 : b * p.cap;
+    const int to = paged ? (int)kv_row(p.pg, p.cap, b, k0) : seq_row + k0;
+    // ---- the slots' rows
+    int row = -1;
+    if (tid < rows) {
+      const int s = next_s < k0 + tid || next_s >= p.cap ? k0 + tid : next_s;   // (as source_of)
+      row = paged ? (int)kv_row(p.pg, p.cap, b, s) : seq_row + s;
+      if (row < 0 || to < 0) {
+        set_status(p.status, CC_ERR_DEVICE_ARG);   // no such page: the slot stays
+        row = -1;
+      }
+    }
+    src_sh[tid] = row;
+    __syncthreads();
+    // ---- 1. the sources, and meanwhile their exponents
+    const int q = tid & 7, r0 = tid >> 3;   // this thread's piece of 16 bytes, and first slot
+    if (small) {
+      if (row >= 0) {
+        uint32_t *v = reinterpret_cast<uint32_t *>(st) + tid;
+        v[0] = p.tokens[row];
+        v[C] = p.pos[row];
+        if (p.acc) v[2 * C] = __float_as_uint(p.acc[row]);
+      }
+    } else if (q < pieces) {
+      const uint32_t dst = smem_u32(st) + tid * 16;
+      const uint8_t *src = buf + first * row_bytes + column + q * 16;
+#pragma unroll
+      for (int i = 0; i < C / kRows; ++i) {
+        const int from = src_sh[r0 + kRows * i];
+        if (from >= 0) copy16(dst + i * kRows * kCompactWidth, src + (long long)from * row_bytes);
+      }
+    }
+    int e[2] = {-1, -1};
+    if (codes) {   // the maxima over 16 slots; a block is 1, 2, 4 or 8 of them
+      if (row >= 0) {
+        const uint8_t *at = exps + (p.pg.head_major ? (first + row) >> log_block : (long long)(row >> log_block) * p.hkv + g);
+        e[0] = at[0];
+        if (heads > 1) e[1] = at[1];
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        int m = row < 0 ? -1 : rank_of(e[h]);
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        if ((lane & 15) == 0) top_sh[h][tid >> 4] = m;
+      }
+    }
     // which chunks of the sequence read from this one's slots
     int r_lo = 0, r_hi = -1;
     if (tid < 32) {
-      const int *reader = p.reader + (size_t)b * p.reader_ld;
-      const int k_lo = reader[c], k_hi = reader[c + 1] - 1;
+      const int *reader = p.reader + (size_t)b * p.reader_ld + c;
+      const int k_lo = reader[0], k_hi = reader[1] - 1;
       r_lo = max(0, k_lo / C);
       r_hi = k_hi >= k_lo ? min(c - 1, k_hi / C) : -1;
     }
-    unsigned *flags = p.flags + (u - (long long)c * p.planes);   // of the sequence's first chunk
-    // ---- what the plane is: heads of an array of codes, columns of h, or the small arrays
-    const bool codes = plane < p.n_arrays * p.array_planes;
-    const bool small = plane == p.planes - 1;
-    const int array = codes ? plane / p.array_planes : 0, part = codes ? plane - array * p.array_planes
-                                                              : plane - p.n_arrays * p.array_planes;
-    uint8_t *buf;
-    long long row_bytes, column;   // bytes between slots, and of the plane's first byte in one
-    int width, heads = 0, g = 0;
-    if (codes) {
-      buf = p.codes[array];
-      if (p.pg.head_major) {
-        g = part;
-        heads = 1;
-        row_bytes = p.head_dim;
-        column = (long long)g * p.cap * p.head_dim;
-      } else {
-        const int each = kCompactWidth / p.head_dim;
-        g = part * each;
-        heads = min(each, p.hkv - g);
-        row_bytes = (long long)p.hkv * p.head_dim;
-        column = (long long)g * p.head_dim;
-      }
-      width = heads * p.head_dim;
-    } else {
-      buf = p.h;
-      row_bytes = p.h_bytes;
-      column = (long long)part * kCompactWidth;
-      width = small ? 0 : min(kCompactWidth, p.h_bytes - part * kCompactWidth);
+    chunk += chunk_step;
+    plane += plane_step;
+    if (plane >= p.planes) {
+      plane -= p.planes;
+      ++chunk;
     }
-    // ---- the slots' places and exponents
-    if (tid < C) {
-      const int k = k0 + tid;
-      long long from = -1, to = -1;
-      int e0 = -1, e1 = -1;
-      if (tid < rows) {
-        const int s = source_of(p, idx, k);
-        if (codes) {
-          long long sr, dr;
-          if (p.pg.head_major) {
-            sr = (long long)b * p.hkv * p.cap + s;
-            dr = (long long)b * p.hkv * p.cap + k;
-          } else {
-            sr = kv_row(p.pg, p.cap, b, s);
-            dr = kv_row(p.pg, p.cap, b, k);
-          }
-          if (sr < 0 || dr < 0) {
-            set_status(p.status, CC_ERR_DEVICE_ARG);   // no such page: the slot stays
-          } else {
-            from = sr * row_bytes + column;
-            to = dr * row_bytes + column;
-            const uint8_t *ex = p.exps[array];
-            if (p.pg.head_major) {
-              e0 = ex[(((long long)b * p.hkv + g) * p.cap + s) >> log_block];
-            } else {
-              const long long at = (sr >> log_block) * p.hkv + g;
-              e0 = ex[at];
-              if (heads > 1) e1 = ex[at + 1];
-            }
-          }
-        } else {
-          from = ((long long)b * p.cap + s) * row_bytes + column;
-          to = ((long long)b * p.cap + k) * row_bytes + column;
-        }
-        if (small) {
-          from = (long long)b * p.cap + s;
-          to = (long long)b * p.cap + k;
-        }
-      }
-      from_sh[tid] = from;
-      to_sh[tid] = to;
-      e_sh[0][tid] = e0;
-      e_sh[1][tid] = e1;
-    }
-    __syncthreads();
-    // ---- 1. the sources
-    const int pieces = width / 16;
-    uint32_t small_v[3] = {0, 0, 0};
-    if (small) {
-      if (tid < C && from_sh[tid] >= 0) {
-        const long long at = from_sh[tid];
-        small_v[0] = p.tokens[at];
-        small_v[1] = p.pos[at];
-        if (p.acc) small_v[2] = __float_as_uint(p.acc[at]);
-        uint32_t *v = reinterpret_cast<uint32_t *>(st);
-#pragma unroll
-        for (int i = 0; i < 3; ++i) v[i * C + tid] = small_v[i];
-      }
-    } else {
-      const uint32_t dst = smem_u32(st);
-      for (int i = tid; i < C * pieces; i += kThreads) {
-        const int r = i / pieces, q = i - r * pieces;
-        if (from_sh[r] >= 0) copy16(dst + r * kCompactWidth + q * 16, buf + from_sh[r] + q * 16);
-      }
-    }
-    // ---- the blocks' new exponents
-    if (tid < 2 * C) {
-      const int h = tid / C, r = tid - h * C;
-      const int first = r & ~(p.block - 1);
-      int top = -1, any = -1;
-      if (h < heads)
-        for (int i = 0; i < p.block; ++i) {
-          const int e = e_sh[h][first + i];
-          any = max(any, e);
-          if (e != kNoNumbers) top = max(top, e);
-        }
-      new_sh[h][r] = top >= 0 ? top : any;   // (none a number: stays 255; no slot: -1)
-    }
+    enter();
     copy_wait_all();
     __syncthreads();
-    // ---- 2. published; 3. the units that read from the destinations
+    // ---- 2. published; 3. the units that read from the destinations, and meanwhile the falls
     if (tid < 32) {
-      if (tid == 0) st_release(&flags[(long long)c * p.planes], 1u);
+      if (tid == 0) st_flag(flags + (size_t)c * p.planes);
       bool go = true;
-      for (int r = r_lo + tid; r <= r_hi; r += 32) go &= wait_flag(&flags[(long long)r * p.planes], p.status);
+      for (int r = r_lo + lane; r <= r_hi; r += 32) go &= wait_flag(flags + (size_t)r * p.planes, p.status);
       go = __all_sync(0xFFFFFFFFu, go);
       if (tid == 0) go_sh = go;
+    }
+    const bool stays = row < 0 || row == to + tid;
+    int top[2] = {-1, -1};   // ranks of the slot's blocks
+    if (codes) {
+      const int i0 = (tid >> 4) & ~((p.block >> 4) - 1);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        for (int i = 0; i < p.block >> 4; ++i) top[h] = max(top[h], top_sh[h][i0 + i]);
+        int fall = stays ? kStays : 0;
+        if (row >= 0 && rank_of(e[h]) != top[h]) fall = e[h] == kNoNumbers ? kNoFall : e[h] == 0 ? 255 : exponent_of(top[h]) - e[h];
+        fall_sh[h][tid] = fall;
+      }
+    } else {
+      fall_sh[0][tid] = stays ? kStays : 0;
     }
     __syncthreads();
     // ---- 4. the destinations
     if (go_sh) {
       if (small) {
-        if (tid < C && to_sh[tid] >= 0 && to_sh[tid] != from_sh[tid]) {
-          const uint32_t *v = reinterpret_cast<const uint32_t *>(st);
-          const long long at = to_sh[tid];
-          p.tokens[at] = v[tid];
-          p.pos[at] = v[C + tid];
-          if (p.acc) p.acc[at] = __uint_as_float(v[2 * C + tid]);
+        if (!stays) {
+          const uint32_t *v = reinterpret_cast<const uint32_t *>(st) + tid;
+          p.tokens[to + tid] = v[0];
+          p.pos[to + tid] = v[C];
+          if (p.acc) p.acc[to + tid] = __uint_as_float(v[2 * C]);
         }
-      } else {
-        for (int i = tid; i < C * pieces; i += kThreads) {
-          const int r = i / pieces, q = i - r * pieces;
-          if (to_sh[r] < 0) continue;
-          uint4 v = *reinterpret_cast<const uint4 *>(st + r * kCompactWidth + q * 16);
-          bool same = to_sh[r] == from_sh[r];
-          if (codes) {
-            const int h = q * 16 / p.head_dim, e = e_sh[h][r], e1 = new_sh[h][r];
-            if (e != e1) {
-              same = false;
-              v = e == kNoNumbers ? make_uint4(kNanCodes, kNanCodes, kNanCodes, kNanCodes)
-                                  : rescale(v, e == 0 ? 255 : e1 - e);
-            }
-          }
-          if (!same) *reinterpret_cast<uint4 *>(buf + to_sh[r] + q * 16) = v;
+      } else if (q < pieces) {
+        uint8_t *dst = buf + (first + to + r0) * row_bytes + column + q * 16;
+        const int *falls = fall_sh[codes ? q * 16 / p.head_dim : 0] + r0;
+        const uint4 *src = reinterpret_cast<const uint4 *>(st) + tid;
+#pragma unroll
+        for (int i = 0; i < C / kRows; ++i, dst += kRows * row_bytes) {
+          const int fall = falls[kRows * i];
+          if (fall < 0) continue;
+          uint4 v = src[kThreads * i];
+          if (fall > 0) v = fall == kNoFall ? make_uint4(kNanCodes, kNanCodes, kNanCodes, kNanCodes) : rescale(v, fall);
+          *reinterpret_cast<uint4 *>(dst) = v;
         }
-        if (codes && tid < 2 * C) {   // a block's first slot writes its exponent
-          const int h = tid / C, r = tid - h * C;
-          if (h < heads && r < rows && (r & (p.block - 1)) == 0 && new_sh[h][r] >= 0) {
-            // (the first slot's page, or that of the slots of its block: one page)
-            long long at;
-            if (p.pg.head_major) {
-              at = (((long long)b * p.hkv + g) * p.cap + k0 + r) >> log_block;
-            } else {
-              const long long dr = kv_row(p.pg, p.cap, b, k0 + r);
-              at = dr < 0 ? -1 : (dr >> log_block) * p.hkv + g + h;
-            }
-            if (at >= 0) p.exps[array][at] = (uint8_t)new_sh[h][r];
-          }
-        }
+      }
+      if (codes && tid < rows && (tid & (p.block - 1)) == 0 && to >= 0) {   // the blocks' exponents, by their first slots
+        uint8_t *at = p.exps[array] + (p.pg.head_major ? (first + to + tid) >> log_block
+                                                      : (long long)((to + tid) >> log_block) * p.hkv + g);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (h < heads && top[h] >= 0) at[h] = (uint8_t)exponent_of(top[h]);
       }
     }
     __syncthreads();   // shared memory is read
