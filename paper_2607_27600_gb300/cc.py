@@ -727,21 +727,20 @@ def cc_kv_join(cfg, parts, part_lses, out, lse=None, stream=None):
     """Attention over disjoint slots joined: parts (a list of [n_rows, Hq, dh] of one
     type) with their log-sum-exp (fp32 [n_rows, Hq] each) into out and lse (or None).
     out may be one of the parts, and lse one of theirs."""
-    c = _cfg(cfg)
-    k = len(parts)
+    c, k = _cfg(cfg), len(parts)
     if k < 1 or len(part_lses) != k:
         raise ValueError(f"{k} parts with {len(part_lses)} lse")
-    if any(x is None for x in (*parts, *part_lses, out)):
+    if out is None or any(x is None for x in parts) or any(x is None for x in part_lses):
         raise TypeError("parts, their lse and out must be CUDA tensors")
-    n, hq = out.shape[0], c.n_q_heads * c.head_dim
-    at = [_row_ptr(x, f"parts[{i}]", n, hq, out.dtype) for i, x in enumerate(parts)]
-    ptrs = (ctypes.c_void_p * k)(*[a[0] for a in at])
-    lds = (ctypes.c_int64 * k)(*[a[1] for a in at])
-    lses = (ctypes.c_void_p * k)(*[_vec_ptr(x, f"part_lses[{i}]", n * c.n_q_heads, torch.float32)
-                                   for i, x in enumerate(part_lses)])
+    n, dtype, heads = out.shape[0], out.dtype, c.n_q_heads
+    hq = heads * c.head_dim
+    ptrs, lds, lses = (ctypes.c_void_p * k)(), (ctypes.c_int64 * k)(), (ctypes.c_void_p * k)()
+    for i in range(k):
+        ptrs[i], lds[i] = _row_ptr(parts[i], "a part", n, hq, dtype)
+        lses[i] = _vec_ptr(part_lses[i], "a part's lse", n * heads, torch.float32)
     _check(load_library().cc_kv_join(
-        c, _dtype(out, "out"), n, k, ptrs, lds, lses, *_row_ptr(out, "out", n, hq, out.dtype),
-        _vec_ptr(lse, "lse", n * c.n_q_heads, torch.float32), _stream(stream)), "cc_kv_join")
+        c, _dtype(out, "out"), n, k, ptrs, lds, lses, *_row_ptr(out, "out", n, hq, dtype),
+        _vec_ptr(lse, "lse", n * heads, torch.float32), _stream(stream)), "cc_kv_join")
 
 
 def cc_kv_accumulate_workspace_size(cfg, cache: Cache, rows: Rows) -> int:

@@ -2095,6 +2095,7 @@ cc_status cc_kv_join(const cc_model_cfg *cfg, cc_dtype dtype, int32_t n_rows, in
   KvJoinParams p{};
   for (int i = 0; i < n_parts; ++i) {
     if (!rows_ok(cfg, part[i], part_ld[i], hq, bytes) || !part_lse[i]) return CC_ERR_INVALID_ARG;
+    if (part[i] == out && part_ld[i] != out_ld && n_rows > 1) return CC_ERR_INVALID_ARG;   // (in place row by row only)
     p.part[i] = part[i];
     p.part_ld[i] = part_ld[i];
     p.part_lse[i] = part_lse[i];

@@ -49,45 +49,83 @@ CC_DEV uint4 pack(const float (&x)[16 / sizeof(T)]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <typename T>
+// PARTS: their number where there are few, all of whose loads then start at once; 0: any
+// number, four at a time after all of their s_i.
+template <typename T, int PARTS>
 __global__ void __launch_bounds__(kThreads) kv_join_kernel(const __grid_constant__ KvJoinParams p) {
-  constexpr int E = 16 / sizeof(T);
+  constexpr int E = 16 / sizeof(T), CHUNK = PARTS > 0 ? PARTS : 4;
+  const int n_parts = PARTS > 0 ? PARTS : p.n_parts;
   const int per_head = p.head_dim / E, per_row = p.hq * per_head;   // threads
-  const long long at = (long long)blockIdx.x * kThreads + threadIdx.x;
+  const long long at = (long long)blockIdx.x * kThreads + threadIdx.x, end = (long long)p.n_rows * per_row;
   // (a warp's threads past the end, whole heads of them, leave together)
-  if (at >= (long long)p.n_rows * per_row) return;
+  if (at >= end) return;
   const unsigned team = __activemask();
-  const int row = (int)(at / per_row), in_row = (int)(at - (long long)row * per_row);
+  const int row = end < (1ll << 32) ? (int)((unsigned)at / (unsigned)per_row) : (int)(at / per_row);
+  const int in_row = (int)(at - (long long)row * per_row);
   const int head = in_row / per_head;
-  const long long rh = (long long)row * p.hq + head;
+  const long long rh = (long long)row * p.hq + head, elem = (long long)in_row * E;
+  uint4 u[CHUNK];
+  float s[CHUNK];
+  // (what a part that saw no slot holds is loaded with the others, and left out)
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int i = 0; i < CHUNK; ++i)
+      if (PARTS > 0 || i0 + i < n_parts) {
+        u[i] = __ldcs(reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(p.part[i0 + i]) +
+                                                      row * p.part_ld[i0 + i] + elem));
+        s[i] = p.part_lse[i0 + i][rh];
+      }
+  };
   float m = -INFINITY;
   bool bad = false;   // a row that failed in a part
-  for (int i = 0; i < p.n_parts; ++i) {
-    const float s = p.part_lse[i][rh];
-    bad |= !(s < INFINITY);
-    m = fmaxf(m, s);
+  load(0);
+  if constexpr (PARTS > 0) {
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+      bad |= !(s[i] < INFINITY);
+      m = fmaxf(m, s[i]);
+    }
+  } else {
+    for (int i = 0; i < n_parts; ++i) {
+      const float si = p.part_lse[i][rh];
+      bad |= !(si < INFINITY);
+      m = fmaxf(m, si);
+    }
   }
   float total = 0.f, y[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) y[e] = 0.f;
-  if (!bad && m > -INFINITY)
-    for (int i = 0; i < p.n_parts; ++i) {
-      const float w = exp2f((p.part_lse[i][rh] - m) * kLog2e);
+  for (int i0 = 0; i0 < n_parts; i0 += CHUNK) {
+    if (i0 > 0) load(i0);
+#pragma unroll
+    for (int i = 0; i < CHUNK; ++i) {
+      if (PARTS == 0 && i0 + i >= n_parts) break;
+      const float w = bad || s[i] == -INFINITY ? 0.f : exp2f((s[i] - m) * kLog2e);
       if (w == 0.f) continue;
       total += w;
       float x[E];
-      unpack<T>(*reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(p.part[i]) + row * p.part_ld[i] +
-                                                 (long long)in_row * E), x);
+      unpack<T>(u[i], x);
 #pragma unroll
       for (int e = 0; e < E; ++e) y[e] = fmaf(w, x[e], y[e]);
     }
-  if (total > 0.f) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) y[e] = y[e] / total;
   }
-  *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(p.out) + row * p.out_ld + (long long)in_row * E) = pack<T>(y);
+  const float inv = total > 0.f ? 1.f / total : 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) y[e] *= inv;
+  *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(p.out) + row * p.out_ld + elem) = pack<T>(y);
   __syncwarp(team);   // (lse may be one of the parts')
   if (p.lse && in_row % per_head == 0) p.lse[rh] = bad ? NAN : total > 0.f ? m + logf(total) : -INFINITY;
+}
+
+template <typename T>
+void launch(const KvJoinParams &p, unsigned grid, cudaStream_t st) {
+  switch (p.n_parts) {
+    case 1: kv_join_kernel<T, 1><<<grid, kThreads, 0, st>>>(p); break;
+    case 2: kv_join_kernel<T, 2><<<grid, kThreads, 0, st>>>(p); break;
+    case 3: kv_join_kernel<T, 3><<<grid, kThreads, 0, st>>>(p); break;
+    case 4: kv_join_kernel<T, 4><<<grid, kThreads, 0, st>>>(p); break;
+    default: kv_join_kernel<T, 0><<<grid, kThreads, 0, st>>>(p);
+  }
 }
 
 }  // namespace
@@ -96,9 +134,9 @@ cudaError_t launch_kv_join(const KvJoinParams &p, cudaStream_t st) {
   const int e = p.dtype == CC_F32 ? 4 : 8;
   const long long threads = (long long)p.n_rows * p.hq * p.head_dim / e;
   const unsigned grid = (unsigned)((threads + kThreads - 1) / kThreads);
-  if (p.dtype == CC_F32) kv_join_kernel<float><<<grid, kThreads, 0, st>>>(p);
-  else if (p.dtype == CC_F16) kv_join_kernel<__half><<<grid, kThreads, 0, st>>>(p);
-  else kv_join_kernel<__nv_bfloat16><<<grid, kThreads, 0, st>>>(p);
+  if (p.dtype == CC_F32) launch<float>(p, grid, st);
+  else if (p.dtype == CC_F16) launch<__half>(p, grid, st);
+  else launch<__nv_bfloat16>(p, grid, st);
   return cudaGetLastError();
 }
 

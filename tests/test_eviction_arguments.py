@@ -85,7 +85,7 @@ def test_join_is_checked(lib):  # noqa: F811
     bad = cc.CC_ERR_INVALID_ARG
     for kw in (dict(n=-1), dict(k=0), dict(dtype=3), dict(part=(BASE, None)), dict(part=(BASE + 8, BASE)),
                dict(ld=(512, 504)), dict(ld=(516, 512)), dict(lses=(None, BASE)), dict(out=None), dict(out=BASE + 4),
-               dict(out_ld=500), dict(dtype=2, ld=(514, 512))):
+               dict(out_ld=500), dict(dtype=2, ld=(514, 512)), dict(ld=(512, 520))):
         assert join(lib, **kw) == bad, kw
     assert lib.cc_kv_join(cfg(), 0, 4, 2, None, None, None, BASE, 512, None, None) == bad
     assert join(lib, k=17) == cc.CC_ERR_UNSUPPORTED
