@@ -39,7 +39,10 @@ constexpr int kThreads = 640;
 // Registers of a launch's 640 threads at 96 shared out anew between its five warpgroups.
 constexpr int kRegsSlots = 104, kRegsOthers = 64;
 static_assert(4 * kRegsSlots + kRegsOthers <= 5 * 96, "more registers than the block is launched with");
-constexpr int kUnitCost = 3;        // of a unit's start, in query tiles
+// Of a unit's start, in query tiles; and of one that some rows do not see, whose masked tiles take longer.
+// (With 3 for both the last shares end 10 % behind the others: 276 against 250 us for a chunk of 2048 rows
+// behind 16384 slots, 32 query heads on 8.)
+constexpr int kUnitCost = 5, kEdgeCost = 7;
 
 template <int DH>
 struct RtSmem {
@@ -78,7 +81,7 @@ CC_DEV int first_tile(const KvReceivedParams &p, const SeqLine &q, int kt) {
 }
 CC_DEV long long seq_length(const KvReceivedParams &p, const SeqLine &q) {
   long long n = (long long)q.nfull * (q.tiles + kUnitCost);
-  for (int kt = q.nfull; kt < q.nk; ++kt) n += q.tiles - first_tile(p, q, kt) + kUnitCost;
+  for (int kt = q.nfull; kt < q.nk; ++kt) n += q.tiles - first_tile(p, q, kt) + kEdgeCost;
   return n * p.hkv;
 }
 CC_DEV long long line_length(const KvReceivedParams &p) {   // a whole warp calls
@@ -139,7 +142,7 @@ struct Pieces {
       long long x = at - before;
       const int span0 = q.tiles + kUnitCost;
       const long long full = (long long)q.nfull * p.hkv * span0;
-      int span = span0, unit = 0;
+      int span = span0, unit = 0, cost = kUnitCost;
       t0 = 0;
       if (x < full) {
         unit = (int)(x / span0);
@@ -148,9 +151,10 @@ struct Pieces {
         g = unit - kt * p.hkv;
       } else {
         x -= full;
+        cost = kEdgeCost;
         for (kt = q.nfull; kt < q.nk; ++kt) {
           t0 = first_tile(p, q, kt);
-          span = q.tiles - t0 + kUnitCost;
+          span = q.tiles - t0 + kEdgeCost;
           if (x < (long long)span * p.hkv) break;
           x -= (long long)span * p.hkv;
         }
@@ -166,8 +170,8 @@ struct Pieces {
       at += to - from;
       begins = from == 0;
       whole = begins && to == span;
-      t1 = t0 + to - kUnitCost;
-      t0 += max(0, from - kUnitCost);
+      t1 = t0 + to - cost;
+      t0 += max(0, from - cost);
       if (t1 > t0) return true;   // (else the share ends before the unit's first tile)
     }
     return false;
@@ -379,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         continue;
       }
-      const int slot0 = u.kt * kUnitSlots + w * KT;
+      const int slot0 = u.kt * kUnitSlots + w * KT, warp_slot0 = slot0 + (warp & 3) * 32;
       // ---- the slots' codes, a slot's scale a factor of its scores (-1: there is no such page)
       {
         const int slot = slot0 + r;
@@ -460,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&s_empty[buf]);   // copied out: the buffer may be refilled
-          if (live && slot0 + KT - 1 <= seen_first) {
+          if (live && warp_slot0 + 31 <= seen_first) {
 #pragma unroll
             for (int k = 0; k < CH / 8; ++k) {
               const float4 y = terms[4 * k];   // of two columns -y and e^-rest
@@ -475,12 +479,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
               for (int i = 0; i < 4; ++i) acc[i] = __ffma2_rn(x[i], make_float2(y.z, y.w), acc[i]);
             }
-          } else if (slot0 <= seen_last) {   // (some row sees some slot)
+          } else if (warp_slot0 <= seen_last) {   // (some row sees some slot)
             // of the lane's columns (8 k, and 8 k + 1), the first that sees the slot
             int from[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              from[i] = p.memory_only ? -1 : (slot0 + (warp & 3) * 32 + mine + 8 * i - pos) * G - col0 - 2 * quad;
+              from[i] = p.memory_only ? -1 : (warp_slot0 + mine + 8 * i - pos) * G - col0 - 2 * quad;
             // (chosen, not multiplied by 0: what a row does not see, or one that adds nothing, may be no number)
             auto weigh = [&](auto some_dead) {
               constexpr bool dead = decltype(some_dead)::value;
@@ -549,21 +553,22 @@ __global__ void __launch_bounds__(kUnitSlots) finish_kernel(const __grid_constan
     if (g0 + tid < p.hkv) {
       const int g = g0 + tid;
       const int span0 = q.tiles + kUnitCost;
-      int span = span0;
+      int span = span0, cost = kUnitCost;
       long long at = before;
       if (kt < q.nfull) {
         at += ((long long)kt * p.hkv + g) * span0;
       } else {
         at += (long long)q.nfull * p.hkv * span0;
-        for (int k = q.nfull; k < kt; ++k) at += (long long)(q.tiles - first_tile(p, q, k) + kUnitCost) * p.hkv;
-        span = q.tiles - first_tile(p, q, kt) + kUnitCost;
+        for (int k = q.nfull; k < kt; ++k) at += (long long)(q.tiles - first_tile(p, q, k) + kEdgeCost) * p.hkv;
+        cost = kEdgeCost;
+        span = q.tiles - first_tile(p, q, kt) + kEdgeCost;
         at += (long long)g * span;
       }
       const int c0 = share_at(at, total, n);
       int lo = c0;
       const int c1 = share_at(at + span - 1, total, n);
       // (shares that end before the first query tile have no sums)
-      while (lo < c1 && total * (lo + 1) / n - at <= kUnitCost) ++lo;
+      while (lo < c1 && total * (lo + 1) / n - at <= cost) ++lo;
       first_sh[tid] = c0 == c1 ? -1 : lo * 2 + (lo == c0 ? 1 : 0);
       last_sh[tid] = c1;
     }
