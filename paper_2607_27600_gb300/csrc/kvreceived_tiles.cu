@@ -539,14 +539,19 @@ __global__ void __launch_bounds__(kThreads, 1)
 __global__ void __launch_bounds__(kUnitSlots) finish_kernel(const __grid_constant__ KvReceivedParams p) {
   // of each KV head's unit: the first share with query tiles of it (-1: it lies in one), the last
   __shared__ int first_sh[kUnitSlots], last_sh[kUnitSlots];
-  pdl_wait();
   const int per_seq = (p.rows.cap + kUnitSlots - 1) / kUnitSlots, tid = threadIdx.x;
   const int b = blockIdx.x / per_seq, kt = blockIdx.x - b * per_seq;
   const SeqLine q = seq_line(p, b);
-  if (kt >= q.nk) return;
+  if (kt >= q.nk) {
+    pdl_wait();
+    return;
+  }
   const long long total = line_length(p), before = length_before(p, b);
   const int n = line_shares(p.shares, total);
   const int slot = kt * kUnitSlots + tid;
+  float *dst = p.acc + (long long)b * p.rows.cap + slot;
+  // (the other kernel leaves the accumulators alone: only its sums are waited for)
+  const float old = slot < q.keys && !(p.first && slot >= q.s.seq) ? *dst : 0.f;
   float sum = 0.f;
   for (int g0 = 0; g0 < p.hkv; g0 += kUnitSlots) {
     __syncthreads();
@@ -573,27 +578,33 @@ __global__ void __launch_bounds__(kUnitSlots) finish_kernel(const __grid_constan
       last_sh[tid] = c1;
     }
     __syncthreads();
-    if (slot < q.keys)
-      for (int i = 0; i < min(kUnitSlots, p.hkv - g0); ++i) {
-        const int first = first_sh[i];   // share, and whether the unit begins there
-        if (first < 0) {
-          const float2 x = reinterpret_cast<const float2 *>(p.part)[((long long)(g0 + i) * p.rows.batch + b) * p.rows.cap + slot];
-          sum += x.x + x.y;
-          continue;
-        }
-        const float2 *cut = reinterpret_cast<const float2 *>(p.cut);
-        float2 x = cut[first * kUnitSlots + tid];
-        for (int c = first / 2 + 1; c <= last_sh[i]; ++c) {
-          const float2 y = cut[2 * c * kUnitSlots + tid];
-          x = make_float2(x.x + y.x, x.y + y.y);
-        }
-        sum += x.x + x.y;
+    if (g0 == 0) pdl_wait();
+    if (slot >= q.keys) continue;
+    const float2 *cut = reinterpret_cast<const float2 *>(p.cut) + tid;
+    const float2 *part = reinterpret_cast<const float2 *>(p.part) + (long long)b * p.rows.cap + slot;
+    const int heads = min(kUnitSlots, p.hkv - g0);
+    for (int i0 = 0; i0 < heads; i0 += 4) {   // (the loads of four heads together)
+      float2 x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (i0 + j >= heads) break;
+        const int first = first_sh[i0 + j];   // share, and whether the unit begins there
+        x[j] = first < 0 ? part[(long long)(g0 + i0 + j) * p.rows.batch * p.rows.cap] : cut[first * kUnitSlots];
       }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (i0 + j >= heads) break;
+        const int first = first_sh[i0 + j];
+        if (first >= 0)
+          for (int c = first / 2 + 1; c <= last_sh[i0 + j]; ++c) {
+            const float2 y = cut[2 * c * kUnitSlots];
+            x[j] = make_float2(x[j].x + y.x, x[j].y + y.y);
+          }
+        sum += x[j].x + x[j].y;
+      }
+    }
   }
-  if (slot < q.keys) {
-    float *dst = p.acc + (long long)b * p.rows.cap + slot;
-    *dst = (p.first && slot >= q.s.seq ? 0.f : *dst) + sum;
-  }
+  if (slot < q.keys) *dst = old + sum;
 }
 
 template <int DH, bool F16>
