@@ -22,8 +22,13 @@
 // (cooperative launch), and a unit waits only on lower ones after publishing its own, so
 // that nothing can deadlock.  A slot that stays where it is and keeps its scale is not written.
 //
-// Bound by HBM: kept codes are read once and written once.  Eight small CTAs an SM hide
-// a unit's chain of loads (indices, exponents and codes, flags).
+// Bound by HBM: kept codes are read once and written once.  Ten small CTAs an SM hide
+// a unit's chain of loads (indices, exponents and codes, flags).  32 layers of 16384 slots to
+// 4096, 8 heads of 128: 105 us, 5.1 TB/s; six ragged sequences that keep nearly all, 4 layers:
+// 135 us, 4.1 TB/s, some 18 us of it waits for lower units, of which few layers leave
+// little else to do; 4 layers of 131072 slots to 8192: 31 us, 2.2 TB/s: a chain of the pre-pass
+// and one unit a CTA.  Measured slower: a second buffer, so that the next unit's codes come
+// during a unit's waits (fewer CTAs fit).
 #include "kvcompact.cuh"
 
 #include <algorithm>

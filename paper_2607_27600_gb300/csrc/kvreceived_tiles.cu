@@ -1,10 +1,10 @@
 // kvreceived_tiles.cu -- the attention that the slots of a block-scaled cache receive
 // from chunks of rows (kvreceived.cu has the definition, and few rows).
 //
-// Bound by the tensor cores and, about as much, by the exponentials: with 128 slots
-// as the M rows of a tcgen05 product and 96 query rows as its N, each thread has a slot
-// and adds that slot's own weights, no sum crosses threads, and the slot's scale is
-// a factor of the thread.  The key codes become bf16 (fp16 for fp16 rows; exact, without
+// The floor is the tensor cores' and, about as high, the exponentials': 128 slots are the
+// M rows of a tcgen05 product and 96 query rows its N, so that a lane keeps the same slots
+// from tile to tile, adds their weights in registers, and has their scales as factors.
+// The key codes become bf16 (fp16 for fp16 rows; exact, without
 // their scale) once per unit and stay in tensor memory as the A operand; the query
 // tiles stream through shared memory by TMA, each for both of a CTA's slot tiles.
 //
@@ -19,6 +19,14 @@
 //                    (warp 17 has the tensor memory)
 //   warp 18          query tiles (TMA)
 //   warp 19          the rows' terms
+//
+// A chunk of 2048 rows behind 16384 slots, 32 query heads of 128 on 8: 241 us (1.2 PFLOP/s:
+// products alone take 150 us, tensor pipe and exponentials each busy half of the time,
+// instructions issued in 63 % of it).  What is left is the slots' warps: without their
+// arithmetic a tile's hand-overs between the roles still take 215 us.
+// Measured slower: weights of a tile's 96 columns by every other four warps (277 us; a buffer
+// of scores is held for longer), scores taken 16 columns at a time (298), the next unit's codes
+// fetched ahead (the same).
 //
 // A row's y is its rounded part, which the scores' multiply-add takes off, and a factor
 // e^-rest of its weights.
@@ -460,6 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int pos = u.q.s.seq + t * p.P;
           const int seen_first = p.memory_only ? 0x7FFFFFFF : pos + first_pos;
           const int seen_last = p.memory_only ? 0x7FFFFFFF : pos + last_pos;
+          const float4 y0 = terms[0];   // (while the scores come; there are no registers for more)
           tmem_ld_wait();
           tc_fence_before();
           __syncwarp();
@@ -467,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (live && warp_slot0 + 31 <= seen_first) {
 #pragma unroll
             for (int k = 0; k < CH / 8; ++k) {
-              const float4 y = terms[4 * k];   // of two columns -y and e^-rest
+              const float4 y = k == 0 ? y0 : terms[4 * k];   // of two columns -y and e^-rest
               float2 x[4];
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
