@@ -493,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             int from[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              from[i] = p.memory_only ? -1 : (warp_slot0 + mine + 8 * i - pos) * G - col0 - 2 * quad;
+              from[i] = p.memory_only ? -1 : max(warp_slot0 + mine + 8 * i - pos, 0) * G - col0 - 2 * quad;   // (none is above P + 31)
             // (chosen, not multiplied by 0: what a row does not see, or one that adds nothing, may be no number)
             auto weigh = [&](auto some_dead) {
               constexpr bool dead = decltype(some_dead)::value;

@@ -2,6 +2,8 @@
 that is held once, attention over it and over each sequence's own memory joined, totals
 of what every slot receives, a refresh by them, and on; eagerly and replayed from
 graphs that share a workspace, on a stream of its own; offsets past 32 bits."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -287,3 +289,31 @@ def test_offsets_past_32_bits(pkg):
             np.testing.assert_array_equal(e[0, :len(tops)].cpu().numpy(), tops)
         np.testing.assert_array_equal(d["tokens"][0, :len(keep)].cpu().numpy(), keep)
         del d, cache
+
+
+def test_a_dead_row_among_many_heads_behind_a_long_memory(pkg):
+    """Slots so far before the rows that distance times heads passes 32 bits, next to a row that adds
+    nothing (so that each weight is chosen).  Scores are 0: a slot gets the live rows' heads times e^-3.
+    672 equal terms in fp32 differ from that by at most 672 * 2^-24, and each by under 2^-20."""
+    from paper_2607_27600_gb300 import cc
+    heads, dh, block, cap, m = 96, 64, 128, 1 << 25, 8
+    n = cap - 256
+    assert n * heads > 2 ** 31
+    s = shape(heads, 1, dh)
+    d = {x: [torch.zeros(1, cap, 1, dh, dtype=torch.uint8, device="cuda")] for x in "kv"}
+    d.update({x + "_exp": [torch.full((1, cap // block, 1), 127, dtype=torch.uint8, device="cuda")] for x in "kv"})
+    d.update(kv_block=block, seq_len=torch.tensor([n], dtype=torch.int32, device="cuda"),
+             tokens=torch.zeros(1, cap, dtype=torch.int32, device="cuda"),
+             pos=torch.zeros(1, cap, dtype=torch.int32, device="cuda"), h2o_acc=torch.zeros(1, cap, device="cuda"))
+    cache = pkg.Cache(d)
+    rows = pkg.Rows(m, torch.tensor([0, m], dtype=torch.int32, device="cuda"), None, m)
+    q = torch.zeros(m, heads, dh, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((m, heads), 3.0, device="cuda")
+    lse[3] = -float("inf")
+    cc.cc_kv_accumulate(s, cache, 0, rows, q, lse, cc.alloc_workspace(cc.cc_kv_accumulate_workspace_size(s, cache, rows)))
+    assert cc.cc_get_status() == cc.CC_OK
+    live = torch.full((cap,), 7.0, dtype=torch.float64, device="cuda")
+    live[n:n + m] = torch.tensor([7.0, 6, 5, 4, 4, 3, 2, 1], dtype=torch.float64, device="cuda")
+    live[n + m:] = 0
+    want = live * heads * math.exp(-3)
+    assert ((d["h2o_acc"][0].double() - want).abs() <= (672 * 2.0 ** -24 + 2.0 ** -20) * want).all()
