@@ -545,7 +545,12 @@ cc_status cc_kv_join(const cc_model_cfg *cfg, cc_dtype dtype, int32_t n_rows, in
  *   lse:   device fp32 [n_rows][Hq].  A row and head whose lse is not finite adds
  *          nothing, whatever the slots hold.
  * Block format only (others: CC_ERR_UNSUPPORTED).  Slots that no row sees keep their
- * totals.  Sums run in a fixed order: the same call gives the same bits. */
+ * totals.  Sums run in a fixed order: the same call gives the same bits.
+ * Chunks take tiles by the rule for bf16 of cc_kv_attention (up to 96 query heads
+ * per KV head; one kernel for the whole call), whose workspace goes by room: 8 * Hkv
+ * bytes for each of batch * cap slots.  There q . K is summed before K's scale: it
+ * must not pass 2^128.  Other rows need next to none.  At most 2^31 - 4097 slots
+ * a sequence (more: CC_ERR_UNSUPPORTED), as in cc_kv_compact. */
 size_t cc_kv_accumulate_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *cache,
                                        const cc_rows *rows);
 cc_status cc_kv_accumulate(const cc_model_cfg *cfg, const cc_kv_cache *cache, int32_t layer,

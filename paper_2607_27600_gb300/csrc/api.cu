@@ -2117,6 +2117,8 @@ cc_status cc_kv_join(const cc_model_cfg *cfg, cc_dtype dtype, int32_t n_rows, in
 
 namespace {
 
+constexpr int kMaxSlots = 0x7FFFFFFF - 4096;   // of a sequence: rounded up to a unit they stay below 2^31
+
 KvReceivedParams kv_received_params(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows, int sms) {
   KvReceivedParams p{};
   p.rows = step_rows(kv, rows);
@@ -2148,7 +2150,7 @@ cc_status kv_compact_params(const cc_model_cfg *c, const cc_kv_cache *kv, KvComp
   if (!kv || kv->batch < 1 || kv->cap < 1 || !kv->k || !kv->v || !kv->tokens || !kv->pos || !kv->seq_len ||
       !kv_layout_ok(kv))
     return CC_ERR_INVALID_ARG;
-  if (kv->kv_format != CC_KV_E4M3_BLOCK) return CC_ERR_UNSUPPORTED;
+  if (kv->kv_format != CC_KV_E4M3_BLOCK || kv->cap > kMaxSlots) return CC_ERR_UNSUPPORTED;
   if (!block_size_ok(kv) || !kv->k_exp || !kv->v_exp) return CC_ERR_INVALID_ARG;
   if ((uint64_t)kv->batch * kv->cap >= (1ull << 31) || kv->batch > 65534 || 2 * c->n_layers > kMaxBlockArrays)
     return CC_ERR_UNSUPPORTED;
@@ -2197,6 +2199,7 @@ cc_status cc_kv_accumulate(const cc_model_cfg *cfg, const cc_kv_cache *kv, int32
   if (kv->kv_format != CC_KV_E4M3_BLOCK || dtype == CC_F32) return CC_ERR_UNSUPPORTED;
   if (dtype != CC_BF16 && dtype != CC_F16) return CC_ERR_INVALID_ARG;
   if (!kv->h2o_acc || (first && memory_only)) return CC_ERR_INVALID_ARG;
+  if (kv->cap > kMaxSlots) return CC_ERR_UNSUPPORTED;
   if (rows->n_rows == 0) return CC_OK;
   if (!rows_ok(cfg, q, q_ld, cfg->n_q_heads, 2) || !lse) return CC_ERR_INVALID_ARG;
   if (!ws || !aligned16(ws) || ws_bytes < cc_kv_accumulate_workspace_size(cfg, kv, rows))

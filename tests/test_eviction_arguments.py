@@ -105,3 +105,10 @@ def test_binding_refuses_before_the_call():
         cc.cc_kv_join(cfg(), [x, None], [torch.zeros(4, 8)] * 2, x)
     with pytest.raises(TypeError):
         cc.cc_kv_join(cfg(), [x], [torch.zeros(4, 8)], x)   # not on a device
+
+
+def test_sequences_next_to_31_bits(lib):  # noqa: F811
+    from paper_2607_27600_gb300 import cc
+    cap = (1 << 31) - 128
+    assert accumulate(lib, kv=cache(h2o_acc=BASE, cap=cap, batch=1)) == cc.CC_ERR_UNSUPPORTED
+    assert compact(lib, kv=cache(cap=cap, batch=1)) == cc.CC_ERR_UNSUPPORTED
