@@ -61,7 +61,8 @@ __global__ void __launch_bounds__(kThreads) kv_join_kernel(const __grid_constant
   const long long at = (long long)blockIdx.x * kThreads + threadIdx.x, end = (long long)p.n_rows * per_row;
   // (a warp's threads past the end, whole heads of them, leave together)
   if (at >= end) return;
-  const unsigned team = __activemask();
+  const long long stay = end - (at - (threadIdx.x & 31));
+  const unsigned team = stay < 32 ? (1u << stay) - 1u : ~0u;
   const int row = end < (1ll << 32) ? (int)((unsigned)at / (unsigned)per_row) : (int)(at / per_row);
   const int in_row = (int)(at - (long long)row * per_row);
   const int head = in_row / per_head;
