@@ -15,8 +15,8 @@
 // share's sequence lie in shared memory as operands, scaled by a power of two per row so
 // that bf16 ones fit fp16 exactly.
 //
-// 64 sequences of up to 17000 slots, a row each of 32 heads of 128 on 8: 213 us, 5.3 TB/s
-// of codes and exponents; 16 sequences of up to 9000, five rows each: 31 us, 2.5 TB/s: too short for
+// 64 sequences of 1500 to 32767 slots, a row each of 32 heads of 128 on 8: 213 us, 5.3 TB/s
+// of codes and exponents; 16 sequences of 250 to 9001, five rows each: 33 us, 2.4 TB/s: too short for
 // more, and with 24 columns of scores 16 warps an SM instead of 24.  Bound by the latency of
 // the loads (long scoreboard first among the stalls, DRAM busy 67 % at 32 sequences).
 #include "kvreceived.cuh"
@@ -304,10 +304,18 @@ __global__ void __launch_bounds__(kWarps * 32, resident(TILES))
                   }
                 }
               };
-              if constexpr (TILES > 0) {
-                float d[TILES][4];
+              // (two chains of products: a step drops the bits below its sum's last, always downwards;
+              // one chain's totals are 2.2e-6 off over 8192 slots, two chains' 0.9e-6)
+              auto add = [](float (&d)[4], const float (&d2)[4]) {
 #pragma unroll
-                for (int t = 0; t < TILES; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.f;
+                for (int c = 0; c < 4; ++c) d[c] += d2[c];
+              };
+              if constexpr (TILES > 0) {
+                float d[TILES][4], d2[TILES][4];
+#pragma unroll
+                for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                  for (int c = 0; c < 4; ++c) d[t][c] = d2[t][c] = 0.f;
 #pragma unroll
                 for (int k = 0; k < KS; k += 2) {
                   uint32_t op[2][4];
@@ -322,12 +330,15 @@ __global__ void __launch_bounds__(kWarps * 32, resident(TILES))
                   for (int t = 0; t < TILES; ++t) {
                     const uint4 q4 = qh[(t * (KS / 2) + k / 2) * 32];
                     mma_f16(d[t], op[0][0], op[0][1], op[0][2], op[0][3], q4.x, q4.y);
-                    mma_f16(d[t], op[1][0], op[1][1], op[1][2], op[1][3], q4.z, q4.w);
+                    mma_f16(d2[t], op[1][0], op[1][1], op[1][2], op[1][3], q4.z, q4.w);
                   }
                 }
                 if (left > 1) load(i);
 #pragma unroll
-                for (int t = 0; t < TILES; ++t) weigh(d[t], rt + 8 * t);
+                for (int t = 0; t < TILES; ++t) {
+                  add(d[t], d2[t]);
+                  weigh(d[t], rt + 8 * t);
+                }
               } else {
                 uint32_t op[KS][4];
 #pragma unroll
@@ -340,13 +351,14 @@ __global__ void __launch_bounds__(kWarps * 32, resident(TILES))
                 if (left > 1) load(i);
 #pragma unroll 1
                 for (int t = 0; t < tiles; ++t, qh += KS / 2 * 32) {
-                  float d[4] = {0.f, 0.f, 0.f, 0.f};
+                  float d[4] = {0.f, 0.f, 0.f, 0.f}, d2[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                   for (int k = 0; k < KS / 2; ++k) {
                     const uint4 q4 = qh[k * 32];
                     mma_f16(d, op[2 * k][0], op[2 * k][1], op[2 * k][2], op[2 * k][3], q4.x, q4.y);
-                    mma_f16(d, op[2 * k + 1][0], op[2 * k + 1][1], op[2 * k + 1][2], op[2 * k + 1][3], q4.z, q4.w);
+                    mma_f16(d2, op[2 * k + 1][0], op[2 * k + 1][1], op[2 * k + 1][2], op[2 * k + 1][3], q4.z, q4.w);
                   }
+                  add(d, d2);
                   weigh(d, rt + 8 * t);
                 }
               }
