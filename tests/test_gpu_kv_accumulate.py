@@ -129,6 +129,43 @@ def test_chunks_match_oracle(pkg, hq, hkv, dh, block, layout, cap, lens, counts,
     np.testing.assert_array_equal(c.run(), got)
 
 
+WIDE = [
+    # groups of many heads: a tile of one or two positions, and more than a tile holds
+    (96, 1, 64, 16, "paged", 256, [50, 130], [70, 2]),
+    (56, 1, 128, 64, "slot", 384, [301], [33]),
+    (48, 1, 64, 32, "head", 256, [0, 200], [41, 5]),
+    (128, 1, 64, 16, "slot", 256, [100, 3], [40, 1]),
+    (256, 1, 128, 32, "head", 256, [30, 77], [5, 0]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hq,hkv,dh,block,layout,cap,lens,counts", WIDE)
+def test_wide_groups(pkg, hq, hkv, dh, block, layout, cap, lens, counts, dtype):
+    from paper_2607_27600_gb300 import cc
+    c = Case(pkg, hq * 1000 + cap, hq, hkv, dh, block, layout, dtype, cap, lens, counts, False)
+    got = c.run()
+    assert cc.cc_get_status() == cc.CC_OK
+    c.check(got)
+    np.testing.assert_array_equal(c.run(), got)
+
+
+@pytest.mark.parametrize("memory", [False, True])
+@pytest.mark.parametrize("most", [3, 90])
+def test_many_sequences(pkg, most, memory):
+    """More sequences than a warp has lanes, some without slots, some without rows."""
+    from paper_2607_27600_gb300 import cc
+    rng = np.random.default_rng(most)
+    lens, counts = rng.integers(0, 160, 70), rng.integers(0, most + 1, 70)
+    lens[rng.integers(0, 70, 20)] = 0
+    counts[rng.integers(0, 70, 20)] = 0
+    c = Case(pkg, most, 8, 2, 64, 32, "paged", "bf16", 256, [int(x) for x in lens], [int(x) for x in counts], memory)
+    got = c.run()
+    assert cc.cc_get_status() == cc.CC_OK
+    c.check(got)
+    np.testing.assert_array_equal(c.run(), got)
+
+
 @pytest.mark.parametrize("counts", [[1, 1, 1], [100, 3, 64]])
 def test_first_layer_of_a_step(pkg, counts):
     """The rows' own slots start from 0, whatever they held."""
