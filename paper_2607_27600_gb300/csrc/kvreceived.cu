@@ -30,8 +30,10 @@ namespace {
 
 constexpr int kWarps = 8;
 constexpr int kStep = 16;            // slots of a warp's step
-// CTAs per SM.
-constexpr int resident(int tiles) { return tiles == 1 ? 3 : 2; }
+// CTAs per SM: two, and three where one tile of query rows leaves the registers and the cache has
+// room for so many slots that it pays.  Two and three, 32/8 heads, a row each: 64 sequences of 32000
+// slots 212 and 203 us, 32 of 16600 114 and 114, one of 16384 12.8 and 14.9; 28/4 heads, one of 8191 8.2 and 10.6.
+constexpr long long kManySteps = 128;   // of a CTA
 constexpr int kSegment = 32;         // steps between joins of the warps' sums
 constexpr int kQueryBytes = 92 * 1024;   // of the queries in shared memory, at most
 
@@ -104,8 +106,8 @@ struct __align__(16) RowTerm {
 
 // TILES: eights of query rows of a KV head in a pass where there are few, all of which take the
 // slots' widened codes as they are made; 0: any number, which are widened first.
-template <typename T, int DH, int TILES>
-__global__ void __launch_bounds__(kWarps * 32, resident(TILES))
+template <typename T, int DH, int TILES, int RESIDENT>
+__global__ void __launch_bounds__(kWarps * 32, RESIDENT)
     kv_received_kernel(const __grid_constant__ KvReceivedParams p) {
   constexpr int KS = DH / 16;        // k steps of K Q^T
   constexpr int W = DH / 16;         // words of a slot that a lane holds
@@ -395,24 +397,24 @@ size_t smem_bytes(const KvReceivedParams &p) {
   return (size_t)p.heads_at_once * p.tiles_at_once * (p.head_dim / 16 * 256 + 8 * sizeof(RowTerm));
 }
 
-template <typename T, int DH, int TILES>
+template <typename T, int DH, int TILES, int RESIDENT = 2>
 cudaError_t launch_tiles(const KvReceivedParams &p, cudaStream_t st) {
   static bool attr_set[64] = {};
   int dev = 0;
   cudaGetDevice(&dev);
   if (dev < 64 && !attr_set[dev]) {
-    const cudaError_t e = cudaFuncSetAttribute(kv_received_kernel<T, DH, TILES>,
+    const cudaError_t e = cudaFuncSetAttribute(kv_received_kernel<T, DH, TILES, RESIDENT>,
                                                cudaFuncAttributeMaxDynamicSharedMemorySize, kQueryBytes);
     if (e != cudaSuccess) return e;
     attr_set[dev] = true;
   }
-  kv_received_kernel<T, DH, TILES><<<p.shares, kWarps * 32, smem_bytes(p), st>>>(p);
+  kv_received_kernel<T, DH, TILES, RESIDENT><<<p.shares, kWarps * 32, smem_bytes(p), st>>>(p);
   return cudaGetLastError();
 }
 template <typename T, int DH>
 cudaError_t launch(const KvReceivedParams &p, cudaStream_t st) {
   switch (p.tiles_at_once) {
-    case 1: return launch_tiles<T, DH, 1>(p, st);
+    case 1: return p.resident == 3 ? launch_tiles<T, DH, 1, 3>(p, st) : launch_tiles<T, DH, 1>(p, st);
     case 2: return launch_tiles<T, DH, 2>(p, st);
     case 3: return launch_tiles<T, DH, 3>(p, st);
     default: return launch_tiles<T, DH, 0>(p, st);
@@ -429,7 +431,9 @@ void kv_received_plan(KvReceivedParams &p, int sms) {
   const long long tiles = ((long long)p.rows.max_rows * G + 7) / 8;
   p.tiles_at_once = (int)std::min<long long>(tiles, room / p.heads_at_once);
   const long long most = (long long)p.rows.batch * ((p.rows.cap + kStep - 1) / kStep);
-  p.shares = (int)std::min<long long>((long long)sms * resident(p.tiles_at_once), most);
+  p.resident = p.tiles_at_once == 1 && most > sms * 3 * kManySteps ? 3 : 2;
+  // (two steps a CTA at least: each brings the queries in for itself)
+  p.shares = (int)std::min<long long>((long long)sms * p.resident, (most + 1) / 2);
 }
 
 cudaError_t launch_kv_received(const KvReceivedParams &p, cudaStream_t st) {

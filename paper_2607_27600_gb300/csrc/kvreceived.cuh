@@ -23,6 +23,7 @@ struct KvReceivedParams {
   int heads_at_once;            // KV heads of a pass over a share's slots
   int tiles_at_once;            // eights of query rows of a KV head in a pass
   int shares;                   // CTAs
+  int resident;                 // of them on an SM
   // chunks (set by launch_kv_received_tiles)
   int P;                        // positions of a query tile
   float *part;                  // [hkv][batch][cap][2]: the sums of whole units, over half of the rows each
