@@ -2137,8 +2137,8 @@ KvReceivedParams kv_received_params(const cc_model_cfg *c, const cc_kv_cache *kv
 
 // Whether a step's rows take the tiles: by the attention's rule for bf16, for either type (the
 // products are of one fp16 or bf16 operand each).  Direct and tiles, 8192 slots: 8 sequences
-// of 32/8 heads: 64 rows of a KV head 31 and 31 us, 128 rows 56 and 32; one sequence of 28/4:
-// 56 rows 15 and 15, 112 rows 23 and 17.
+// of 16/4 heads: 80 rows of a KV head 34 and 44 us, 96 rows 44 and 42; one sequence of 28/4:
+// 56 rows 13 and 15, 84 rows 19 and 15.
 bool received_on_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows) {
   return c->n_q_heads / c->n_kv_heads <= kReceivedMaxGroup && step_on_tiles(c, kv, rows, false);
 }

@@ -31,8 +31,9 @@ namespace {
 constexpr int kWarps = 8;
 constexpr int kStep = 16;            // slots of a warp's step
 // CTAs per SM: two, and three where one tile of query rows leaves the registers and the cache has
-// room for so many slots that it pays.  Two and three, 32/8 heads, a row each: 64 sequences of 32000
-// slots 212 and 203 us, 32 of 16600 114 and 114, one of 16384 12.8 and 14.9; 28/4 heads, one of 8191 8.2 and 10.6.
+// room for so many slots that it pays.  Two and three, a row each: 64 sequences of 32000 slots, 16/4
+// heads, 212 and 203 us; 32 of 16600, 32/8 heads, 114 and 114; four of 16384, 16/4 heads, 12.8 and 14.9; one of
+// 8191, 28/4 heads, 8.2 and 10.6.
 constexpr long long kManySteps = 128;   // of a CTA
 constexpr int kSegment = 32;         // steps between joins of the warps' sums
 constexpr int kQueryBytes = 92 * 1024;   // of the queries in shared memory, at most
