@@ -489,11 +489,14 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int i = 0; i < 4; ++i) acc[i] = __ffma2_rn(x[i], make_float2(y.z, y.w), acc[i]);
             }
           } else if (warp_slot0 <= seen_last) {   // (some row sees some slot)
-            // of the lane's columns (8 k, and 8 k + 1), the first that sees the slot
+            // of the lane's columns (8 k, and 8 k + 1), the first that sees the slot; none where no row of the
+            // tile does: the columns that hold no query come behind the rows, and 0 times no number is none
             int from[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              from[i] = p.memory_only ? -1 : max(warp_slot0 + mine + 8 * i - pos, 0) * G - col0 - 2 * quad;   // (none is above P + 31)
+            for (int i = 0; i < 4; ++i) {
+              const int after = warp_slot0 + mine + 8 * i - pos;   // (at most P + 31)
+              from[i] = p.memory_only ? -1 : after >= p.P ? QT : max(after, 0) * G - col0 - 2 * quad;
+            }
             // (chosen, not multiplied by 0: what a row does not see, or one that adds nothing, may be no number)
             auto weigh = [&](auto some_dead) {
               constexpr bool dead = decltype(some_dead)::value;
