@@ -569,9 +569,10 @@ cc_status cc_kv_accumulate(const cc_model_cfg *cfg, const cc_kv_cache *cache, in
  * keep_count[b] keep their bits.
  * A count outside [0, cap] is reported as CC_ERR_DEVICE_ARG and taken as 0.  An entry
  * of keep_idx out of order or range is reported; what its sequence's slots then hold is
- * unspecified.  A block-table entry outside the pool is reported and the slots that come
- * from its page or go to it stay as they are.  A page belongs to one sequence: no two
- * entries for held slots may name the same one. */
+ * unspecified.  A block-table entry outside the pool is reported: K and V of the slots that
+ * would come from its page stay where they are (their own source, brought to their block's
+ * new scale like the others), those that would go to it are written nowhere.  A page belongs
+ * to one sequence: no two entries for held slots may name the same one. */
 size_t cc_kv_compact_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *cache);
 cc_status cc_kv_compact(const cc_model_cfg *cfg, const cc_kv_cache *cache, const int32_t *keep_idx,
                         const int32_t *keep_count, void *ws, size_t ws_bytes, void *stream);

@@ -249,8 +249,10 @@ __global__ void __launch_bounds__(kThreads, kResident) compact_kernel(const __gr
       const int s = next_s < k0 + tid || next_s >= p.cap ? k0 + tid : next_s;   // (as source_of)
       row = paged ? (int)kv_row(p.pg, p.cap, b, s) : seq_row + s;
       if (row < 0 || to < 0) {
-        set_status(p.status, CC_ERR_DEVICE_ARG);   // no such page: the slot stays
-        row = -1;
+        // no such page: the destination's is not written; without the source's the slot is its own
+        // source, whose codes come to its block's new scale as the others' do
+        set_status(p.status, CC_ERR_DEVICE_ARG);
+        row = to < 0 ? -1 : to + tid;
       }
     }
     src_sh[tid] = row;
