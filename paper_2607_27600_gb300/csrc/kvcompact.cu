@@ -130,8 +130,9 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
   const int J = kept_of(p, b), n = p.seq_len[b];
   const int32_t *idx = p.keep_idx + (size_t)b * p.cap;
   int *reader = p.reader + (size_t)b * p.reader_ld;
-  for (int k = blockIdx.x * kPlanThreads + threadIdx.x; k < J; k += gridDim.x * kPlanThreads) {
-    const int s = idx[k], before = k > 0 ? idx[k - 1] : -1;
+  // (unsigned: the last steps pass 2^31)
+  for (unsigned at = blockIdx.x * kPlanThreads + threadIdx.x; at < (unsigned)J; at += gridDim.x * kPlanThreads) {
+    const int k = (int)at, s = idx[k], before = k > 0 ? idx[k - 1] : -1;
     if (s < k || s >= n || s <= before || n > p.cap) set_status(p.status, CC_ERR_DEVICE_ARG);
     const int c = source_of(p, idx, k) / kCompactChunk;
     for (int u = k > 0 ? source_of(p, idx, k - 1) / kCompactChunk + 1 : 0; u <= c; ++u) reader[u] = k;
