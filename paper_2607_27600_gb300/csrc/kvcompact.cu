@@ -13,8 +13,8 @@
 // blocks) of 128 bytes of one array's slots: a head or two, which have their own scales
 // and depend on nothing else.  It
 //   1. copies its sources to shared memory (cp.async) with their exponents,
-//   2. publishes that they are read,
-//   3. waits (bounded) for the lower units of its array and heads that read from its
+//   2. publishes that they are read (release),
+//   3. waits (acquire, bounded) for the lower units of its array and heads that read from its
 //      destinations, which a pre-pass finds from keep_idx, and
 //   4. rescales and writes.
 // Units are numbered sequence by sequence, slots ascending, the arrays and heads of
@@ -24,11 +24,11 @@
 //
 // Bound by HBM: kept codes are read once and written once.  Ten small CTAs an SM hide
 // a unit's chain of loads (indices, exponents and codes, flags).  32 layers of 16384 slots to
-// 4096, 8 heads of 128: 105 us, 5.1 TB/s; six ragged sequences that keep nearly all, 4 layers:
-// 135 us, 4.1 TB/s, some 18 us of it waits for lower units, of which few layers leave
-// little else to do; 4 layers of 131072 slots to 8192: 31 us, 2.2 TB/s: a chain of the pre-pass
-// and one unit a CTA.  Measured slower: a second buffer, so that the next unit's codes come
-// during a unit's waits (fewer CTAs fit).
+// 4096, 8 heads of 128: 108 us, 5.0 TB/s; six ragged sequences that keep nearly all, 4 layers:
+// 155 us, 3.6 TB/s: each unit waits for the one before and its release (20 us of it), of which few layers
+// leave little else to do; 4 layers of 131072 slots to 8192: 32 us, 2.1 TB/s: a chain of the pre-pass
+// and one or two units a CTA.  Measured slower: a second buffer, so that the next unit's codes come
+// during a unit's waits (fewer CTAs fit); the release by another warp than the one that waits (the same).
 #include "kvcompact.cuh"
 
 #include <algorithm>
@@ -47,15 +47,18 @@ constexpr int kStays = -1, kNoFall = 256;   // falls of a slot that is not writt
 constexpr uint32_t kNanCodes = 0x7F7F7F7Fu;
 constexpr int kSharedBatch = 512;    // sequences whose first chunks fit in shared memory
 
-// Flags by relaxed accesses.  A unit's sources have arrived in shared memory before its flag is
-// stored, and a unit stores nothing before it has seen the flags, so that neither needs an
-// order among other accesses; a release would wait for the last unit's stores as well.
-CC_DEV void st_flag(unsigned *p) {
-  asm volatile("st.relaxed.gpu.global.u32 [%0], %1;" ::"l"(p), "r"(1u) : "memory");
+// A unit's reads of its sources come before the writes of the units that wait for its flag by
+// release and acquire.  A release waits for the stores of the CTA's last unit too, so that a
+// unit none of whose sources can be overwritten stores its flag relaxed: there is nothing to
+// order.  Released and always relaxed: 32 layers of 16384 slots to 4096 108 and 105 us (always
+// released 115), six ragged sequences that keep nearly all 154 and 135.
+CC_DEV void st_flag(unsigned *p, bool release) {
+  if (release) asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p), "r"(1u) : "memory");
+  else asm volatile("st.relaxed.gpu.global.u32 [%0], %1;" ::"l"(p), "r"(1u) : "memory");
 }
 CC_DEV unsigned ld_flag(const unsigned *p) {
   unsigned v;
-  asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
   return v;
 }
 CC_DEV bool wait_flag(const unsigned *flag, unsigned *status) {
@@ -246,8 +249,10 @@ __global__ void __launch_bounds__(kThreads, kResident) compact_kernel(const __gr
     const int to = paged ? (int)kv_row(p.pg, p.cap, b, k0) : seq_row + k0;
     // ---- the slots' rows
     int row = -1;
+    bool later = false;   // the source, or its block's exponent, is a later chunk's to write
     if (tid < rows) {
       const int s = next_s < k0 + tid || next_s >= p.cap ? k0 + tid : next_s;   // (as source_of)
+      later = s >= k0 + C && s < (J + C - 1) / C * C;
       row = paged ? (int)kv_row(p.pg, p.cap, b, s) : seq_row + s;
       if (row < 0 || to < 0) {
         // no such page: the destination's is not written; without the source's the slot is its own
@@ -307,10 +312,10 @@ __global__ void __launch_bounds__(kThreads, kResident) compact_kernel(const __gr
     }
     enter();
     copy_wait_all();
-    __syncthreads();
+    const bool awaited = __syncthreads_or(later);
     // ---- 2. published; 3. the units that read from the destinations, and meanwhile the falls
     if (tid < 32) {
-      if (tid == 0) st_flag(flags + (size_t)c * p.planes);
+      if (tid == 0) st_flag(flags + (size_t)c * p.planes, awaited);
       bool go = true;
       for (int r = r_lo + lane; r <= r_hi; r += 32) go &= wait_flag(flags + (size_t)r * p.planes, p.status);
       go = __all_sync(0xFFFFFFFFu, go);
