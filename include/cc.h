@@ -506,7 +506,8 @@ cc_status cc_kv_append(const cc_model_cfg *cfg, const cc_kv_cache *cache, int32_
  * not by what is held: 4 * Hkv * head_dim bytes for each of batch * cap slots.  There
  * a bf16 row's probabilities are rounded to bf16 before they weigh the values (scores
  * past 2^30 are out of its range); the other kernel rounds them to fp16.  An fp16
- * row's are two such parts in either. */
+ * row's are two such parts in either.  The other kernel rounds small elements of q as
+ * cc_kv_accumulate does. */
 size_t cc_kv_attention_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *cache,
                                       const cc_rows *rows);
 cc_status cc_kv_attention(const cc_model_cfg *cfg, const cc_kv_cache *cache, int32_t layer,
@@ -549,8 +550,10 @@ cc_status cc_kv_join(const cc_model_cfg *cfg, cc_dtype dtype, int32_t n_rows, in
  * Chunks take tiles by the rule for bf16 of cc_kv_attention (up to 96 query heads
  * per KV head; one kernel for the whole call), whose workspace goes by room: 8 * Hkv
  * bytes for each of batch * cap slots.  There q . K is summed before K's scale: it
- * must not pass 2^128.  Other rows need next to none.  At most 2^31 - 4097 slots
- * a sequence (more: CC_ERR_UNSUPPORTED), as in cc_kv_compact. */
+ * must not pass 2^128.  Other rows need next to none; of these, elements of q more than
+ * 2^24 (fp16: 2^21) below the largest of their row and head are rounded, by at most
+ * 2^-32 of that one.  At most 2^31 - 4097 slots a sequence (more: CC_ERR_UNSUPPORTED),
+ * as in cc_kv_compact. */
 size_t cc_kv_accumulate_workspace_size(const cc_model_cfg *cfg, const cc_kv_cache *cache,
                                        const cc_rows *rows);
 cc_status cc_kv_accumulate(const cc_model_cfg *cfg, const cc_kv_cache *cache, int32_t layer,

@@ -8,8 +8,9 @@
 // above, so that the largest 2^(x + lv - mv) fills fp16, in which the
 // probabilities meet the codes (exact in fp16) on the tensor cores.  Both are
 // whole numbers: every rescaling is by a power of two.  mv is held as dv = mv - m, which
-// stays exact where scores are past 2^24.  Queries are scaled by a
-// power of two per row so that bf16 ones fit fp16 exactly; sums are fp32.  A bf16 row's
+// stays exact where scores are past 2^24.  Queries come to fp16 scaled by a
+// power of two per row: exact but for elements more than 2^24 (fp16 rows: 2^21) below the row's
+// largest, which are off by at most 2^-32 of that one; sums are fp32.  A bf16 row's
 // probabilities are one fp16 each (out against 64 bits 0.00165, with fp32 ones 0.00163).
 //
 // Bound by the cache's bytes: a tcgen05 tile of 128 query rows would be

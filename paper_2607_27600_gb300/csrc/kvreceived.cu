@@ -12,8 +12,9 @@
 // sums in registers.  A warp takes 16 slots of all heads, each lane 32 bytes of a slot's
 // 128 straight into the registers that the products read (which element of a row meets
 // which k index is free as long as Q agrees), several heads ahead.  The queries of a
-// share's sequence lie in shared memory as operands, scaled by a power of two per row so
-// that bf16 ones fit fp16 exactly.
+// share's sequence lie in shared memory as fp16 operands, scaled by a power of two per row and head:
+// exact but for elements more than 2^24 (fp16 rows: 2^21) below the largest, which are off by at
+// most 2^-32 of that one.
 //
 // 64 sequences of 1500 to 32767 slots, a row each of 32 heads of 128 on 8: 213 us, 5.3 TB/s
 // of codes and exponents; 16 sequences of 250 to 9001, five rows each: 33 us, 2.4 TB/s: too short for
