@@ -527,8 +527,9 @@ cc_status cc_kv_attention(const cc_model_cfg *cfg, const cc_kv_cache *cache, int
  *     part_ld[i] elements apart, and device fp32 [n_rows][Hq];
  *   out, lse: as a part; lse may be NULL.  Either may lie exactly where one of the
  *     parts (its lse) does, with the same pitch, and must not overlap them otherwise.
- * A part whose lse is -inf saw no slot and is not looked at; a row and head with only
- * such gets 0 and -inf.  One whose lse is NaN or +inf in any part gets 0 and NaN. */
+ * A part whose lse is -inf saw no slot and is not looked at, nor is one whose weight is 0 in
+ * fp32 (some 103 below the largest lse); a row and head with only -inf gets 0 and -inf.
+ * One whose lse is NaN or +inf in any part gets 0 and NaN. */
 cc_status cc_kv_join(const cc_model_cfg *cfg, cc_dtype dtype, int32_t n_rows, int32_t n_parts,
                      const void *const *part, const int64_t *part_ld, const float *const *part_lse,
                      void *out, int64_t out_ld, float *lse, void *stream);

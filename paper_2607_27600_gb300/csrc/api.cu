@@ -2138,7 +2138,9 @@ KvReceivedParams kv_received_params(const cc_model_cfg *c, const cc_kv_cache *kv
 // Whether a step's rows take the tiles: by the attention's rule for bf16, for either type (the
 // products are of one fp16 or bf16 operand each).  Direct and tiles, 8192 slots: 8 sequences
 // of 16/4 heads: 80 rows of a KV head 34 and 44 us, 96 rows 44 and 42; one sequence of 28/4:
-// 56 rows 13 and 15, 84 rows 19 and 15.
+// 56 rows 13 and 15, 84 rows 19 and 15.  One kernel for the whole call: a chunk among many single rows is
+// slow on either.  63 single rows after 8192 slots, 32/8 heads, 113 us; with a chunk of 500 (49 us by
+// itself) 7300 on the direct kernel, with one of 2048 (138) 736 on tiles.
 bool received_on_tiles(const cc_model_cfg *c, const cc_kv_cache *kv, const cc_rows *rows) {
   return c->n_q_heads / c->n_kv_heads <= kReceivedMaxGroup && step_on_tiles(c, kv, rows, false);
 }

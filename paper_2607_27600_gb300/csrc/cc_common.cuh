@@ -194,9 +194,11 @@ CC_DEV uint64_t make_policy_evict_first() {
 // Rules that keep a chain of such kernels ordered as a stream is:
 //   - every CTA executes pdl_wait before it exits, so a grid completes only
 //     after all grids before it have;
-//   - a kernel touches nothing before pdl_wait but weights (the few-row GEMM's
-//     first tiles), which no kernel of a call writes; each API call with such
-//     a kernel begins with a plain launch, which waits for whatever wrote them.
+//   - a kernel touches nothing before pdl_wait but what no earlier kernel of its
+//     call writes: weights (the few-row GEMM's first tiles); the lengths, row
+//     bounds and totals that the join of the attention received from chunks starts
+//     from.  Each API call with such a kernel begins with a plain launch, which
+//     waits for whatever wrote them.
 CC_DEV void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 CC_DEV void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

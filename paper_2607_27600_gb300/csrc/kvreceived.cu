@@ -17,7 +17,7 @@
 // most 2^-32 of that one.
 //
 // 64 sequences of 1500 to 32767 slots, a row each of 32 heads of 128 on 8: 213 us, 5.3 TB/s
-// of codes and exponents; 16 sequences of 250 to 9001, five rows each: 33 us, 2.4 TB/s: too short for
+// of codes and exponents; 16 sequences of 250 to 9001, five rows each: 33 us, 2.3 TB/s: too short for
 // more, and with 24 columns of scores 16 warps an SM instead of 24.  Bound by the latency of
 // the loads (long scoreboard first among the stalls, DRAM busy 67 % at 32 sequences).
 #include "kvreceived.cuh"

@@ -20,10 +20,12 @@
 //   warp 18          query tiles (TMA)
 //   warp 19          the rows' terms
 //
-// A chunk of 2048 rows behind 16384 slots, 32 query heads of 128 on 8: 241 us (1.2 PFLOP/s:
-// products alone take 150 us, tensor pipe and exponentials each busy half of the time,
-// instructions issued in 63 % of it).  What is left is the slots' warps: without their
-// arithmetic a tile's hand-overs between the roles still take 215 us.
+// A chunk of 2048 rows behind 14336 slots, 32 query heads of 128 on 8: 221 us (1.17 PFLOP/s).  One
+// behind 16384 slots took 241 us when the products alone took 150, tensor pipe and
+// exponentials each busy half of the time, instructions issued in 63 % of it; without the slots'
+// warps' arithmetic the hand-overs of a tile between the roles still took 215 us.
+// A score's k steps are one chain of products: totals are 3.6e-7 off (300 fp16 rows of 28/4 heads 6.4e-7),
+// where two chains a score keep few rows (kvreceived.cu) below 1.4e-6 and plain fp32 gives 2e-7.
 // Measured slower: weights of a tile's 96 columns by every other four warps (277 us; a buffer
 // of scores is held for longer), scores taken 16 columns at a time (298), the next unit's codes
 // fetched ahead (the same).
@@ -49,7 +51,7 @@ constexpr int kRegsSlots = 104, kRegsOthers = 64;
 static_assert(4 * kRegsSlots + kRegsOthers <= 5 * 96, "more registers than the block is launched with");
 // Of a unit's start, in query tiles; and of one that some rows do not see, whose masked tiles take longer.
 // (With 3 for both the last shares end 10 % behind the others: 276 against 250 us for a chunk of 2048 rows
-// behind 16384 slots, 32 query heads on 8.)
+// behind 16384 slots, 32 query heads of 128 on 8: the only shape at which the two were chosen.)
 constexpr int kUnitCost = 5, kEdgeCost = 7;
 
 template <int DH>
